@@ -301,6 +301,57 @@ lasgd_status lasgd_set_elastic(lasgd_ctx *ctx, float alpha, float beta);
  */
 lasgd_status lasgd_sgd_ar_step(lasgd_ctx *ctx, float lr);
 
+/* ---- gradient norms and clipping ------------------------------------------------
+ *
+ * Every replica is a worker with gradients of its own, so each has a norm of its own over its whole parameter list,
+ *     n_k = sqrt(sum over all tensors and elements of g[k]^2),
+ * and clipping to max_norm scales its gradients by c_k = min(1, max_norm / (n_k + LASGD_CLIP_EPS)).  Norms are summed in
+ * fp64 from the elements on, in a fixed order (the same gradients give the same bits), and rounded to fp32 once.  c_k is rounded to
+ * fp32 once, and so is c_k g (in place: to the storage type).  c_k = 1 leaves every bit as it is.
+ *
+ * A norm is not finite exactly when one of the gradients is an infinity or a NaN.  With skip_nonfinite such a replica
+ * sits out what the call does with its gradients: clip_grads leaves them as they are, a step leaves x and v as they are (it
+ * still takes part in a global update of the same call).  Without, the formulas above are followed as they stand: after an infinity
+ * c_k is 0 (and 0 times infinity NaN), after a NaN it is NaN.
+ *
+ * All of it runs on the main stream, also the norms; ordering against the stream the gradients were made on is the caller's,
+ * as for every step.  The first of these calls asks for a little device memory that it needs between its kernels (8 KiB a replica),
+ * lasgd_sgd_ar_step_clip also for the mean gradient's array; a call that finds none returns ALLOC and enqueues nothing.  The clipped updates
+ * take tiles of 256 elements whatever lasgd_tuning.vec says.
+ */
+#define LASGD_CLIP_EPS 1e-6
+
+typedef struct {
+    float max_norm;         /* >= 0; infinity: nothing is scaled, norms are taken and skip_nonfinite holds    */
+    int32_t skip_nonfinite; /* != 0: replicas whose norm is not finite sit out, see above                      */
+    float *norms;           /* device [K], 4-byte aligned, or NULL: n_k is written for the replicas that take part,
+                               the other entries stay (lasgd_sgd_ar_step_clip: [1])                              */
+} lasgd_clip;
+
+/* norms[k] <- n_k for the replicas in `mask` (non-empty); norms: device [K].  The parameters and the state are not touched.
+ * Errors: INVALID (NULL, misaligned, bad mask), STATE (a replica is unbound), ALLOC, HIP. */
+lasgd_status lasgd_grad_norms(lasgd_ctx *ctx, uint64_t mask, float *norms);
+
+/* g[k] <- c_k g[k], in place, for the replicas in `mask` (non-empty), for callers whose update is not one of this library's or who want to
+ * look at the clipped gradients; the clipped updates below do not need it, and move less.  Gradients with c_k = 1 are not written.
+ * Errors: as lasgd_grad_norms, plus INVALID for a NULL clip or a max_norm that is negative or NaN. */
+lasgd_status lasgd_clip_grads(lasgd_ctx *ctx, uint64_t mask, const lasgd_clip *clip);
+
+/* lasgd_local_step_ex with c_k g[k] in the place of g[k]; the gradients are only read.  fp32 storage: exactly lasgd_clip_grads and
+ * lasgd_local_step_ex, same roundings; bf16 storage: c_k g[k] stays in fp32.
+ * Errors: as lasgd_local_step_ex, plus INVALID as lasgd_clip_grads, and ALLOC. */
+lasgd_status lasgd_local_step_clip(lasgd_ctx *ctx, const float *lr, uint64_t mask, const lasgd_clip *clip);
+
+/* lasgd_step_merge_ex with clipped gradients in the local update of the replicas in step_mask.
+ * Errors: as lasgd_step_merge_ex, plus INVALID as lasgd_clip_grads, and ALLOC. */
+lasgd_status lasgd_step_merge_clip(lasgd_ctx *ctx, const float *lr, uint64_t step_mask, uint64_t merge_mask,
+                                   int32_t resnapshot, const lasgd_clip *clip);
+
+/* lasgd_sgd_ar_step with the mean gradient clipped: one norm, that of the mean gradient, one c, and (skip_nonfinite) all replicas
+ * sit out together.  norms: device [1].
+ * Errors: as lasgd_sgd_ar_step, plus INVALID as lasgd_clip_grads, and ALLOC. */
+lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *ctx, float lr, const lasgd_clip *clip);
+
 /*
  * Parity probe: wait for both streams, then copy one array to host memory as
  * fp32.  tensor >= 0: that tensor of replica k, n must equal numel[tensor];

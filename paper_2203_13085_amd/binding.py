@@ -28,7 +28,8 @@ EXPORTS = ["lasgd_create", "lasgd_bind", "lasgd_init_master", "lasgd_local_step"
            "lasgd_last_error", "lasgd_destroy", "lasgd_local_step_ex", "lasgd_snapshot_ex",
            "lasgd_average_ex", "lasgd_merge_ex", "lasgd_step_merge_ex", "lasgd_set_elastic",
            "lasgd_sgd_ar_step", "lasgd_global_update_static", "lasgd_step_merge_average",
-           "lasgd_zero_grads"]
+           "lasgd_zero_grads", "lasgd_grad_norms", "lasgd_clip_grads", "lasgd_local_step_clip",
+           "lasgd_step_merge_clip", "lasgd_sgd_ar_step_clip"]
 
 
 class LasgdError(RuntimeError):
@@ -43,6 +44,10 @@ class Config(ctypes.Structure):
                 ("momentum", ctypes.c_float), ("nesterov", ctypes.c_int32),
                 ("weight_decay", ctypes.POINTER(ctypes.c_float)), ("wd_scalar", ctypes.c_float),
                 ("main_stream", ctypes.c_void_p), ("side_stream", ctypes.c_void_p)]
+
+
+class Clip(ctypes.Structure):
+    _fields_ = [("max_norm", ctypes.c_float), ("skip_nonfinite", ctypes.c_int32), ("norms", ctypes.c_void_p)]
 
 
 class Tuning(ctypes.Structure):
@@ -93,6 +98,12 @@ def load() -> ctypes.CDLL:
     L.lasgd_set_elastic.argtypes = [P, f32, f32]
     L.lasgd_sgd_ar_step.argtypes = [P, f32]
     L.lasgd_global_update_static.argtypes = [i32, i64, ctypes.POINTER(P), ctypes.POINTER(P), i32, P]
+    clip = ctypes.POINTER(Clip)
+    L.lasgd_grad_norms.argtypes = [P, u64, P]
+    L.lasgd_clip_grads.argtypes = [P, u64, clip]
+    L.lasgd_local_step_clip.argtypes = [P, f32p, u64, clip]
+    L.lasgd_step_merge_clip.argtypes = [P, f32p, u64, u64, i32, clip]
+    L.lasgd_sgd_ar_step_clip.argtypes = [P, f32, clip]
     L.lasgd_last_error.argtypes = [P]
     L.lasgd_last_error.restype = ctypes.c_char_p
     L.lasgd_destroy.argtypes = [P]
@@ -234,6 +245,33 @@ class Context:
 
     def sgd_ar_step(self, lr: float) -> None:
         self._check(self._L.lasgd_sgd_ar_step(self._h, lr))
+
+    # -- gradient norms and clipping: `norms` is a device address ([K] floats; sgd_ar_step_clip: one), masks default to all replicas
+    def _mask(self, mask: Optional[int]) -> int:
+        return (1 << self.K) - 1 if mask is None else mask
+
+    def grad_norms(self, norms: int, mask: Optional[int] = None) -> None:
+        self._check(self._L.lasgd_grad_norms(self._h, self._mask(mask), norms or None))
+
+    def clip_grads(self, max_norm: float, mask: Optional[int] = None, *, skip_nonfinite: bool = False,
+                   norms: Optional[int] = None) -> None:
+        c = Clip(max_norm, skip_nonfinite, norms or None)
+        self._check(self._L.lasgd_clip_grads(self._h, self._mask(mask), ctypes.byref(c)))
+
+    def local_step_clip(self, lr, max_norm: float, mask: Optional[int] = None, *, skip_nonfinite: bool = False,
+                        norms: Optional[int] = None) -> None:
+        c = Clip(max_norm, skip_nonfinite, norms or None)
+        self._check(self._L.lasgd_local_step_clip(self._h, self._lrs(lr), self._mask(mask), ctypes.byref(c)))
+
+    def step_merge_clip(self, lr, max_norm: float, step_mask: Optional[int] = None, merge_mask: Optional[int] = None,
+                        resnapshot: bool = True, *, skip_nonfinite: bool = False, norms: Optional[int] = None) -> None:
+        c = Clip(max_norm, skip_nonfinite, norms or None)
+        self._check(self._L.lasgd_step_merge_clip(self._h, self._lrs(lr), self._mask(step_mask), self._mask(merge_mask),
+                                                  int(resnapshot), ctypes.byref(c)))
+
+    def sgd_ar_step_clip(self, lr: float, max_norm: float, *, skip_nonfinite: bool = False, norms: Optional[int] = None) -> None:
+        c = Clip(max_norm, skip_nonfinite, norms or None)
+        self._check(self._L.lasgd_sgd_ar_step_clip(self._h, lr, ctypes.byref(c)))
 
     def read_state(self, which: int, k: int = 0, tensor: int = -1) -> np.ndarray:
         # an out-of-range tensor index is the library's to refuse

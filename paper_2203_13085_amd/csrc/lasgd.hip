@@ -11,6 +11,7 @@
 // The state machine refuses call orders in which s or z could be overwritten
 // while the other stream may still read them.
 #include "lasgd_kernels.hip.h"
+#include "lasgd_clip.hip.h"
 #include "../../include/lasgd.h"
 
 #include <cmath>
@@ -57,6 +58,9 @@ struct lasgd_ctx {
     float *v = nullptr, *s = nullptr, *z = nullptr, *x32 = nullptr;
     float *gbar = nullptr;           // mean gradient [npad] of an SGD All-Reduce step in two kernels, see reserve_mean_grad
     bool gbar_tried = false;         // asked for; without it the step always takes one kernel
+    char *norm_mem = nullptr;        // what the clipped calls keep between their kernels, see reserve_norms
+    double *norm_part = nullptr;     // [K][kNormParts]
+    Clip *clip = nullptr;            // [K]
     // one set of lookup tables per tile size ever used (vec = 1, 2, 4), kept until destroy: a graph captured
     // under one tile size still points at its tables after the tile size has been changed
     struct Tables {
@@ -331,6 +335,29 @@ hipError_t launch_nt(const ApplyArgs &a, const ExtArgs *xa, dim3 grid, dim3 bs, 
     return hipGetLastError();
 }
 
+template <int OP, bool BF16>
+hipError_t launch_clip(const ApplyArgs &a, const ExtArgs &xa, const Clip *clip, dim3 grid, dim3 bs, hipStream_t st, int nt)
+{
+    const uint32_t lds = pace_lds(OP, BF16, &xa, nt, 1, bs.x / 64u, all_at_s(a));
+    if constexpr (OP == OP_STEP_MERGE) {
+        if (nt == 7) {
+            hipLaunchKernelGGL((apply_clip_kernel<OP, BF16, 7>), grid, bs, lds, st, a, xa, clip);
+            return hipGetLastError();
+        }
+    }
+    if (nt & 3) hipLaunchKernelGGL((apply_clip_kernel<OP, BF16, 3>), grid, bs, lds, st, a, xa, clip);
+    else hipLaunchKernelGGL((apply_clip_kernel<OP, BF16, 0>), grid, bs, lds, st, a, xa, clip);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t launch_mean_clip(const ApplyArgs &a, const Clip *clip, dim3 grid, dim3 bs, hipStream_t st, int nt)
+{
+    if (nt & 3) hipLaunchKernelGGL((step_mean_clip_kernel<BF16, 3>), grid, bs, pace_lds(OP_STEP_MEAN, BF16, nullptr, nt, 1, bs.x / 64u, false), st, a, clip);
+    else hipLaunchKernelGGL((step_mean_clip_kernel<BF16, 0>), grid, bs, 0, st, a, clip);
+    return hipGetLastError();
+}
+
 // Streaming and in tiles of 256 elements only.
 template <int OP, bool BF16>
 hipError_t launch_one(const ApplyArgs &a, dim3 grid, dim3 bs, hipStream_t st)
@@ -376,6 +403,16 @@ void fill_common(const lasgd_ctx *c, ApplyArgs &a)
     a.k_as_double = (double)c->K;
 }
 
+// Tiles of 256 elements, whose tables every context has from its beginning.
+void fill_fine(const lasgd_ctx *c, ApplyArgs &a)
+{
+    const lasgd_ctx::Tables &t = c->tables_by_vec[0];
+    a.blocks = t.blocks;
+    a.tile0 = t.tile0;
+    a.ntiles = t.ntiles;
+    a.tile_elems = 256u;
+}
+
 // A multi-tensor pass, planned (arguments, grid; everything that can be refused)
 // and then launched on the main stream.  Callers plan before they enqueue any
 // stream dependency, so that a refused call leaves both streams untouched.
@@ -385,14 +422,17 @@ struct ApplyPlan {
     dim3 grid{1}, bs{64};
     bool has_ext = false;
     ExtArgs ext{};
+    const Clip *clip = nullptr;      // the clipped form, which takes tiles of 256 elements whatever the tuning says
 };
 
 // xa == nullptr: every replica takes part, one step size, alpha = 1 (the plain kernels).
-lasgd_status plan_apply(lasgd_ctx *c, ApplyPlan &p, int op, float lr, int resnap, const ExtArgs *xa = nullptr)
+lasgd_status plan_apply(lasgd_ctx *c, ApplyPlan &p, int op, float lr, int resnap, const ExtArgs *xa = nullptr, const Clip *clip = nullptr)
 {
     if (op < OP_STEP || op > OP_STEP_MEAN) return fail(c, LASGD_ERR_INVALID, "unknown op %d", op);
     ApplyArgs &a = p.a;
     fill_common(c, a);
+    p.clip = clip;
+    if (clip) fill_fine(c, a);
     int kper = (op == OP_MERGE || op == OP_STEP_MERGE || op == OP_STEP_MEAN) ? c->tune.kper_merge : c->tune.kper_step;
     const int taking = xa ? __builtin_popcountll(xa->step_mask | xa->merge_mask) : c->K;
     if (kper < 1) kper = 1;
@@ -536,12 +576,16 @@ lasgd_status launch_apply(lasgd_ctx *c, ApplyPlan &p)
     const lasgd_status st = place_models(c, &p.a, writes ? taking : 0, p.op == OP_SNAPSHOT);
     if (st != LASGD_OK) return st;
     backwards(c, p.a, p.a.wpb);
-    const int vec = c->tune.vec;
-    int nt = hint_of(c, p.op == OP_STEP && c->fused_cycle ? USE_FUSED : USE_CYCLE);
+    const int vec = p.clip ? 1 : c->tune.vec;
+    int nt = hint_of(c, p.op == OP_STEP && c->fused_cycle ? USE_FUSED : p.clip && p.op == OP_STEP_MEAN ? USE_SGD_AR : USE_CYCLE);
     if (nt == 3 && vec == 1 && word_first(p.op, (uint64_t)c->K * c->npad, all_at_s(p.a))) nt |= 4;
     const ExtArgs *xa = p.has_ext ? &p.ext : nullptr;
     hipError_t e = hipSuccess;
-    switch (p.op) {
+    if (p.clip) {
+        if (p.op == OP_STEP_MEAN) e = bf16 ? launch_mean_clip<true>(p.a, p.clip, p.grid, p.bs, c->main, nt) : launch_mean_clip<false>(p.a, p.clip, p.grid, p.bs, c->main, nt);
+        else if (p.op == OP_STEP) e = bf16 ? launch_clip<OP_STEP, true>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt) : launch_clip<OP_STEP, false>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt);
+        else e = bf16 ? launch_clip<OP_STEP_MERGE, true>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt) : launch_clip<OP_STEP_MERGE, false>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt);
+    } else switch (p.op) {
     case OP_STEP: e = launch_op<OP_STEP>(p.a, xa, p.grid, p.bs, c->main, vec, nt, bf16); break;
     case OP_MERGE: e = launch_op<OP_MERGE>(p.a, xa, p.grid, p.bs, c->main, vec, nt, bf16); break;
     case OP_STEP_MERGE: e = launch_op<OP_STEP_MERGE>(p.a, xa, p.grid, p.bs, c->main, vec, nt, bf16); break;
@@ -799,6 +843,7 @@ void release(lasgd_ctx *c)
         if (t.mem) (void)hipFree(t.mem);
     if (c->records) (void)hipFree(c->records);
     if (c->gbar) (void)hipFree(c->gbar);
+    if (c->norm_mem) (void)hipFree(c->norm_mem);
     if (c->evA) (void)hipEventDestroy(c->evA);
     if (c->evZ) (void)hipEventDestroy(c->evZ);
     delete c;
@@ -985,7 +1030,64 @@ static bool fill_ext(const lasgd_ctx *c, ExtArgs &x, const float *lr, uint64_t s
     return uniform;
 }
 
-static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uint64_t mask)
+// ---- gradient norms and clipping -------------------------------------------
+
+// What the kernels of a call hand on: the parts of each sum, and what comes of each norm.  For those alone that make the calls it is for; the
+// first of them asks, before it enqueues anything, also while it is being recorded.
+constexpr uint32_t kNormParts = 1024;
+static lasgd_status reserve_norms(lasgd_ctx *c)
+{
+    if (c->norm_mem) return LASGD_OK;
+    const size_t parts = (size_t)c->K * kNormParts * sizeof(double);
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;        // allowed while a stream of this thread is being recorded, and not recorded
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+    const hipError_t e = hipMalloc((void **)&c->norm_mem, parts + (size_t)c->K * sizeof(Clip));
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        c->norm_mem = nullptr;
+        return fail(c, LASGD_ERR_ALLOC, "no memory for the gradient norms: %s", hipGetErrorString(e));
+    }
+    c->norm_part = (double *)c->norm_mem;
+    c->clip = (Clip *)(c->norm_mem + parts);
+    return LASGD_OK;
+}
+
+static lasgd_status check_clip(lasgd_ctx *c, const lasgd_clip *clip)
+{
+    if (!clip) return fail(c, LASGD_ERR_INVALID, "NULL clip");
+    if (!(clip->max_norm >= 0.f)) return fail(c, LASGD_ERR_INVALID, "max_norm must be >= 0 (infinity: no limit)");
+    if ((uintptr_t)clip->norms & 3u) return fail(c, LASGD_ERR_INVALID, "norms is not 4-byte aligned");
+    return LASGD_OK;
+}
+
+// Norms of the replicas in `mask`, and (clips) what comes of them, on the main stream.
+static lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, bool clips = true)
+{
+    ApplyArgs a{};
+    fill_common(c, a);
+    fill_fine(c, a);
+    NormArgs n{};
+    n.part = c->norm_part;
+    n.parts = (a.ntiles + 15u) / 16u < kNormParts ? (a.ntiles + 15u) / 16u : kNormParts;
+    n.mask = mask;
+    n.count = (uint32_t)__builtin_popcountll(mask);
+    n.clip = clips ? c->clip : nullptr;
+    n.norms = clip.norms;
+    n.max_norm = clip.max_norm;
+    n.skip_nonfinite = clip.skip_nonfinite;
+    if (c->storage == LASGD_BF16) hipLaunchKernelGGL((grad_norm_kernel<true>), dim3(n.parts, n.count), dim3(kNormThreads), 0, c->main, a, n);
+    else hipLaunchKernelGGL((grad_norm_kernel<false>), dim3(n.parts, n.count), dim3(kNormThreads), 0, c->main, a, n);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) {
+        hipLaunchKernelGGL(finish_norm_kernel, dim3(n.count), dim3(kNormThreads), 0, c->main, n, (uint32_t)c->K);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return LASGD_OK;
+}
+
+static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uint64_t mask, const lasgd_clip *clip = nullptr)
 {
     lasgd_status st = check_ready_to_step(c, lr_k ? 0.f : lr);
     if (st != LASGD_OK) return st;
@@ -995,6 +1097,13 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
     if (!mask) return LASGD_OK;                        // nobody steps: nothing to enqueue
     ExtArgs x{};
     const bool uniform = fill_ext(c, x, lr_k, mask, 0);
+    if (clip) {
+        ApplyPlan p;
+        if ((st = reserve_norms(c)) != LASGD_OK) return st;
+        if ((st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, c->clip)) != LASGD_OK) return st;
+        if ((st = enqueue_norms(c, mask, *clip)) != LASGD_OK) return st;
+        return launch_apply(c, p);
+    }
     if (uniform && mask == c->all) return enqueue_apply(c, OP_STEP, lr_k[0], 0);
     return enqueue_apply(c, OP_STEP, 0.f, 0, &x);
 }
@@ -1055,7 +1164,7 @@ static lasgd_status do_average(lasgd_ctx *c, uint64_t mask)
 }
 
 static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, uint64_t step_mask,
-                             uint64_t merge_mask, int32_t resnapshot)
+                             uint64_t merge_mask, int32_t resnapshot, const lasgd_clip *clip = nullptr)
 {
     lasgd_status st = check_ready_to_step(c, lr_k ? 0.f : lr);
     if (st != LASGD_OK) return st;
@@ -1072,9 +1181,13 @@ static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, 
     const bool plain = merge_mask == c->all && c->alpha == 1.f &&
                        (op == OP_MERGE || (step_mask == c->all && uniform));
     ApplyPlan p;
-    if (plain) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0);
+    if (clip && (st = reserve_norms(c)) != LASGD_OK) return st;
+    if (clip) st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, c->clip);
+    else if (plain) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0);
     else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x);
     if (st != LASGD_OK) return st;
+    // the norms need no z: they are taken while the mean may still be on its way
+    if (clip && step_mask && (st = enqueue_norms(c, step_mask, *clip)) != LASGD_OK) return st;
     // nothing can be refused any more: now the main stream waits for z (unless z is made on this very stream)
     if (!c->z_on_main) LASGD_HIP(c, hipStreamWaitEvent(c->main, c->evZ, 0));
     st = launch_apply(c, p);
@@ -1232,6 +1345,101 @@ lasgd_status lasgd_sgd_ar_step(lasgd_ctx *c, float lr)
     c->at_s = 0;
     if (two && !c->gbar_tried) reserve_mean_grad(c);
     return LASGD_OK;
+}
+
+lasgd_status lasgd_grad_norms(lasgd_ctx *c, uint64_t mask, float *norms)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    if (!norms) return fail(c, LASGD_ERR_INVALID, "NULL norms");
+    const lasgd_clip clip{0.f, 0, norms};
+    lasgd_status st = check_clip(c, &clip);
+    if (st != LASGD_OK) return st;
+    if ((st = check_mask(c, mask, false, "mask")) != LASGD_OK) return st;
+    if (c->n_bound != c->K) return fail(c, LASGD_ERR_STATE, "%d of %d replicas are bound", c->n_bound, c->K);
+    if ((st = reserve_norms(c)) != LASGD_OK) return st;
+    return enqueue_norms(c, mask, clip, false);
+}
+
+lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *clip)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    lasgd_status st = check_clip(c, clip);
+    if (st != LASGD_OK) return st;
+    if ((st = check_mask(c, mask, false, "mask")) != LASGD_OK) return st;
+    if (c->n_bound != c->K) return fail(c, LASGD_ERR_STATE, "%d of %d replicas are bound", c->n_bound, c->K);
+    if ((st = reserve_norms(c)) != LASGD_OK) return st;
+    if ((st = enqueue_norms(c, mask, *clip)) != LASGD_OK) return st;
+    ApplyArgs a{};
+    fill_common(c, a);
+    fill_fine(c, a);
+    NormArgs n{};
+    n.mask = mask;
+    n.count = (uint32_t)__builtin_popcountll(mask);
+    n.clip = c->clip;
+    const dim3 grid(a.ntiles < 8192u ? a.ntiles : 8192u, n.count);
+    if (c->storage == LASGD_BF16) hipLaunchKernelGGL((scale_grads_kernel<true>), grid, dim3(64), 0, c->main, a, n);
+    else hipLaunchKernelGGL((scale_grads_kernel<false>), grid, dim3(64), 0, c->main, a, n);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return LASGD_OK;
+}
+
+lasgd_status lasgd_local_step_clip(lasgd_ctx *c, const float *lr, uint64_t mask, const lasgd_clip *clip)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    if (!lr) return fail(c, LASGD_ERR_INVALID, "NULL learning-rate array");
+    const lasgd_status st = check_clip(c, clip);
+    if (st != LASGD_OK) return st;
+    return do_local_step(c, lr, 0.f, mask, clip);
+}
+
+lasgd_status lasgd_step_merge_clip(lasgd_ctx *c, const float *lr, uint64_t step_mask, uint64_t merge_mask, int32_t resnapshot,
+                                   const lasgd_clip *clip)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    if (!lr) return fail(c, LASGD_ERR_INVALID, "NULL learning-rate array");
+    const lasgd_status st = check_clip(c, clip);
+    if (st != LASGD_OK) return st;
+    return do_merge(c, OP_STEP_MERGE, lr, 0.f, step_mask, merge_mask, resnapshot, clip);
+}
+
+lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *c, float lr, const lasgd_clip *clip)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    lasgd_status st = check_clip(c, clip);
+    if (st != LASGD_OK) return st;
+    if ((st = check_ready_to_step(c, lr)) != LASGD_OK) return st;
+    if (!c->gbar) reserve_mean_grad(c);
+    if (!c->gbar) return fail(c, LASGD_ERR_ALLOC, "no memory for the mean gradient");
+    if ((st = reserve_norms(c)) != LASGD_OK) return st;
+    ApplyPlan p;
+    if ((st = plan_apply(c, p, OP_STEP_MEAN, lr, 0, nullptr, c->clip)) != LASGD_OK) return st;
+    p.a.z = c->gbar;
+    ApplyArgs a = p.a;
+    a.nwaves = a.ntiles;
+    const bool bf16 = c->storage == LASGD_BF16, nt = (hint_of(c, USE_SGD_AR) & 1) != 0;
+    if (bf16 && nt) hipLaunchKernelGGL((mean_grad_kernel<true, 3>), dim3(a.ntiles), dim3(64), 0, c->main, a);
+    else if (bf16) hipLaunchKernelGGL((mean_grad_kernel<true, 0>), dim3(a.ntiles), dim3(64), 0, c->main, a);
+    else if (nt) hipLaunchKernelGGL((mean_grad_kernel<false, 3>), dim3(a.ntiles), dim3(64), 0, c->main, a);
+    else hipLaunchKernelGGL((mean_grad_kernel<false, 0>), dim3(a.ntiles), dim3(64), 0, c->main, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    NormArgs n{};
+    n.part = c->norm_part;
+    n.parts = (a.ntiles + 15u) / 16u < kNormParts ? (a.ntiles + 15u) / 16u : kNormParts;
+    n.mask = 1u;
+    n.count = 1u;
+    n.clip = c->clip;
+    n.norms = clip->norms;
+    n.max_norm = clip->max_norm;
+    n.skip_nonfinite = clip->skip_nonfinite;
+    hipLaunchKernelGGL(flat_norm_kernel, dim3(n.parts), dim3(kNormThreads), 0, c->main, c->gbar, c->packed / 4u, n);
+    if ((e = hipGetLastError()) == hipSuccess) {
+        hipLaunchKernelGGL(finish_norm_kernel, dim3(1), dim3(kNormThreads), 0, c->main, n, 1u);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return launch_apply(c, p);
 }
 
 lasgd_status lasgd_step_merge_average(lasgd_ctx *c, float lr)

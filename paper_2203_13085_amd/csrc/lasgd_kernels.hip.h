@@ -114,6 +114,12 @@ struct ExtArgs {
     float neg_lr_k[64];     // -eta per replica
 };
 
+// What the clipped calls make of a replica's gradient norm: the gradients count times c, and with skip the replica takes no local update.
+struct Clip {
+    float c;
+    uint32_t skip;
+};
+
 // ---- 128-bit / 64-bit accesses, optionally with the streaming hint --------
 // NT: 1 the hint on loads, 2 on stores; 4 belongs to the kernels that ask for a word of their model before their loads.
 // Every pointer the kernels dereference is device (global) memory.  Pointers
@@ -357,10 +363,13 @@ template <bool FULL> __device__ __forceinline__ uint32_t lane_elems(uint32_t e0,
 // there: 4 bytes a replica-parameter fewer per update, 8 where an update follows directly, which then reads s once.  us before /
 // after, over three states in turn: ResNet-18 list K = 12, two fused updates in a row 1405 / 990; ResNet-50 K = 32, an update
 // every eight steps 21617 / 21212.
-template <int VEC, int OP, bool BF16, int NT, bool FULL, bool EXT, bool ALONE, bool AT_S>
+//
+// CLIP: the gradient counts times clip.c (rounded once, as if it had been scaled in place), and a replica to be skipped keeps its model and
+// momentum: written as they were, so that whoever counts on this call having written them finds them.
+template <int VEC, int OP, bool BF16, int NT, bool FULL, bool EXT, bool ALONE, bool AT_S, bool CLIP>
 __device__ __forceinline__ void apply_tile(const ApplyArgs &a, void *xu, const void *gu, const float *xr, float *xm,
                                            float *v, float *s, const float4 (&zt)[VEC], float wd,
-                                           uint32_t count, uint32_t lane, float neg_lr, float alpha)
+                                           uint32_t count, uint32_t lane, float neg_lr, float alpha, Clip clip)
 {
     constexpr bool NEED_G = (OP == OP_STEP || OP == OP_STEP_MERGE);
     constexpr bool STEPS = NEED_G || OP == OP_STEP_MEAN;       // with a gradient of its own, or the mean of all
@@ -431,9 +440,14 @@ __device__ __forceinline__ void apply_tile(const ApplyArgs &a, void *xu, const v
         const uint32_t e = j * 256u + lane * 4u, n = lane_elems<FULL>(e, count);
         if constexpr (AT_S) ss[j] = x[j];
         if constexpr (OP == OP_STEP_MEAN) g[j] = zt[j];
-        if constexpr (STEPS)
-            LASGD_FOR4(step_elem(comp(x[j], c), comp(vv[j], c), compv(g[j], c), wd, a.mu,
-                                 neg_lr, a.nesterov);)
+        if constexpr (STEPS) {
+            if constexpr (CLIP) {
+                if (!clip.skip)
+                    LASGD_FOR4(step_elem(comp(x[j], c), comp(vv[j], c), clip.c * compv(g[j], c), wd, a.mu, neg_lr, a.nesterov);)
+            } else
+                LASGD_FOR4(step_elem(comp(x[j], c), comp(vv[j], c), compv(g[j], c), wd, a.mu,
+                                     neg_lr, a.nesterov);)
+        }
         if constexpr (NEED_S) {
             if constexpr (EXT)
                 LASGD_FOR4(comp(x[j], c) = merge_elem_elastic(compv(x[j], c), compv(ss[j], c), compv(zt[j], c), alpha);)
@@ -494,8 +508,9 @@ template <bool EXT> __device__ __forceinline__ uint32_t replica_at(const ApplyAr
 // per item, items strided over the grid.  All table reads are wave-uniform.
 // The waves of a workgroup are independent (no LDS, no barrier), so the
 // workgroup size (64, 128 or 256 threads) is purely a dispatch-granularity knob.
-template <int VEC, int OP, bool BF16, int NT, bool EXT>
-__device__ __forceinline__ void apply_body(const ApplyArgs &a, const ExtArgs *xa)
+// clip: of each replica, or (OP_STEP_MEAN) the one of them all.
+template <int VEC, int OP, bool BF16, int NT, bool EXT, bool CLIP = false>
+__device__ __forceinline__ void apply_body(const ApplyArgs &a, const ExtArgs *xa, const Clip *clip = nullptr)
 {
     constexpr bool NEED_Z = (OP == OP_MERGE || OP == OP_STEP_MERGE || OP == OP_STEP_MEAN);
     const uint32_t lane = threadIdx.x & 63u;
@@ -564,10 +579,15 @@ __device__ __forceinline__ void apply_body(const ApplyArgs &a, const ExtArgs *xa
             float *xm = BF16 ? a.x32 + ao : nullptr;
             const bool at_s = BF16 && ((in_s >> k) & 1ull);
             const float *xr = at_s ? a.s + ao : xm;
+            Clip cl{1.f, 0u};
+            if constexpr (CLIP) {
+                const LASGD_CONST_AS Clip *p = as_const(clip) + (OP == OP_STEP_MEAN ? 0u : k);
+                cl = Clip{p->c, p->skip};
+            }
 #define LASGD_TILE_AT(OPX, NLR, AL, AT)                                                                      \
     do {                                                                                                     \
-        if (__builtin_expect(full, 1)) apply_tile<VEC, OPX, BF16, NT, true, EXT, OPX == OP, AT>(a, xu, gu, xr, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, NLR, AL); \
-        else apply_tile<VEC, OPX, BF16, NT, false, EXT, OPX == OP, AT>(a, xu, gu, xr, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, NLR, AL);     \
+        if (__builtin_expect(full, 1)) apply_tile<VEC, OPX, BF16, NT, true, EXT, OPX == OP, AT, CLIP>(a, xu, gu, xr, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, NLR, AL, cl); \
+        else apply_tile<VEC, OPX, BF16, NT, false, EXT, OPX == OP, AT, CLIP>(a, xu, gu, xr, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, NLR, AL, cl);     \
     } while (0)
 #define LASGD_TILE(OPX, NLR, AL)                                                                             \
     do {                                                                                                     \
@@ -616,6 +636,20 @@ template <int VEC, int OP, bool BF16, int NT>
 __global__ __launch_bounds__(256) void apply_ext_kernel(const ApplyArgs a, const ExtArgs xa)
 {
     apply_body<VEC, OP, BF16, NT, true>(a, &xa);
+}
+
+// The clipped forms, in tiles of 256 elements: a local step, or a step with the global update, of the replicas in the masks, and a step of
+// all with the mean gradient.
+template <int OP, bool BF16, int NT>
+__global__ __launch_bounds__(256) void apply_clip_kernel(const ApplyArgs a, const ExtArgs xa, const Clip *clip)
+{
+    apply_body<1, OP, BF16, NT, true, true>(a, &xa, clip);
+}
+
+template <bool BF16, int NT>
+__global__ __launch_bounds__(256) void step_mean_clip_kernel(const ApplyArgs a, const Clip *clip)
+{
+    apply_body<1, OP_STEP_MEAN, BF16, NT, false, true>(a, nullptr, clip);
 }
 
 // ---- the mean (Sec. 3, Eq. 8) -----------------------------------------------
