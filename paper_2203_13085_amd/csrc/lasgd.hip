@@ -59,8 +59,10 @@ struct lasgd_ctx {
     float *gbar = nullptr;           // mean gradient [npad] of an SGD All-Reduce step in two kernels, see reserve_mean_grad
     bool gbar_tried = false;         // asked for; without it the step always takes one kernel
     char *norm_mem = nullptr;        // what the clipped calls keep between their kernels, see reserve_norms
-    double *norm_part = nullptr;     // [K][kNormParts]
+    double *norm_part = nullptr;     // [K][kNormParts], or kMeanParts of the mean gradient
     Clip *clip = nullptr;            // [K]
+    uint32_t *arrived = nullptr;     // [K][kArriveStride], zero between calls
+    bool arrived_clear = false;      // it has been cleared, on the main stream and not in a recording
     // one set of lookup tables per tile size ever used (vec = 1, 2, 4), kept until destroy: a graph captured
     // under one tile size still points at its tables after the tile size has been changed
     struct Tables {
@@ -335,27 +337,33 @@ hipError_t launch_nt(const ApplyArgs &a, const ExtArgs *xa, dim3 grid, dim3 bs, 
     return hipGetLastError();
 }
 
-template <int OP, bool BF16>
-hipError_t launch_clip(const ApplyArgs &a, const ExtArgs &xa, const Clip *clip, dim3 grid, dim3 bs, hipStream_t st, int nt)
+template <int OP, bool BF16, int NT>
+hipError_t launch_clip_nt(const ApplyArgs &a, const ExtArgs *xa, const Clip *clip, dim3 grid, dim3 bs, uint32_t lds, hipStream_t st)
 {
-    const uint32_t lds = pace_lds(OP, BF16, &xa, nt, 1, bs.x / 64u, all_at_s(a));
-    if constexpr (OP == OP_STEP_MERGE) {
-        if (nt == 7) {
-            hipLaunchKernelGGL((apply_clip_kernel<OP, BF16, 7>), grid, bs, lds, st, a, xa, clip);
+    if constexpr (OP != OP_STEP_MEAN) {
+        if (xa) {
+            hipLaunchKernelGGL((apply_clip_ext_kernel<OP, BF16, NT>), grid, bs, lds, st, a, *xa, clip);
             return hipGetLastError();
         }
     }
-    if (nt & 3) hipLaunchKernelGGL((apply_clip_kernel<OP, BF16, 3>), grid, bs, lds, st, a, xa, clip);
-    else hipLaunchKernelGGL((apply_clip_kernel<OP, BF16, 0>), grid, bs, lds, st, a, xa, clip);
+    hipLaunchKernelGGL((apply_clip_kernel<OP, BF16, NT>), grid, bs, lds, st, a, clip);
     return hipGetLastError();
 }
 
-template <bool BF16>
-hipError_t launch_mean_clip(const ApplyArgs &a, const Clip *clip, dim3 grid, dim3 bs, hipStream_t st, int nt)
+// Hints all on or all off.
+template <int OP, bool BF16>
+hipError_t launch_clip(const ApplyArgs &a, const ExtArgs *xa, const Clip *clip, dim3 grid, dim3 bs, hipStream_t st, int nt)
 {
-    if (nt & 3) hipLaunchKernelGGL((step_mean_clip_kernel<BF16, 3>), grid, bs, pace_lds(OP_STEP_MEAN, BF16, nullptr, nt, 1, bs.x / 64u, false), st, a, clip);
-    else hipLaunchKernelGGL((step_mean_clip_kernel<BF16, 0>), grid, bs, 0, st, a, clip);
-    return hipGetLastError();
+    const uint32_t lds = pace_lds(OP, BF16, xa, nt, 1, bs.x / 64u, all_at_s(a));
+    if constexpr (OP == OP_STEP_MERGE)
+        if (nt == 7) return launch_clip_nt<OP, BF16, 7>(a, xa, clip, grid, bs, lds, st);
+    return nt & 3 ? launch_clip_nt<OP, BF16, 3>(a, xa, clip, grid, bs, lds, st) : launch_clip_nt<OP, BF16, 0>(a, xa, clip, grid, bs, lds, st);
+}
+
+template <int OP>
+hipError_t launch_clip(const ApplyArgs &a, const ExtArgs *xa, const Clip *clip, dim3 grid, dim3 bs, hipStream_t st, int nt, bool bf16)
+{
+    return bf16 ? launch_clip<OP, true>(a, xa, clip, grid, bs, st, nt) : launch_clip<OP, false>(a, xa, clip, grid, bs, st, nt);
 }
 
 // Streaming and in tiles of 256 elements only.
@@ -582,9 +590,9 @@ lasgd_status launch_apply(lasgd_ctx *c, ApplyPlan &p)
     const ExtArgs *xa = p.has_ext ? &p.ext : nullptr;
     hipError_t e = hipSuccess;
     if (p.clip) {
-        if (p.op == OP_STEP_MEAN) e = bf16 ? launch_mean_clip<true>(p.a, p.clip, p.grid, p.bs, c->main, nt) : launch_mean_clip<false>(p.a, p.clip, p.grid, p.bs, c->main, nt);
-        else if (p.op == OP_STEP) e = bf16 ? launch_clip<OP_STEP, true>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt) : launch_clip<OP_STEP, false>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt);
-        else e = bf16 ? launch_clip<OP_STEP_MERGE, true>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt) : launch_clip<OP_STEP_MERGE, false>(p.a, p.ext, p.clip, p.grid, p.bs, c->main, nt);
+        if (p.op == OP_STEP_MEAN) e = launch_clip<OP_STEP_MEAN>(p.a, nullptr, p.clip, p.grid, p.bs, c->main, nt, bf16);
+        else if (p.op == OP_STEP) e = launch_clip<OP_STEP>(p.a, xa, p.clip, p.grid, p.bs, c->main, nt, bf16);
+        else e = launch_clip<OP_STEP_MERGE>(p.a, xa, p.clip, p.grid, p.bs, c->main, nt, bf16);
     } else switch (p.op) {
     case OP_STEP: e = launch_op<OP_STEP>(p.a, xa, p.grid, p.bs, c->main, vec, nt, bf16); break;
     case OP_MERGE: e = launch_op<OP_MERGE>(p.a, xa, p.grid, p.bs, c->main, vec, nt, bf16); break;
@@ -825,6 +833,135 @@ lasgd_status check_ready_to_step(lasgd_ctx *c, float lr)
     return LASGD_OK;
 }
 
+// ---- gradient norms and clipping -------------------------------------------
+
+// What the kernels of a call hand on: the parts of each sum, and what comes of each norm.  For those alone that make the calls it is for; the
+// first of them asks, before it enqueues anything, also while it is being recorded.
+constexpr uint32_t kNormParts = 768;      // see grad_norm_kernel
+// us at 512 / 1024 / 2048 / 8192 workgroups, all calls: ResNet-50 list K = 8 691 / 692 / 695 / 697, ResNet-18 K = 8 315 / 316 / 316 / 321, MobileNetV2
+// K = 4 48.3 / 51.4 / 54.0 / 62.2, one vector of 2^20, K = 4 15.7 / 18.6 / 18.5 / 18.5.
+constexpr uint32_t kMeanParts = 512;
+uint32_t norm_groups(uint32_t ntiles, uint32_t replicas)      // workgroups for each of them
+{
+    const uint32_t runs = (ntiles + kNormRun - 1u) / kNormRun, most = kNormParts / replicas;
+    return runs < most ? runs : most;
+}
+lasgd_status reserve_norms(lasgd_ctx *c)
+{
+    if (c->norm_mem) return LASGD_OK;
+    const size_t parts = ((size_t)c->K * kNormParts > kMeanParts ? (size_t)c->K * kNormParts : kMeanParts) * sizeof(double);
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;        // allowed while a stream of this thread is being recorded, and not recorded
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+    const hipError_t e = hipMalloc((void **)&c->norm_mem, parts + (size_t)c->K * (sizeof(Clip) + kArriveStride * sizeof(uint32_t)));
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        c->norm_mem = nullptr;
+        return fail(c, LASGD_ERR_ALLOC, "no memory for the gradient norms: %s", hipGetErrorString(e));
+    }
+    c->norm_part = (double *)c->norm_mem;
+    c->arrived = (uint32_t *)(c->norm_mem + parts);
+    c->clip = (Clip *)(c->arrived + (size_t)c->K * kArriveStride);
+    return LASGD_OK;
+}
+
+lasgd_status check_clip(lasgd_ctx *c, const lasgd_clip *clip)
+{
+    if (!clip) return fail(c, LASGD_ERR_INVALID, "NULL clip");
+    if (!(clip->max_norm >= 0.f)) return fail(c, LASGD_ERR_INVALID, "max_norm must be >= 0 (infinity: no limit)");
+    if ((uintptr_t)clip->norms & 3u) return fail(c, LASGD_ERR_INVALID, "norms is not 4-byte aligned");
+    return LASGD_OK;
+}
+
+// Before the first kernel that counts.  A recorded clear runs whenever its graph does, so until one has run by itself every
+// call brings its own.
+hipError_t clear_arrived(lasgd_ctx *c)
+{
+    if (c->arrived_clear) return hipSuccess;
+    hipLaunchKernelGGL(clear_kernel, dim3(1), dim3(64), 0, c->main, c->arrived, (uint32_t)c->K * kArriveStride);
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess && !is_capturing(c->main)) c->arrived_clear = true;
+    return e;
+}
+
+uint32_t mean_norm_groups(uint32_t ntiles)                    // of four waves, each with a tile at a time; whole rows of XCDs
+{
+    const uint32_t all = ((ntiles + 3u) / 4u + 7u) & ~7u;
+    return all < kMeanParts ? all : kMeanParts;
+}
+
+NormArgs norm_args(const lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, uint32_t ntiles)
+{
+    NormArgs n{};
+    n.part = c->norm_part;
+    n.arrived = c->arrived;
+    n.stride = kNormParts;
+    n.mask = mask;
+    n.count = (uint32_t)__builtin_popcountll(mask);
+    n.parts = norm_groups(ntiles, n.count);
+    n.clip = c->clip;
+    n.norms = clip.norms;
+    n.max_norm = clip.max_norm;
+    n.skip_nonfinite = clip.skip_nonfinite;
+    return n;
+}
+
+uint64_t grad_bytes(const lasgd_ctx *c, uint32_t replicas) { return replicas * c->packed * (c->storage == LASGD_BF16 ? 2u : 4u); }
+
+// Gradients are read for their norm and then again.  So many replicas are taken at a time as leave their gradients in the 256 MB memory-side
+// cache until then: from 104 MiB of gradients on two batches or more of one length.  us at so many MB of gradients a batch, all at once last (three
+// states in turn; the unclipped step): ResNet-18 list K = 8 47 342, 94 329, 140 334, 187 353, 374 357 (293); ResNet-50 K = 8 102 736, 204 774, 818 812
+// (631), bf16 K = 32 51 2693, 102 2633, 204 2675, 409 2832, 1636 2891 (2600); MobileNetV2 K = 16 28 215, 56 197, 84 200, 98 201, 112 209, 224 209
+// (172), bf16 K = 32 28 to 112 370, 224 384; six vectors of 20,000,001 80 420, 160 434, 480 454 (373).  In place, everything scaled: ResNet-50 K = 8
+// 102 265, 818 294.  A global update reads z for all replicas of a tile, and in batches it reads z again: ResNet-18 K = 8, with its mean, 94 MB
+// 566, all at once 547, bf16 K = 16 845, 803.  So it takes the norms of all first.
+//
+// A read for the norm goes without the hint where the second one follows soon enough, us without / with: step, MobileNetV2 K = 4 48.8 / 51.6, K = 8
+// 100.9 / 102.1, bf16 K = 16 185 / 197; step + update, with its mean, MobileNetV2 K = 8 (112 MB) 161 / 168, bf16 K = 16 246 / 252, K = 32 (224 MB) 479 / 483, fp32
+// K = 16 (224 MB) 326 / 321, ResNet-18 K = 8 558 / 547, bf16 K = 12 (280 MB) 607 / 595.  The norms alone: MobileNetV2 bf16 K = 16 17.5 / 16.8, ResNet-50 K = 8
+// 134 / 117.5.
+constexpr uint64_t kNormBytes = 104ull << 20, kNormHintFrom = 160ull << 20;
+uint32_t norm_batch(const lasgd_ctx *c, uint32_t replicas)
+{
+    const uint64_t batches = (grad_bytes(c, replicas) + kNormBytes - 1) / kNormBytes;
+    return batches >= replicas ? 1u : (uint32_t)((replicas + batches - 1) / batches);
+}
+
+// The lowest `count` replicas of `left`, which it loses.
+uint64_t take_replicas(uint64_t &left, uint32_t count)
+{
+    uint64_t rest = left;
+    for (uint32_t i = 0; i < count; ++i) rest &= rest - 1ull;
+    const uint64_t taken = left ^ rest;
+    left = rest;
+    return taken;
+}
+
+// Norms of the replicas in `mask`, and (clips) what comes of them, on the main stream.
+lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, bool clips = true)
+{
+    ApplyArgs a{};
+    fill_common(c, a);
+    fill_fine(c, a);
+    NormArgs n = norm_args(c, mask, clip, a.ntiles);
+    if (!clips) n.clip = nullptr;
+    hipError_t e = clear_arrived(c);
+    if (e == hipSuccess) {
+        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 1) != 0 : !clips || grad_bytes(c, n.count) >= kNormHintFrom;
+        const dim3 grid(n.parts, n.count), bs(kNormThreads);
+        if (c->storage == LASGD_BF16) {
+            if (hint) hipLaunchKernelGGL((grad_norm_kernel<true, 1>), grid, bs, 0, c->main, a, n);
+            else hipLaunchKernelGGL((grad_norm_kernel<true, 0>), grid, bs, 0, c->main, a, n);
+        } else {
+            if (hint) hipLaunchKernelGGL((grad_norm_kernel<false, 1>), grid, bs, 0, c->main, a, n);
+            else hipLaunchKernelGGL((grad_norm_kernel<false, 0>), grid, bs, 0, c->main, a, n);
+        }
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return LASGD_OK;
+}
+
 // Until no queued clear of the gradients can still read the records.  Clears run on streams that the caller names and may
 // since have destroyed, so this waits for the device: an event after each clear would do for the stream alone, but costs
 // every clear 3.5 us on the device (MobileNetV2 list, K = 4, clear + accumulate + step twice 251 us without, 258 with).
@@ -1030,63 +1167,6 @@ static bool fill_ext(const lasgd_ctx *c, ExtArgs &x, const float *lr, uint64_t s
     return uniform;
 }
 
-// ---- gradient norms and clipping -------------------------------------------
-
-// What the kernels of a call hand on: the parts of each sum, and what comes of each norm.  For those alone that make the calls it is for; the
-// first of them asks, before it enqueues anything, also while it is being recorded.
-constexpr uint32_t kNormParts = 1024;
-static lasgd_status reserve_norms(lasgd_ctx *c)
-{
-    if (c->norm_mem) return LASGD_OK;
-    const size_t parts = (size_t)c->K * kNormParts * sizeof(double);
-    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;        // allowed while a stream of this thread is being recorded, and not recorded
-    (void)hipThreadExchangeStreamCaptureMode(&mode);
-    const hipError_t e = hipMalloc((void **)&c->norm_mem, parts + (size_t)c->K * sizeof(Clip));
-    (void)hipThreadExchangeStreamCaptureMode(&mode);
-    if (e != hipSuccess) {
-        (void)hipGetLastError();
-        c->norm_mem = nullptr;
-        return fail(c, LASGD_ERR_ALLOC, "no memory for the gradient norms: %s", hipGetErrorString(e));
-    }
-    c->norm_part = (double *)c->norm_mem;
-    c->clip = (Clip *)(c->norm_mem + parts);
-    return LASGD_OK;
-}
-
-static lasgd_status check_clip(lasgd_ctx *c, const lasgd_clip *clip)
-{
-    if (!clip) return fail(c, LASGD_ERR_INVALID, "NULL clip");
-    if (!(clip->max_norm >= 0.f)) return fail(c, LASGD_ERR_INVALID, "max_norm must be >= 0 (infinity: no limit)");
-    if ((uintptr_t)clip->norms & 3u) return fail(c, LASGD_ERR_INVALID, "norms is not 4-byte aligned");
-    return LASGD_OK;
-}
-
-// Norms of the replicas in `mask`, and (clips) what comes of them, on the main stream.
-static lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, bool clips = true)
-{
-    ApplyArgs a{};
-    fill_common(c, a);
-    fill_fine(c, a);
-    NormArgs n{};
-    n.part = c->norm_part;
-    n.parts = (a.ntiles + 15u) / 16u < kNormParts ? (a.ntiles + 15u) / 16u : kNormParts;
-    n.mask = mask;
-    n.count = (uint32_t)__builtin_popcountll(mask);
-    n.clip = clips ? c->clip : nullptr;
-    n.norms = clip.norms;
-    n.max_norm = clip.max_norm;
-    n.skip_nonfinite = clip.skip_nonfinite;
-    if (c->storage == LASGD_BF16) hipLaunchKernelGGL((grad_norm_kernel<true>), dim3(n.parts, n.count), dim3(kNormThreads), 0, c->main, a, n);
-    else hipLaunchKernelGGL((grad_norm_kernel<false>), dim3(n.parts, n.count), dim3(kNormThreads), 0, c->main, a, n);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess) {
-        hipLaunchKernelGGL(finish_norm_kernel, dim3(n.count), dim3(kNormThreads), 0, c->main, n, (uint32_t)c->K);
-        e = hipGetLastError();
-    }
-    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
-    return LASGD_OK;
-}
-
 static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uint64_t mask, const lasgd_clip *clip = nullptr)
 {
     lasgd_status st = check_ready_to_step(c, lr_k ? 0.f : lr);
@@ -1100,9 +1180,18 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
     if (clip) {
         ApplyPlan p;
         if ((st = reserve_norms(c)) != LASGD_OK) return st;
-        if ((st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, c->clip)) != LASGD_OK) return st;
-        if ((st = enqueue_norms(c, mask, *clip)) != LASGD_OK) return st;
-        return launch_apply(c, p);
+        const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking);
+        const bool plain = uniform && mask == c->all && batch == taking;
+        if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, c->clip)) != LASGD_OK) return st;
+        if (batch == taking) return (st = enqueue_norms(c, mask, *clip)) != LASGD_OK ? st : launch_apply(c, p);
+        while (mask) {
+            x.step_mask = take_replicas(mask, batch);
+            ApplyPlan q;               // of fewer replicas than p, which was not refused
+            if ((st = plan_apply(c, q, OP_STEP, 0.f, 0, &x, c->clip)) != LASGD_OK) return st;
+            if ((st = enqueue_norms(c, x.step_mask, *clip)) != LASGD_OK) return st;
+            if ((st = launch_apply(c, q)) != LASGD_OK) return st;
+        }
+        return LASGD_OK;
     }
     if (uniform && mask == c->all) return enqueue_apply(c, OP_STEP, lr_k[0], 0);
     return enqueue_apply(c, OP_STEP, 0.f, 0, &x);
@@ -1182,9 +1271,9 @@ static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, 
                        (op == OP_MERGE || (step_mask == c->all && uniform));
     ApplyPlan p;
     if (clip && (st = reserve_norms(c)) != LASGD_OK) return st;
-    if (clip) st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, c->clip);
-    else if (plain) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0);
-    else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x);
+    const Clip *coefficients = clip ? c->clip : nullptr;
+    if (plain) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0, nullptr, coefficients);
+    else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, coefficients);
     if (st != LASGD_OK) return st;
     // the norms need no z: they are taken while the mean may still be on its way
     if (clip && step_mask && (st = enqueue_norms(c, step_mask, *clip)) != LASGD_OK) return st;
@@ -1368,19 +1457,25 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
     if ((st = check_mask(c, mask, false, "mask")) != LASGD_OK) return st;
     if (c->n_bound != c->K) return fail(c, LASGD_ERR_STATE, "%d of %d replicas are bound", c->n_bound, c->K);
     if ((st = reserve_norms(c)) != LASGD_OK) return st;
-    if ((st = enqueue_norms(c, mask, *clip)) != LASGD_OK) return st;
     ApplyArgs a{};
     fill_common(c, a);
     fill_fine(c, a);
-    NormArgs n{};
-    n.mask = mask;
-    n.count = (uint32_t)__builtin_popcountll(mask);
-    n.clip = c->clip;
-    const dim3 grid(a.ntiles < 8192u ? a.ntiles : 8192u, n.count);
-    if (c->storage == LASGD_BF16) hipLaunchKernelGGL((scale_grads_kernel<true>), grid, dim3(64), 0, c->main, a, n);
-    else hipLaunchKernelGGL((scale_grads_kernel<false>), grid, dim3(64), 0, c->main, a, n);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask)); mask;) {
+        const uint64_t now = take_replicas(mask, batch);
+        if ((st = enqueue_norms(c, now, *clip)) != LASGD_OK) return st;
+        const NormArgs n = norm_args(c, now, *clip, a.ntiles);
+        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 3) != 0 : grad_bytes(c, (uint32_t)c->K) >= kNormBytes;
+        const dim3 grid(n.parts, n.count), bs(kNormThreads);
+        if (c->storage == LASGD_BF16) {
+            if (hint) hipLaunchKernelGGL((scale_grads_kernel<true, 3>), grid, bs, 0, c->main, a, n);
+            else hipLaunchKernelGGL((scale_grads_kernel<true, 0>), grid, bs, 0, c->main, a, n);
+        } else {
+            if (hint) hipLaunchKernelGGL((scale_grads_kernel<false, 3>), grid, bs, 0, c->main, a, n);
+            else hipLaunchKernelGGL((scale_grads_kernel<false, 0>), grid, bs, 0, c->main, a, n);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    }
     return LASGD_OK;
 }
 
@@ -1415,27 +1510,19 @@ lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *c, float lr, const lasgd_clip *cl
     ApplyPlan p;
     if ((st = plan_apply(c, p, OP_STEP_MEAN, lr, 0, nullptr, c->clip)) != LASGD_OK) return st;
     p.a.z = c->gbar;
-    ApplyArgs a = p.a;
-    a.nwaves = a.ntiles;
-    const bool bf16 = c->storage == LASGD_BF16, nt = (hint_of(c, USE_SGD_AR) & 1) != 0;
-    if (bf16 && nt) hipLaunchKernelGGL((mean_grad_kernel<true, 3>), dim3(a.ntiles), dim3(64), 0, c->main, a);
-    else if (bf16) hipLaunchKernelGGL((mean_grad_kernel<true, 0>), dim3(a.ntiles), dim3(64), 0, c->main, a);
-    else if (nt) hipLaunchKernelGGL((mean_grad_kernel<false, 3>), dim3(a.ntiles), dim3(64), 0, c->main, a);
-    else hipLaunchKernelGGL((mean_grad_kernel<false, 0>), dim3(a.ntiles), dim3(64), 0, c->main, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
-    NormArgs n{};
-    n.part = c->norm_part;
-    n.parts = (a.ntiles + 15u) / 16u < kNormParts ? (a.ntiles + 15u) / 16u : kNormParts;
-    n.mask = 1u;
-    n.count = 1u;
-    n.clip = c->clip;
-    n.norms = clip->norms;
-    n.max_norm = clip->max_norm;
-    n.skip_nonfinite = clip->skip_nonfinite;
-    hipLaunchKernelGGL(flat_norm_kernel, dim3(n.parts), dim3(kNormThreads), 0, c->main, c->gbar, c->packed / 4u, n);
-    if ((e = hipGetLastError()) == hipSuccess) {
-        hipLaunchKernelGGL(finish_norm_kernel, dim3(1), dim3(kNormThreads), 0, c->main, n, 1u);
+    NormArgs n = norm_args(c, 1u, *clip, p.a.ntiles);
+    n.parts = mean_norm_groups(p.a.ntiles);
+    const bool nt = (hint_of(c, USE_SGD_AR) & 1) != 0;
+    hipError_t e = clear_arrived(c);
+    if (e == hipSuccess) {
+        const dim3 grid(n.parts), bs(kNormThreads);
+        if (c->storage == LASGD_BF16) {
+            if (nt) hipLaunchKernelGGL((mean_grad_norm_kernel<true, 3>), grid, bs, 0, c->main, p.a, n);
+            else hipLaunchKernelGGL((mean_grad_norm_kernel<true, 0>), grid, bs, 0, c->main, p.a, n);
+        } else {
+            if (nt) hipLaunchKernelGGL((mean_grad_norm_kernel<false, 3>), grid, bs, 0, c->main, p.a, n);
+            else hipLaunchKernelGGL((mean_grad_norm_kernel<false, 0>), grid, bs, 0, c->main, p.a, n);
+        }
         e = hipGetLastError();
     }
     if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));

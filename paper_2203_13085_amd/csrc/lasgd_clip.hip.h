@@ -13,10 +13,13 @@
 namespace lasgd {
 
 constexpr uint32_t kNormThreads = 256;
+constexpr uint32_t kNormRun = 16;              // tiles a workgroup takes at a time
+constexpr uint32_t kArriveStride = 32;          // words: 128 bytes
 
 struct NormArgs {
-    double *part;           // [K][parts] a workgroup's sum of squares
-    uint32_t parts;         // workgroups a replica
+    double *part;           // [K][stride] a workgroup's sum of squares
+    uint32_t *arrived;      // [K][kArriveStride] how many of them are there
+    uint32_t stride, parts; // workgroups a replica, at most and in this call
     uint64_t mask;          // replicas that take part
     uint32_t count;         // how many they are
     Clip *clip;             // [K] what comes of it, or NULL
@@ -68,69 +71,206 @@ __device__ __forceinline__ float4 grad_at(const char *g, uint32_t e, uint32_t n)
     return r;
 }
 
-// Sums of squares of one replica's gradients (blockIdx.y: of which), tile by tile.
+// A workgroup has added up its share of replica k.  The last of the replica's workgroups adds the shares, in their order whoever is last, and is the
+// one to say what comes of the norm: a kernel of its own for that costs a short call 2-4 us.  The counter is back at zero
+// for the next call on the stream.
+//
+// Shares and counter are only ever touched by atomics of device scope, which bypass the XCDs' own L2s, so no cache has to be written back
+// or invalidated for them.  What is needed beyond is that a share is in memory before its arrival is counted: the store is waited
+// for.  (Left to an acquire-release addition, every workgroup writes back and invalidates its L2: norms of ResNet-50 K = 32 bf16
+// 1863 us in place of 280.)  Counters of different replicas lie on lines of their own, kArriveStride apart.
+__device__ __forceinline__ void join_norm(const NormArgs &n, uint32_t k, uint32_t group, uint32_t groups, double acc)
+{
+    __shared__ uint32_t last;
+    double *part = n.part + (size_t)k * n.stride;
+    acc = block_sum(acc);
+    if (groups == 1u) {
+        if (threadIdx.x == 0u) finish_norm(n, k, acc);
+        return;
+    }
+    if (threadIdx.x == 0u) {
+        __hip_atomic_store(part + group, acc, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        last = __hip_atomic_fetch_add(n.arrived + k * kArriveStride, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == groups;
+    }
+    __syncthreads();
+    if (!last) return;
+    acc = 0.0;
+    for (uint32_t i = threadIdx.x; i < groups; i += kNormThreads) acc += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    acc = block_sum(acc);
+    if (threadIdx.x != 0u) return;
+    __hip_atomic_store(n.arrived + k * kArriveStride, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    finish_norm(n, k, acc);
+}
+
+__global__ void clear_kernel(uint32_t *p, uint32_t n)
+{
+    for (uint32_t i = threadIdx.x; i < n; i += 64u) p[i] = 0u;
+}
+
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+
+template <int NT> __device__ __forceinline__ u32x4_t ld_u4(const char *p)
+{
+    if constexpr (NT & 1) return __builtin_nontemporal_load(as_global<u32x4_t>(p));
+    else return *as_global<u32x4_t>(p);
+}
+template <int NT> __device__ __forceinline__ void st_u4(char *p, u32x4_t v)
+{
+    if constexpr (NT & 2) __builtin_nontemporal_store(v, as_global<u32x4_t>(p));
+    else *as_global<u32x4_t>(p) = v;
+}
+template <bool BF16> __device__ __forceinline__ void add_squares(double &a0, double &a1, u32x4_t v)
+{
+    if constexpr (BF16) {
+        add_squares(a0, widen4(make_uint2(v.x, v.y)));
+        add_squares(a1, widen4(make_uint2(v.z, v.w)));
+    } else {
+        a0 = __builtin_fma((double)__uint_as_float(v.x), (double)__uint_as_float(v.x), a0);
+        a1 = __builtin_fma((double)__uint_as_float(v.y), (double)__uint_as_float(v.y), a1);
+        a0 = __builtin_fma((double)__uint_as_float(v.z), (double)__uint_as_float(v.z), a0);
+        a1 = __builtin_fma((double)__uint_as_float(v.w), (double)__uint_as_float(v.w), a1);
+    }
+}
+
+// A workgroup's runs of 16 tiles, a quarter of a block of the lookup table.  A run inside one tensor, as nearly all of a long list are,
+// takes one lookup: its address, or NULL where several tensors meet in it or the list ends.
 template <bool BF16>
+__device__ __forceinline__ char *whole_run(const ApplyArgs &a, uint32_t k, uint32_t first, uint32_t entry)
+{
+    if (entry & kMoreInBlock) return nullptr;
+    const Record rec = load_record(a, k, entry);
+    const uint32_t off = (first - rec.arow) * 256u;                  // a tensor's first row in the arenas is its first tile
+    return rec.numel - off >= kNormRun * 256u ? reinterpret_cast<char *>(rec.g) + (uint64_t)off * (BF16 ? 2u : 4u) : nullptr;
+}
+
+// Any run, tile by tile: four of a wave's tiles from `tile` on, every fourth one.
+struct FourTiles {
+    char *g[4];             // the tensor's gradient from the tile on
+    uint32_t n[4];          // how many of the lane's four elements there are
+    float4 v[4];
+};
+// starts: at most 64 tensors start in a block; each lane holds one's first tile, and how many of them are not beyond a tile says whose it is.
+__device__ __forceinline__ uint32_t later_starts(const ApplyArgs &a, uint32_t t0)
+{
+    const uint32_t t = t0 + 1u + (threadIdx.x & 63u);
+    return t < a.n_tensors ? as_global<uint32_t>(a.tile0)[t] : 0xffffffffu;
+}
+template <bool BF16>
+__device__ __forceinline__ void load_four(FourTiles &f, const ApplyArgs &a, uint32_t k, uint32_t t0, uint32_t starts, uint32_t tile, uint32_t end)
+{
+    const uint32_t e = (threadIdx.x & 63u) * 4u;
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u, tile += 4u) {
+        f.n[u] = 0;
+        if (tile < end) {
+            const Record rec = load_record(a, k, t0 + (uint32_t)__popcll(__ballot(starts <= tile)));
+            const uint32_t off = (tile - rec.arow) * 256u;
+            f.g[u] = reinterpret_cast<char *>(rec.g) + (uint64_t)off * (BF16 ? 2u : 4u);
+            f.n[u] = lane_elems<false>(e, rec.numel - off);
+        }
+        f.v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (f.n[u]) f.v[u] = grad_at<BF16>(f.g[u], e, f.n[u]);
+    }
+}
+
+// Sums of squares of one replica's gradients (blockIdx.y: of which).
+//
+// Few workgroups that go on (norm_groups in the host code): a share, and its arrival, is one atomic each at the memory all XCDs see. us, 768
+// workgroups / 1024 / 1536 / 2048: ResNet-50 list K = 8 117.5 / 117.7 / 121.5 / 125.5 (6.96 TB/s), ResNet-18 K = 8 53.4 / 54.7 / 57.2 / 58.6,
+// MobileNetV2 bf16 K = 16 16.8 / 16.8 / 17.2 / 17.5, one vector of 30,000,001 17.9 / 19.0 / 20.5 / 25.7; ResNet-50 bf16 K = 32 is 227 to 229 with all. Three
+// of them a CU have 48 KiB of fp32 loads in flight.  Runs of 64 tiles, at their best number of workgroups: 127, 54.8, 18.2, 17.5, 225.
+template <bool BF16, int NT>
 __global__ __launch_bounds__(256) void grad_norm_kernel(const ApplyArgs a, const NormArgs n)
 {
-    const uint32_t lane = threadIdx.x & 63u, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr uint32_t ROUNDS = kNormRun * 256u * (BF16 ? 2u : 4u) / (256u * 16u);          // of 16 bytes a thread
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t k = n.count == a.K ? blockIdx.y : nth_bit(n.mask, blockIdx.y);
-    double acc = 0.0;
-    for (uint32_t tile = blockIdx.x * 4u + w; tile < a.ntiles; tile += n.parts * 4u) {
-        const uint32_t tensor = tensor_of(a, tile);
-        const Record rec = load_record(a, k, tensor);
-        const Tile t = locate(a, rec, tile, tensor, 256u);
-        const char *g = reinterpret_cast<const char *>(rec.g) + t.toff * (BF16 ? 2 : 4);
-        const uint32_t e = lane * 4u;
-        add_squares(acc, grad_at<BF16>(g, e, lane_elems<false>(e, t.count)));
+    const uint32_t runs = (a.ntiles + kNormRun - 1u) / kNormRun;
+    double a0 = 0.0, a1 = 0.0;
+    for (uint32_t b = blockIdx.x; b < runs; b += n.parts) {
+        const uint32_t first = b * kNormRun, entry = as_const(a.blocks)[first >> kBlockShift];
+        if (const char *p = whole_run<BF16>(a, k, first, entry)) {
+            u32x4_t v[ROUNDS];
+#pragma unroll
+            for (uint32_t u = 0; u < ROUNDS; ++u) v[u] = ld_u4<NT>(p + threadIdx.x * 16u + u * 4096u);
+#pragma unroll
+            for (uint32_t u = 0; u < ROUNDS; ++u) add_squares<BF16>(a0, a1, v[u]);
+            continue;
+        }
+        const uint32_t t0 = entry & ~kMoreInBlock, starts = later_starts(a, t0);
+        const uint32_t end = first + kNormRun < a.ntiles ? first + kNormRun : a.ntiles;
+        FourTiles f;
+        load_four<BF16>(f, a, k, t0, starts, first + w, end);
+#pragma unroll
+        for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, f.v[u]);
     }
-    acc = block_sum(acc);
-    if (threadIdx.x == 0u) n.part[(size_t)k * n.parts + blockIdx.x] = acc;
+    join_norm(n, k, blockIdx.x, n.parts, a0 + a1);
 }
 
-// The same of one vector: the mean gradient, `nvec` groups of four elements.
-__global__ __launch_bounds__(256) void flat_norm_kernel(const float *v, uint64_t nvec, const NormArgs n)
+// The mean gradient of all replicas (mean_grad_tile) and its norm in one pass.  A wave's tiles stay on its XCD, where the step looks for them.
+template <bool BF16, int NT>
+__global__ __launch_bounds__(256) void mean_grad_norm_kernel(const ApplyArgs a, const NormArgs n)
 {
+    const uint32_t lane = threadIdx.x & 63u, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     double acc = 0.0;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < nvec; i += (uint64_t)n.parts * 256u) add_squares(acc, ld4<0>(v + i * 4u));
-    acc = block_sum(acc);
-    if (threadIdx.x == 0u) n.part[blockIdx.x] = acc;
+    for (uint32_t tile = w * n.parts + blockIdx.x; tile < a.ntiles; tile += 4u * n.parts) {
+        const uint32_t tensor = tensor_of(a, tile);
+        const Tile t = locate(a, load_record(a, 0, tensor), tile, tensor, 256u);
+        // the lanes beyond a tensor's end have a mean of zero
+        if (t.count == 256u) add_squares(acc, mean_grad_tile<BF16, NT, true>(a, t, tensor, lane));
+        else add_squares(acc, mean_grad_tile<BF16, NT, false>(a, t, tensor, lane));
+    }
+    join_norm(n, 0u, blockIdx.x, n.parts, acc);
 }
 
-// One workgroup a replica: the parts in order.
-__global__ __launch_bounds__(256) void finish_norm_kernel(const NormArgs n, const uint32_t all)
-{
-    const uint32_t k = n.count == all ? blockIdx.x : nth_bit(n.mask, blockIdx.x);
-    double acc = 0.0;
-    for (uint32_t i = threadIdx.x; i < n.parts; i += 256u) acc += n.part[(size_t)k * n.parts + i];
-    acc = block_sum(acc);
-    if (threadIdx.x == 0u) finish_norm(n, k, acc);
-}
+__device__ __forceinline__ float4 times(float4 v, float c) { return make_float4(v.x * c, v.y * c, v.z * c, v.w * c); }
 
 // Clipping in place: gradients times c, rounded once to the storage type, where c is not 1.
-template <bool BF16>
-__global__ __launch_bounds__(64) void scale_grads_kernel(const ApplyArgs a, const NormArgs n)
+template <bool BF16, int NT>
+__global__ __launch_bounds__(256) void scale_grads_kernel(const ApplyArgs a, const NormArgs n)
 {
-    const uint32_t e = threadIdx.x * 4u;
+    constexpr uint32_t ROUNDS = kNormRun * 256u * (BF16 ? 2u : 4u) / (256u * 16u);
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = (threadIdx.x & 63u) * 4u;
     const uint32_t k = n.count == a.K ? blockIdx.y : nth_bit(n.mask, blockIdx.y);
-    const LASGD_CONST_AS Clip *cl = as_const(n.clip) + k;
-    const float scale = cl->c;
-    if (cl->skip || scale == 1.f) return;
-    for (uint32_t tile = blockIdx.x; tile < a.ntiles; tile += gridDim.x) {
-        const uint32_t tensor = tensor_of(a, tile);
-        const Record rec = load_record(a, k, tensor);
-        const Tile t = locate(a, rec, tile, tensor, 256u);
-        char *g = reinterpret_cast<char *>(rec.g) + t.toff * (BF16 ? 2 : 4);
-        const uint32_t m = lane_elems<false>(e, t.count);
-        float4 v = grad_at<BF16>(g, e, m);
-        v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
-        if (m == 4u) {
-            if constexpr (BF16) st2<0>(reinterpret_cast<uint16_t *>(g) + e, round4(v));
-            else st4<0>(reinterpret_cast<float *>(g) + e, v);
-        } else {
-            LASGD_FOR4(if (c < 3 && (uint32_t)c < m) {
-                if constexpr (BF16) as_global<uint16_t>(g)[e + c] = (uint16_t)bf16_round(compv(v, c));
-                else as_global<float>(g)[e + c] = compv(v, c);
-            })
+    const Clip cl = load_clip(n.clip, k);
+    if (cl.skip || cl.c == 1.f) return;
+    const uint32_t runs = (a.ntiles + kNormRun - 1u) / kNormRun;
+    for (uint32_t b = blockIdx.x; b < runs; b += n.parts) {
+        const uint32_t first = b * kNormRun, entry = as_const(a.blocks)[first >> kBlockShift];
+        if (char *p = whole_run<BF16>(a, k, first, entry)) {
+            u32x4_t v[ROUNDS];
+#pragma unroll
+            for (uint32_t u = 0; u < ROUNDS; ++u) v[u] = ld_u4<NT>(p + threadIdx.x * 16u + u * 4096u);
+#pragma unroll
+            for (uint32_t u = 0; u < ROUNDS; ++u) {
+                if constexpr (BF16) {
+                    const uint2 lo = round4(times(widen4(make_uint2(v[u].x, v[u].y)), cl.c)), hi = round4(times(widen4(make_uint2(v[u].z, v[u].w)), cl.c));
+                    v[u] = u32x4_t{lo.x, lo.y, hi.x, hi.y};
+                } else {
+                    const float4 t = times(make_float4(__uint_as_float(v[u].x), __uint_as_float(v[u].y), __uint_as_float(v[u].z), __uint_as_float(v[u].w)), cl.c);
+                    v[u] = u32x4_t{__float_as_uint(t.x), __float_as_uint(t.y), __float_as_uint(t.z), __float_as_uint(t.w)};
+                }
+                st_u4<NT>(p + threadIdx.x * 16u + u * 4096u, v[u]);
+            }
+            continue;
+        }
+        const uint32_t t0 = entry & ~kMoreInBlock, starts = later_starts(a, t0);
+        const uint32_t end = first + kNormRun < a.ntiles ? first + kNormRun : a.ntiles;
+        FourTiles f;
+        load_four<BF16>(f, a, k, t0, starts, first + w, end);
+#pragma unroll
+        for (uint32_t u = 0; u < 4u; ++u) {
+            const float4 v = times(f.v[u], cl.c);
+            if (f.n[u] == 4u) {
+                if constexpr (BF16) st2<0>(reinterpret_cast<uint16_t *>(f.g[u]) + e, round4(v));
+                else st4<0>(reinterpret_cast<float *>(f.g[u]) + e, v);
+            } else {
+                LASGD_FOR4(if (c < 3 && (uint32_t)c < f.n[u]) {
+                    if constexpr (BF16) as_global<uint16_t>(f.g[u])[e + c] = (uint16_t)bf16_round(compv(v, c));
+                    else as_global<float>(f.g[u])[e + c] = compv(v, c);
+                })
+            }
         }
     }
 }

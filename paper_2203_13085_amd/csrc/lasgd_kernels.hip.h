@@ -478,6 +478,13 @@ __device__ __forceinline__ void apply_tile(const ApplyArgs &a, void *xu, const v
     }
 }
 
+// Beside the replica's record, so that it costs no wait of its own.
+__device__ __forceinline__ Clip load_clip(const Clip *clip, uint32_t k)
+{
+    const LASGD_CONST_AS Clip *p = as_const(clip) + k;
+    return Clip{p->c, p->skip};
+}
+
 // Position of the n-th set bit (n = 0: the lowest) of a word that has more than n: halve the word six times.
 __device__ __forceinline__ uint32_t nth_bit(uint64_t word, uint32_t n)
 {
@@ -517,6 +524,7 @@ __device__ __forceinline__ void apply_body(const ApplyArgs &a, const ExtArgs *xa
     // the shape travels in the arguments: reading it from the dispatch would be a vector load before everything else
     const uint32_t wave0 = __builtin_amdgcn_readfirstlane(blockIdx.x * a.wpb + (threadIdx.x >> 6));
     load_together(a);
+    if constexpr (CLIP) asm volatile("" ::"s"(clip));
     uint32_t word = 0;
     bool looked = false;
     for (uint32_t i0 = wave0; i0 < a.nitems; i0 += a.nwaves) {
@@ -554,6 +562,8 @@ __device__ __forceinline__ void apply_body(const ApplyArgs &a, const ExtArgs *xa
             }
         }
         Record rec = load_record(a, replica_at<EXT>(a, xa, k0), tensor);
+        Clip cl{1.f, 0u};
+        if constexpr (CLIP) cl = load_clip(clip, OP == OP_STEP_MEAN ? 0u : replica_at<EXT>(a, xa, k0));
         const uint64_t in_s = !BF16 || word >= kSettled ? 0ull : a.at_s;
         const Tile t = locate(a, rec, tile, tensor, 256u * VEC);
         const bool full = (t.count == 256u * VEC);
@@ -579,11 +589,6 @@ __device__ __forceinline__ void apply_body(const ApplyArgs &a, const ExtArgs *xa
             float *xm = BF16 ? a.x32 + ao : nullptr;
             const bool at_s = BF16 && ((in_s >> k) & 1ull);
             const float *xr = at_s ? a.s + ao : xm;
-            Clip cl{1.f, 0u};
-            if constexpr (CLIP) {
-                const LASGD_CONST_AS Clip *p = as_const(clip) + (OP == OP_STEP_MEAN ? 0u : k);
-                cl = Clip{p->c, p->skip};
-            }
 #define LASGD_TILE_AT(OPX, NLR, AL, AT)                                                                      \
     do {                                                                                                     \
         if (__builtin_expect(full, 1)) apply_tile<VEC, OPX, BF16, NT, true, EXT, OPX == OP, AT, CLIP>(a, xu, gu, xr, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, NLR, AL, cl); \
@@ -616,6 +621,7 @@ __device__ __forceinline__ void apply_body(const ApplyArgs &a, const ExtArgs *xa
 #undef LASGD_TILE_AT
             if (++j == k1) break;
             rec = load_record(a, replica_at<EXT>(a, xa, j), tensor);
+            if constexpr (CLIP && OP != OP_STEP_MEAN) cl = load_clip(clip, replica_at<EXT>(a, xa, j));
         }
     }
     if constexpr (BF16 && (NEED_Z || OP == OP_STEP)) {         // they write the master copy from the model, wherever that is
@@ -638,18 +644,17 @@ __global__ __launch_bounds__(256) void apply_ext_kernel(const ApplyArgs a, const
     apply_body<VEC, OP, BF16, NT, true>(a, &xa);
 }
 
-// The clipped forms, in tiles of 256 elements: a local step, or a step with the global update, of the replicas in the masks, and a step of
-// all with the mean gradient.
+// The clipped forms, in tiles of 256 elements: all replicas with one step size, and those of the masks with one each.
 template <int OP, bool BF16, int NT>
-__global__ __launch_bounds__(256) void apply_clip_kernel(const ApplyArgs a, const ExtArgs xa, const Clip *clip)
+__global__ __launch_bounds__(256) void apply_clip_kernel(const ApplyArgs a, const Clip *clip)
 {
-    apply_body<1, OP, BF16, NT, true, true>(a, &xa, clip);
+    apply_body<1, OP, BF16, NT, false, true>(a, nullptr, clip);
 }
 
-template <bool BF16, int NT>
-__global__ __launch_bounds__(256) void step_mean_clip_kernel(const ApplyArgs a, const Clip *clip)
+template <int OP, bool BF16, int NT>
+__global__ __launch_bounds__(256) void apply_clip_ext_kernel(const ApplyArgs a, const ExtArgs xa, const Clip *clip)
 {
-    apply_body<1, OP_STEP_MEAN, BF16, NT, false, true>(a, nullptr, clip);
+    apply_body<1, OP, BF16, NT, true, true>(a, &xa, clip);
 }
 
 // ---- the mean (Sec. 3, Eq. 8) -----------------------------------------------
@@ -1089,7 +1094,7 @@ __global__ __launch_bounds__(1024) void sgd_ar_kernel(const ApplyArgs a, const u
 // order, so the result is that of the one kernel to the bit.  It moves 8 bytes a parameter more than the one kernel and gains
 // from one-wave workgroups; mean_grad_first in the host code holds the line and both sides.
 template <bool BF16, int NT, bool FULL>
-__device__ __forceinline__ void mean_grad_tile(const ApplyArgs &a, const Tile &t, uint32_t tensor, uint32_t lane)
+__device__ __forceinline__ float4 mean_grad_tile(const ApplyArgs &a, const Tile &t, uint32_t tensor, uint32_t lane)
 {
     constexpr uint32_t N = 8;
     const uint32_t e = lane * 4u, n = lane_elems<FULL>(e, t.count);
@@ -1125,7 +1130,9 @@ __device__ __forceinline__ void mean_grad_tile(const ApplyArgs &a, const Tile &t
     if (k + 2u <= a.K) { rows(k, Count<2>{}); k += 2u; }
     if (k < a.K) rows(k, Count<1>{});
     // a whole row: the arena is padded, and the step that reads it takes whole rows too
-    st4<0>(a.z + t.aoff + e, make_float4(group_mean_of(a0, a), group_mean_of(a1, a), group_mean_of(a2, a), group_mean_of(a3, a)));
+    const float4 mean = make_float4(group_mean_of(a0, a), group_mean_of(a1, a), group_mean_of(a2, a), group_mean_of(a3, a));
+    st4<0>(a.z + t.aoff + e, mean);
+    return mean;
 }
 
 template <bool BF16, int NT>

@@ -382,6 +382,44 @@ def test_no_limit_is_the_unclipped_call_to_the_bit(K, numels, storage):
         b.close()
 
 
+@pytest.mark.parametrize("storage,K,n", [("f32", 9, 3_100_003), ("bf16", 20, 2_800_003)])
+def test_more_gradients_than_a_cache_holds(storage, K, n):
+    """From 104 MiB of gradients on a step, and clipping in place, take some replicas at a time: plain and masked, after updates that
+    leave a bf16 model in one place, and recorded."""
+    r = Rig(K, (n, 33, 256), storage, side_stream=False)
+    full, part = (1 << K) - 1, ((1 << K) - 1) & 0xFFEB7
+    try:
+        g = r.grads(0)
+        r.load(g)
+        most = r.max_norm(g)
+        use = r.clipped(g, most)
+        lrs = [r.w.lr * (1.0 - 0.01 * k) for k in range(K)]
+        for o in (r.orc, r.ctx):
+            o.snapshot()
+            o.average()
+        r.ctx.step_merge_clip(r.w.lr, most, norms=r.norms.data_ptr())
+        r.orc.local_step(use, r.w.lr)
+        r.orc.merge(True)
+        graph = torch.cuda.CUDAGraph()
+        r.ctx.sync()
+        with torch.cuda.graph(graph, stream=r.dev.main):
+            r.ctx.local_step_clip(r.w.lr, most)
+        for rep in range(2):
+            with torch.cuda.stream(r.dev.main):
+                graph.replay()
+            r.orc.local_step(use, r.w.lr)
+        r.ctx.local_step_clip(lrs, most, part, norms=r.norms.data_ptr())
+        r.orc.local_step(use, lrs, mask=part)
+        r.same("at the end")
+        check_norms(r.read_norms(), [norm64(a) for a in g])
+        r.ctx.clip_grads(most, part)
+        for k in range(K):
+            want = use[k] if (part >> k) & 1 else g[k]
+            np.testing.assert_array_equal(r.device_grads(k), W.bf16_bits_to_f32(W.to_bf16_bits(want)) if r.bf16 else want)
+    finally:
+        r.close()
+
+
 def mean_gradient(g):
     acc = np.zeros(g[0].size)
     for a in g:
