@@ -117,7 +117,20 @@ def run_variant(args, w, make, alg) -> dict:
     steps_done = 0          # replica-steps, for params/s
     nbytes = 0.0
 
-    if args.mode == "sgd_ar":
+    if args.mode == "clip":
+        # about the norm of every replica's gradients: some are scaled and some are not
+        max_norm = float(np.float32(1e-3 * N ** 0.5))
+        dev.prologue(w.lr, max_norm)
+
+        def one():
+            nonlocal steps_done, nbytes
+            tau = 0
+            for _ in range(w.m):
+                tau = dev.iteration(w.lr, tau, w.m, max_norm=max_norm)
+            steps_done += K * w.m
+            nbytes += (w.m - 1) * alg["local_step"] + alg["step_merge"] + alg["average"]
+        what = "the headline cycle with every replica's gradients clipped to a global norm in each local update (gradients counted once)"
+    elif args.mode == "sgd_ar":
         def one():
             nonlocal steps_done, nbytes
             c.sgd_ar_step(w.lr)
@@ -213,9 +226,10 @@ def main() -> int:
     ap.add_argument("--calib-copy", action="store_true",
                     help="also run three plain 1 GiB device copies first (a kernel of known traffic, "
                          "to calibrate profiler byte counters)")
-    ap.add_argument("--mode", default="lasgd", choices=["lasgd", "sgd_ar", "dynamic", "elastic", "partial"],
+    ap.add_argument("--mode", default="lasgd", choices=["lasgd", "sgd_ar", "dynamic", "elastic", "partial", "clip"],
                     help="lasgd: the headline cycle; the others time the extended entry points "
-                         "(SGD All-Reduce step, scripted adaptive cadence, alpha=beta=0.5, 75%% partial All-Reduce)")
+                         "(SGD All-Reduce step, scripted adaptive cadence, alpha=beta=0.5, 75%% partial All-Reduce, the headline "
+                         "cycle with clipped gradients)")
     ap.add_argument("--tune", type=str, default="", help="k=v,k=v launch-shape knobs (lasgd_tuning fields)")
     args = ap.parse_args()
     if args.gpus != 1:

@@ -158,6 +158,10 @@ class Context:
         if st != OK:
             raise LasgdError(st, self._L.lasgd_last_error(None).decode())
         self._h = h
+        self._all = (1 << self.K) - 1
+        self._clip_arg = Clip()
+        self._clip_ref = ctypes.byref(self._clip_arg)
+        self._step_size = self._step_sizes = None
         self.bound_grads = [None] * self.K        # per replica: the gradient addresses in effect (a ctypes array)
 
     # -- plumbing ---------------------------------------------------------
@@ -246,32 +250,42 @@ class Context:
     def sgd_ar_step(self, lr: float) -> None:
         self._check(self._L.lasgd_sgd_ar_step(self._h, lr))
 
-    # -- gradient norms and clipping: `norms` is a device address ([K] floats; sgd_ar_step_clip: one), masks default to all replicas
-    def _mask(self, mask: Optional[int]) -> int:
-        return (1 << self.K) - 1 if mask is None else mask
+    # -- gradient norms and clipping ------------------------------------------
+    # norms: a device address, [K] floats (sgd_ar_step_clip: one); a mask of None is all replicas.  Short calls are bound by the
+    # host, so the arguments' structures are made once and filled in (a step size for all replicas: when it changes).
+    def _clip(self, max_norm: float, skip_nonfinite: bool, norms: Optional[int]):
+        c = self._clip_arg
+        c.max_norm, c.skip_nonfinite, c.norms = max_norm, skip_nonfinite, norms
+        return self._clip_ref
+
+    def _steps(self, lr):
+        if type(lr) is not float:
+            return self._lrs(lr)
+        if lr != self._step_size:
+            self._step_sizes, self._step_size = self._lrs(lr), lr
+        return self._step_sizes
 
     def grad_norms(self, norms: int, mask: Optional[int] = None) -> None:
-        self._check(self._L.lasgd_grad_norms(self._h, self._mask(mask), norms or None))
+        self._check(self._L.lasgd_grad_norms(self._h, self._all if mask is None else mask, norms))
 
     def clip_grads(self, max_norm: float, mask: Optional[int] = None, *, skip_nonfinite: bool = False,
                    norms: Optional[int] = None) -> None:
-        c = Clip(max_norm, skip_nonfinite, norms or None)
-        self._check(self._L.lasgd_clip_grads(self._h, self._mask(mask), ctypes.byref(c)))
+        self._check(self._L.lasgd_clip_grads(self._h, self._all if mask is None else mask,
+                                             self._clip(max_norm, skip_nonfinite, norms)))
 
     def local_step_clip(self, lr, max_norm: float, mask: Optional[int] = None, *, skip_nonfinite: bool = False,
                         norms: Optional[int] = None) -> None:
-        c = Clip(max_norm, skip_nonfinite, norms or None)
-        self._check(self._L.lasgd_local_step_clip(self._h, self._lrs(lr), self._mask(mask), ctypes.byref(c)))
+        self._check(self._L.lasgd_local_step_clip(self._h, self._steps(lr), self._all if mask is None else mask,
+                                                  self._clip(max_norm, skip_nonfinite, norms)))
 
     def step_merge_clip(self, lr, max_norm: float, step_mask: Optional[int] = None, merge_mask: Optional[int] = None,
                         resnapshot: bool = True, *, skip_nonfinite: bool = False, norms: Optional[int] = None) -> None:
-        c = Clip(max_norm, skip_nonfinite, norms or None)
-        self._check(self._L.lasgd_step_merge_clip(self._h, self._lrs(lr), self._mask(step_mask), self._mask(merge_mask),
-                                                  int(resnapshot), ctypes.byref(c)))
+        self._check(self._L.lasgd_step_merge_clip(self._h, self._steps(lr), self._all if step_mask is None else step_mask,
+                                                  self._all if merge_mask is None else merge_mask, int(resnapshot),
+                                                  self._clip(max_norm, skip_nonfinite, norms)))
 
     def sgd_ar_step_clip(self, lr: float, max_norm: float, *, skip_nonfinite: bool = False, norms: Optional[int] = None) -> None:
-        c = Clip(max_norm, skip_nonfinite, norms or None)
-        self._check(self._L.lasgd_sgd_ar_step_clip(self._h, lr, ctypes.byref(c)))
+        self._check(self._L.lasgd_sgd_ar_step_clip(self._h, lr, self._clip(max_norm, skip_nonfinite, norms)))
 
     def read_state(self, which: int, k: int = 0, tensor: int = -1) -> np.ndarray:
         # an out-of-range tensor index is the library's to refuse

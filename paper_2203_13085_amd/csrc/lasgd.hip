@@ -434,12 +434,12 @@ struct ApplyPlan {
 };
 
 // xa == nullptr: every replica takes part, one step size, alpha = 1 (the plain kernels).
-lasgd_status plan_apply(lasgd_ctx *c, ApplyPlan &p, int op, float lr, int resnap, const ExtArgs *xa = nullptr, const Clip *clip = nullptr)
+lasgd_status plan_apply(lasgd_ctx *c, ApplyPlan &p, int op, float lr, int resnap, const ExtArgs *xa = nullptr, bool clip = false)
 {
     if (op < OP_STEP || op > OP_STEP_MEAN) return fail(c, LASGD_ERR_INVALID, "unknown op %d", op);
     ApplyArgs &a = p.a;
     fill_common(c, a);
-    p.clip = clip;
+    p.clip = clip ? c->clip : nullptr;
     if (clip) fill_fine(c, a);
     int kper = (op == OP_MERGE || op == OP_STEP_MERGE || op == OP_STEP_MEAN) ? c->tune.kper_merge : c->tune.kper_step;
     const int taking = xa ? __builtin_popcountll(xa->step_mask | xa->merge_mask) : c->K;
@@ -962,6 +962,34 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
     return LASGD_OK;
 }
 
+// Lists this short take one launch for norm and update (small_step_kernel): the host is what bounds two of them.  us, two launches / one, three
+// states in turn: step, 300 to 16384 elements, K = 3 to 64 7.1-8.0 / 4.0-4.9; in place 5.4-6.8 / 3.2-3.9; step + update, with its mean, 300 elements
+// K = 3 9.2 / 7.1, 16384 K = 16 12.6 / 10.1; 9000 K = 64 12.8 / 11.3, but 16384 K = 64 (4096 tiles in 64 workgroups) 13.8 / 14.3.
+bool one_launch(const lasgd_ctx *c, int op, uint32_t replicas)
+{
+    const uint32_t ntiles = c->tables_by_vec[0].ntiles;
+    return ntiles <= 4u * kSmallWaves && (op != OP_STEP_MERGE || ntiles * replicas <= 3072u);
+}
+
+lasgd_status launch_small(lasgd_ctx *c, ApplyPlan &p, const lasgd_clip &clip)
+{
+    const uint64_t taking = p.ext.step_mask | p.ext.merge_mask;
+    const lasgd_status st = place_models(c, &p.a, taking);
+    if (st != LASGD_OK) return st;
+    const NormArgs n = norm_args(c, taking, clip, p.a.ntiles);
+    const dim3 grid(n.count), bs(64u * kSmallWaves);
+    if (p.op == OP_STEP) {
+        if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_step_kernel<OP_STEP, true>), grid, bs, 0, c->main, p.a, p.ext, n);
+        else hipLaunchKernelGGL((small_step_kernel<OP_STEP, false>), grid, bs, 0, c->main, p.a, p.ext, n);
+    } else {
+        if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_step_kernel<OP_STEP_MERGE, true>), grid, bs, 0, c->main, p.a, p.ext, n);
+        else hipLaunchKernelGGL((small_step_kernel<OP_STEP_MERGE, false>), grid, bs, 0, c->main, p.a, p.ext, n);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return LASGD_OK;
+}
+
 // Until no queued clear of the gradients can still read the records.  Clears run on streams that the caller names and may
 // since have destroyed, so this waits for the device: an event after each clear would do for the stream alone, but costs
 // every clear 3.5 us on the device (MobileNetV2 list, K = 4, clear + accumulate + step twice 251 us without, 258 with).
@@ -1179,15 +1207,16 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
     const bool uniform = fill_ext(c, x, lr_k, mask, 0);
     if (clip) {
         ApplyPlan p;
+        if (one_launch(c, OP_STEP, (uint32_t)__builtin_popcountll(mask))) return (st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK ? st : launch_small(c, p, *clip);
         if ((st = reserve_norms(c)) != LASGD_OK) return st;
         const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking);
         const bool plain = uniform && mask == c->all && batch == taking;
-        if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, c->clip)) != LASGD_OK) return st;
+        if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, true)) != LASGD_OK) return st;
         if (batch == taking) return (st = enqueue_norms(c, mask, *clip)) != LASGD_OK ? st : launch_apply(c, p);
         while (mask) {
             x.step_mask = take_replicas(mask, batch);
             ApplyPlan q;               // of fewer replicas than p, which was not refused
-            if ((st = plan_apply(c, q, OP_STEP, 0.f, 0, &x, c->clip)) != LASGD_OK) return st;
+            if ((st = plan_apply(c, q, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK) return st;
             if ((st = enqueue_norms(c, x.step_mask, *clip)) != LASGD_OK) return st;
             if ((st = launch_apply(c, q)) != LASGD_OK) return st;
         }
@@ -1270,16 +1299,16 @@ static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, 
     const bool plain = merge_mask == c->all && c->alpha == 1.f &&
                        (op == OP_MERGE || (step_mask == c->all && uniform));
     ApplyPlan p;
-    if (clip && (st = reserve_norms(c)) != LASGD_OK) return st;
-    const Clip *coefficients = clip ? c->clip : nullptr;
-    if (plain) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0, nullptr, coefficients);
-    else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, coefficients);
+    const bool small = clip && one_launch(c, op, (uint32_t)__builtin_popcountll(step_mask | merge_mask));
+    if (clip && !small && (st = reserve_norms(c)) != LASGD_OK) return st;
+    if (plain && !small) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0, nullptr, clip != nullptr);
+    else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, clip != nullptr);
     if (st != LASGD_OK) return st;
     // the norms need no z: they are taken while the mean may still be on its way
-    if (clip && step_mask && (st = enqueue_norms(c, step_mask, *clip)) != LASGD_OK) return st;
+    if (clip && !small && step_mask && (st = enqueue_norms(c, step_mask, *clip)) != LASGD_OK) return st;
     // nothing can be refused any more: now the main stream waits for z (unless z is made on this very stream)
     if (!c->z_on_main) LASGD_HIP(c, hipStreamWaitEvent(c->main, c->evZ, 0));
-    st = launch_apply(c, p);
+    st = small ? launch_small(c, p, *clip) : launch_apply(c, p);
     if (st != LASGD_OK) return st;
     c->pending_mask &= ~merge_mask;
     if (resnapshot) c->snap_mask |= merge_mask;
@@ -1456,10 +1485,17 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
     if (st != LASGD_OK) return st;
     if ((st = check_mask(c, mask, false, "mask")) != LASGD_OK) return st;
     if (c->n_bound != c->K) return fail(c, LASGD_ERR_STATE, "%d of %d replicas are bound", c->n_bound, c->K);
-    if ((st = reserve_norms(c)) != LASGD_OK) return st;
     ApplyArgs a{};
     fill_common(c, a);
     fill_fine(c, a);
+    if (one_launch(c, OP_STEP, (uint32_t)c->K)) {
+        const NormArgs n = norm_args(c, mask, *clip, a.ntiles);
+        if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_scale_kernel<true>), dim3(n.count), dim3(64u * kSmallWaves), 0, c->main, a, n);
+        else hipLaunchKernelGGL((small_scale_kernel<false>), dim3(n.count), dim3(64u * kSmallWaves), 0, c->main, a, n);
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? LASGD_OK : fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    }
+    if ((st = reserve_norms(c)) != LASGD_OK) return st;
     for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask)); mask;) {
         const uint64_t now = take_replicas(mask, batch);
         if ((st = enqueue_norms(c, now, *clip)) != LASGD_OK) return st;
@@ -1508,7 +1544,7 @@ lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *c, float lr, const lasgd_clip *cl
     if (!c->gbar) return fail(c, LASGD_ERR_ALLOC, "no memory for the mean gradient");
     if ((st = reserve_norms(c)) != LASGD_OK) return st;
     ApplyPlan p;
-    if ((st = plan_apply(c, p, OP_STEP_MEAN, lr, 0, nullptr, c->clip)) != LASGD_OK) return st;
+    if ((st = plan_apply(c, p, OP_STEP_MEAN, lr, 0, nullptr, true)) != LASGD_OK) return st;
     p.a.z = c->gbar;
     NormArgs n = norm_args(c, 1u, *clip, p.a.ntiles);
     n.parts = mean_norm_groups(p.a.ntiles);

@@ -36,30 +36,34 @@ __device__ __forceinline__ void add_squares(double &acc, float4 g)
     acc = __builtin_fma((double)g.w, (double)g.w, acc);
 }
 
-// The sum over a workgroup, in thread 0.
-__device__ __forceinline__ double block_sum(double acc)
+// The sum over a workgroup of W waves, in thread 0.
+template <uint32_t W> __device__ __forceinline__ double block_sum(double acc)
 {
-    __shared__ double wave[kNormThreads / 64u];
+    __shared__ double wave[W];
 #pragma unroll
     for (int d = 32; d; d >>= 1) acc += __shfl_down(acc, d, 64);
     if ((threadIdx.x & 63u) == 0u) wave[threadIdx.x >> 6] = acc;
     __syncthreads();
-    if (threadIdx.x == 0u)
-        for (uint32_t w = 1; w < kNormThreads / 64u; ++w) acc += wave[w];
+    if (threadIdx.x == 0u) {
+#pragma unroll
+        for (uint32_t w = 1; w < W; ++w) acc += wave[w];
+    }
     return acc;
 }
 
 // What comes of replica k's sum of squares.
-__device__ __forceinline__ void finish_norm(const NormArgs &n, uint32_t k, double sum)
+__device__ __forceinline__ Clip clip_of(const NormArgs &n, uint32_t k, double sum)
 {
     const double norm = __builtin_sqrt(sum);
     if (n.norms) *as_global<float>(n.norms + k) = (float)norm;
-    if (n.clip) {
-        const double c = (double)n.max_norm / (norm + 1e-6);
-        const bool finite = norm <= 1.7976931348623157e308;
-        n.clip[k].c = c >= 1.0 ? 1.f : (float)c;               // a NaN stays one
-        n.clip[k].skip = n.skip_nonfinite && !finite ? 1u : 0u;
-    }
+    const double c = (double)n.max_norm / (norm + 1e-6);
+    const bool finite = norm <= 1.7976931348623157e308;
+    return Clip{c >= 1.0 ? 1.f : (float)c, n.skip_nonfinite && !finite ? 1u : 0u};          // a NaN stays one
+}
+__device__ __forceinline__ void finish_norm(const NormArgs &n, uint32_t k, double sum)
+{
+    const Clip c = clip_of(n, k, sum);
+    if (n.clip) n.clip[k] = c;
 }
 
 template <bool BF16>
@@ -83,7 +87,7 @@ __device__ __forceinline__ void join_norm(const NormArgs &n, uint32_t k, uint32_
 {
     __shared__ uint32_t last;
     double *part = n.part + (size_t)k * n.stride;
-    acc = block_sum(acc);
+    acc = block_sum<kNormThreads / 64u>(acc);
     if (groups == 1u) {
         if (threadIdx.x == 0u) finish_norm(n, k, acc);
         return;
@@ -97,7 +101,7 @@ __device__ __forceinline__ void join_norm(const NormArgs &n, uint32_t k, uint32_
     if (!last) return;
     acc = 0.0;
     for (uint32_t i = threadIdx.x; i < groups; i += kNormThreads) acc += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    acc = block_sum(acc);
+    acc = block_sum<kNormThreads / 64u>(acc);
     if (threadIdx.x != 0u) return;
     __hip_atomic_store(n.arrived + k * kArriveStride, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     finish_norm(n, k, acc);
@@ -144,7 +148,7 @@ __device__ __forceinline__ char *whole_run(const ApplyArgs &a, uint32_t k, uint3
     return rec.numel - off >= kNormRun * 256u ? reinterpret_cast<char *>(rec.g) + (uint64_t)off * (BF16 ? 2u : 4u) : nullptr;
 }
 
-// Any run, tile by tile: four of a wave's tiles from `tile` on, every fourth one.
+// Any run, tile by tile: four of a wave's tiles from `tile` on, every W-th one.
 struct FourTiles {
     char *g[4];             // the tensor's gradient from the tile on
     uint32_t n[4];          // how many of the lane's four elements there are
@@ -156,12 +160,12 @@ __device__ __forceinline__ uint32_t later_starts(const ApplyArgs &a, uint32_t t0
     const uint32_t t = t0 + 1u + (threadIdx.x & 63u);
     return t < a.n_tensors ? as_global<uint32_t>(a.tile0)[t] : 0xffffffffu;
 }
-template <bool BF16>
+template <bool BF16, uint32_t W>
 __device__ __forceinline__ void load_four(FourTiles &f, const ApplyArgs &a, uint32_t k, uint32_t t0, uint32_t starts, uint32_t tile, uint32_t end)
 {
     const uint32_t e = (threadIdx.x & 63u) * 4u;
 #pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u, tile += 4u) {
+    for (uint32_t u = 0; u < 4u; ++u, tile += W) {
         f.n[u] = 0;
         if (tile < end) {
             const Record rec = load_record(a, k, t0 + (uint32_t)__popcll(__ballot(starts <= tile)));
@@ -201,7 +205,7 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const ApplyArgs a, const
         const uint32_t t0 = entry & ~kMoreInBlock, starts = later_starts(a, t0);
         const uint32_t end = first + kNormRun < a.ntiles ? first + kNormRun : a.ntiles;
         FourTiles f;
-        load_four<BF16>(f, a, k, t0, starts, first + w, end);
+        load_four<BF16, 4>(f, a, k, t0, starts, first + w, end);
 #pragma unroll
         for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, f.v[u]);
     }
@@ -225,6 +229,20 @@ __global__ __launch_bounds__(256) void mean_grad_norm_kernel(const ApplyArgs a, 
 }
 
 __device__ __forceinline__ float4 times(float4 v, float c) { return make_float4(v.x * c, v.y * c, v.z * c, v.w * c); }
+
+template <bool BF16>
+__device__ __forceinline__ void store_grad(char *g, uint32_t e, uint32_t n, float4 v)
+{
+    if (n == 4u) {
+        if constexpr (BF16) st2<0>(reinterpret_cast<uint16_t *>(g) + e, round4(v));
+        else st4<0>(reinterpret_cast<float *>(g) + e, v);
+    } else {
+        LASGD_FOR4(if (c < 3 && (uint32_t)c < n) {
+            if constexpr (BF16) as_global<uint16_t>(g)[e + c] = (uint16_t)bf16_round(compv(v, c));
+            else as_global<float>(g)[e + c] = compv(v, c);
+        })
+    }
+}
 
 // Clipping in place: gradients times c, rounded once to the storage type, where c is not 1.
 template <bool BF16, int NT>
@@ -258,20 +276,71 @@ __global__ __launch_bounds__(256) void scale_grads_kernel(const ApplyArgs a, con
         const uint32_t t0 = entry & ~kMoreInBlock, starts = later_starts(a, t0);
         const uint32_t end = first + kNormRun < a.ntiles ? first + kNormRun : a.ntiles;
         FourTiles f;
-        load_four<BF16>(f, a, k, t0, starts, first + w, end);
+        load_four<BF16, 4>(f, a, k, t0, starts, first + w, end);
 #pragma unroll
-        for (uint32_t u = 0; u < 4u; ++u) {
-            const float4 v = times(f.v[u], cl.c);
-            if (f.n[u] == 4u) {
-                if constexpr (BF16) st2<0>(reinterpret_cast<uint16_t *>(f.g[u]) + e, round4(v));
-                else st4<0>(reinterpret_cast<float *>(f.g[u]) + e, v);
-            } else {
-                LASGD_FOR4(if (c < 3 && (uint32_t)c < f.n[u]) {
-                    if constexpr (BF16) as_global<uint16_t>(f.g[u])[e + c] = (uint16_t)bf16_round(compv(v, c));
-                    else as_global<float>(f.g[u])[e + c] = compv(v, c);
-                })
-            }
-        }
+        for (uint32_t u = 0; u < 4u; ++u) store_grad<BF16>(f.g[u], e, f.n[u], times(f.v[u], cl.c));
+    }
+}
+
+// ---- short lists ---------------------------------------------------------------
+// Replicas of at most 64 tiles, the first block of the lookup table: a workgroup of sixteen waves takes one, a wave at most four of its tiles.  Their
+// gradients wait in registers for the norm, and everything is one launch.  Bound by latency.
+constexpr uint32_t kSmallWaves = 16;
+
+// The gradients of replica k, in f, and what comes of their norm, in all threads.
+template <bool BF16>
+__device__ __forceinline__ Clip small_norm(FourTiles &f, const ApplyArgs &a, const NormArgs &n, uint32_t k, uint32_t starts, uint32_t w)
+{
+    __shared__ Clip shared;
+    load_four<BF16, kSmallWaves>(f, a, k, 0u, starts, w, a.ntiles);
+    double acc = 0.0;
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, f.v[u]);
+    acc = block_sum<kSmallWaves>(acc);
+    if (threadIdx.x == 0u) shared = clip_of(n, k, acc);
+    __syncthreads();
+    return shared;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(1024) void small_scale_kernel(const ApplyArgs a, const NormArgs n)
+{
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = (threadIdx.x & 63u) * 4u;
+    const uint32_t k = n.count == a.K ? blockIdx.x : nth_bit(n.mask, blockIdx.x);
+    FourTiles f;
+    const Clip cl = small_norm<BF16>(f, a, n, k, later_starts(a, 0u), w);
+    if (cl.skip || cl.c == 1.f) return;
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u) store_grad<BF16>(f.g[u], e, f.n[u], times(f.v[u], cl.c));
+}
+
+// A local step, or one with the global update, of the replicas in the masks.  bf16 models this short are never in s alone.
+template <int OP, bool BF16>
+__global__ __launch_bounds__(1024) void small_step_kernel(const ApplyArgs a, const ExtArgs xa, const NormArgs n)
+{
+    const uint32_t lane = threadIdx.x & 63u, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t k = replica_at<true>(a, &xa, blockIdx.x);
+    const bool in_step = (xa.step_mask >> k) & 1ull, in_merge = (xa.merge_mask >> k) & 1ull;
+    const uint32_t starts = later_starts(a, 0u);
+    Clip cl{1.f, 0u};
+    FourTiles f;
+    if (in_step) cl = small_norm<BF16>(f, a, n, k, starts, w);
+    for (uint32_t tile = w; tile < a.ntiles; tile += kSmallWaves) {
+        const uint32_t tensor = (uint32_t)__popcll(__ballot(starts <= tile));
+        const Record rec = load_record(a, k, tensor);
+        const Tile t = locate(a, rec, tile, tensor, 256u);
+        float4 zt[1] = {make_float4(0.f, 0.f, 0.f, 0.f)};
+        if constexpr (OP == OP_STEP_MERGE) zt[0] = ld4<0>(a.z + t.aoff + lane * 4u);
+        char *xu = reinterpret_cast<char *>(rec.x) + t.toff * (BF16 ? 2u : 4u);
+        const char *gu = reinterpret_cast<const char *>(rec.g) + t.toff * (BF16 ? 2u : 4u);
+        const size_t ao = (size_t)k * a.npad + t.aoff;
+        float *xm = BF16 ? a.x32 + ao : nullptr;
+        const float nlr = xa.neg_lr_k[k];
+#define LASGD_SMALL(OPX) apply_tile<1, OPX, BF16, 0, false, true, false, false, true>(a, xu, gu, xm, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, nlr, xa.alpha, cl)
+        if (OP == OP_STEP || !in_merge) LASGD_SMALL(OP_STEP);
+        else if (in_step) LASGD_SMALL(OP_STEP_MERGE);
+        else LASGD_SMALL(OP_MERGE);
+#undef LASGD_SMALL
     }
 }
 

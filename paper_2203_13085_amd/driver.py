@@ -108,28 +108,39 @@ class DeviceReplicas:
         return self._get(self.x[k])
 
     # ---- Algorithm 1 with a fixed cadence ------------------------------------
-    def prologue(self, lr: float) -> None:
-        self.ctx.local_step(lr)      # steps 2-3
+    def _local_step(self, lr: float, max_norm: Optional[float]) -> None:
+        if max_norm is None:
+            self.ctx.local_step(lr)
+        else:
+            self.ctx.local_step_clip(lr, max_norm)
+
+    def prologue(self, lr: float, max_norm: Optional[float] = None) -> None:
+        self._local_step(lr, max_norm)   # steps 2-3
         self.ctx.snapshot()          # step 4: send
         self.ctx.average()           #         the All-Reduce starts on the side stream
 
-    def iteration(self, lr: float, tau: int, m: int, fused: bool = True, fused_mean: bool = False) -> int:
+    def iteration(self, lr: float, tau: int, m: int, fused: bool = True, fused_mean: bool = False,
+                  max_norm: Optional[float] = None) -> int:
         """Steps 6-9 for one tick of the local clock; returns the new tau.
+        max_norm: every replica's gradients are clipped to this norm in its local update (not with fused_mean).
         fused_mean: the global update and the next All-Reduce go out as one pass on the
         main stream (lasgd_step_merge_average) instead of step_merge + average."""
+        assert max_norm is None or not fused_mean, "the pass that also takes the mean does not clip"
         tau += 1
         if tau == m:
             if fused_mean:
                 self.ctx.step_merge_average(lr)
                 return 0
-            if fused:
+            if fused and max_norm is not None:
+                self.ctx.step_merge_clip(lr, max_norm)
+            elif fused:
                 self.ctx.step_merge(lr, True)
             else:
-                self.ctx.local_step(lr)
+                self._local_step(lr, max_norm)
                 self.ctx.merge(True)
             self.ctx.average()
             return 0
-        self.ctx.local_step(lr)
+        self._local_step(lr, max_norm)
         return tau
 
     def adaptive_iteration(self, lr: float, tau: int, tau_max: int, fused_mean: bool = False) -> tuple:

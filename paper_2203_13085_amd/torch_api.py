@@ -12,6 +12,10 @@ Gradient tensors are allocated here once and attached to the parameters
 (`p.grad`), so that autograd accumulates into buffers whose addresses never
 change; clear them with `zero_grad()` of this class (or
 `module.zero_grad(set_to_none=False)`), never by dropping them.
+
+With `max_grad_norm` every local update clips: each replica's gradients count times min(1, max_grad_norm / (norm + 1e-6)), the
+norm taken over all its parameters, inside the update and without writing the gradients.  `clip_grad_norm_()` scales them
+in place, for a program that updates by itself.
 """
 from __future__ import annotations
 
@@ -45,12 +49,19 @@ _walk = _load_walk()
 class LASGD:
     def __init__(self, replicas: Sequence[torch.nn.Module], lr: float, momentum: float = 0.9,
                  nesterov: bool = True, weight_decay: float = 0.0, m: int = 1,
-                 no_decay_1d: bool = False, side_stream: bool = True):
+                 no_decay_1d: bool = False, side_stream: bool = True, max_grad_norm: Optional[float] = None,
+                 skip_nonfinite: bool = False):
         """replicas: K modules with identical parameter lists on the same GPU, already
         holding the same initial weights (every node starts from the same model).
         m: local steps per global update (tau_max with the early exit disabled).
-        no_decay_1d: apply no weight decay to 1-D tensors (norm scales, biases)."""
+        no_decay_1d: apply no weight decay to 1-D tensors (norm scales, biases).
+        max_grad_norm: clip every replica's gradients to this norm in step() (None: no clipping; infinity: take the norms only);
+        step() then leaves the norms before clipping in `grad_norms`, a tensor of K floats on the GPU.
+        skip_nonfinite (with max_grad_norm): a replica whose gradients hold an infinity or a NaN takes no local update in
+        that step, and keeps its momentum; it still takes part in a global update."""
         assert len(replicas) >= 1 and m >= 1
+        assert max_grad_norm is None or max_grad_norm >= 0.0
+        assert max_grad_norm is not None or not skip_nonfinite, "skip_nonfinite needs a max_grad_norm (infinity: no limit)"
         self.replicas = list(replicas)
         self.params: List[List[torch.nn.Parameter]] = [[p for p in r.parameters() if p.requires_grad] for r in self.replicas]
         first = self.params[0]
@@ -66,6 +77,9 @@ class LASGD:
         self._flat = [p for ps in self.params for p in ps]
         self._bytes = np.array([p.numel() * p.element_size() for p in self._flat], dtype=np.uint64)    # what the library clears
         self.lr, self.m, self.tau, self.t = float(lr), int(m), 0, 0
+        self.max_grad_norm = None if max_grad_norm is None else float(max_grad_norm)
+        self.skip_nonfinite = bool(skip_nonfinite)
+        self.grad_norms = torch.zeros(len(self.replicas), device=dev)
         self.device = dev
         self.main = torch.cuda.Stream(device=dev)
         self.side = torch.cuda.Stream(device=dev) if side_stream else self.main
@@ -101,6 +115,30 @@ class LASGD:
             for g in grads:
                 g.zero_()
 
+    def clip_grad_norm_(self, max_norm: float, skip_nonfinite: bool = False) -> torch.Tensor:
+        """Scale every replica's gradients in place to a norm of at most `max_norm`, on the current stream's time line.
+        Returns the K norms before clipping, on the GPU.  skip_nonfinite: gradients with an infinity or a NaN stay as they are."""
+        self._check_in_place()
+        norms = torch.empty_like(self.grad_norms)
+        cur = torch.cuda.current_stream(self.device)
+        self.main.wait_stream(cur)                  # also with the memory of `norms`, which cur may have used before
+        self.ctx.clip_grads(float(max_norm), skip_nonfinite=skip_nonfinite, norms=norms.data_ptr())
+        cur.wait_stream(self.main)
+        torch.autograd.graph.increment_version([p.grad for p in self._flat])
+        return norms
+
+    def _check_in_place(self) -> None:
+        # the library scales the buffers it is bound to: each gradient has to be the one that was bound, plain
+        if _walk and self.ctx.is_open and _walk.state(self._flat, torch.nn.Parameter, b"".join(self.ctx.bound_grads), False,
+                                                      self._bytes) == 0:
+            return
+        assert self.ctx.is_open, "the optimizer is closed"
+        bound = [a for g in self.ctx.bound_grads for a in g]
+        for p, at, size in zip(self._flat, bound, self._bytes):
+            assert p.grad is not None, "a gradient buffer was dropped (use zero_grad(set_to_none=False))"
+            assert (p.grad.data_ptr() == at and p.grad.is_contiguous() and p.grad.dtype == p.dtype
+                    and p.grad.numel() * p.grad.element_size() == size), "a gradient is not the buffer that was bound"
+
     def _eager(self) -> bool:
         # the library's tables are there, nobody watches torch's operations, and no graph is recorded that could outlive the tables
         return (torch._C._len_torch_dispatch_stack() == 0 and torch._C._len_torch_function_stack() == 0
@@ -125,7 +163,7 @@ class LASGD:
         self.main.wait_stream(cur)                  # gradients are complete before the update reads them
         fired = False
         if not self._started:                       # steps 2-5: first update, send, start the All-Reduce
-            self.ctx.local_step(lr)
+            self._local_step(lr)
             self.ctx.snapshot()
             self.ctx.average()
             self._started = True
@@ -133,13 +171,23 @@ class LASGD:
         else:                                       # steps 6-9
             self.tau += 1
             if self.tau >= self.m:
-                self.ctx.step_merge(lr, True)
+                if self.max_grad_norm is None:
+                    self.ctx.step_merge(lr, True)
+                else:
+                    self.ctx.step_merge_clip(lr, self.max_grad_norm, skip_nonfinite=self.skip_nonfinite,
+                                             norms=self.grad_norms.data_ptr())
                 self.ctx.average()
                 self.tau, self.t, fired = 0, self.t + 1, True
             else:
-                self.ctx.local_step(lr)
+                self._local_step(lr)
         cur.wait_stream(self.main)                  # the next forward sees the new parameters
         return fired
+
+    def _local_step(self, lr: float) -> None:
+        if self.max_grad_norm is None:
+            self.ctx.local_step(lr)
+        else:
+            self.ctx.local_step_clip(lr, self.max_grad_norm, skip_nonfinite=self.skip_nonfinite, norms=self.grad_norms.data_ptr())
 
     def center(self) -> torch.Tensor:
         """The current mean model z (flat, fp32), e.g. for evaluation."""

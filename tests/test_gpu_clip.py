@@ -114,6 +114,11 @@ LISTS = {
     "many": tuple(1 + (37 * i) % 300 for i in range(150)),              # several tensors in every block of tiles, more than sixteen in some
     "blocks": (64 * 256, 64 * 256 - 1, 64 * 256 + 1, 5, 3 * 64 * 256 + 77),
     "long": (1_300_001, 3, 70_000),
+    "64 tiles": (16_384,),
+    "64 of one": (1,) * 64,
+    "63 and 300": (1,) * 62 + (300,),
+    "65 tiles": (16_385,),
+    "65 of one": (1,) * 65,
 }
 
 
@@ -178,7 +183,8 @@ def test_norms_of_values_whose_squares_leave_fp32(value, storage):
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
-@pytest.mark.parametrize("name,K", [("one", 1), ("odd", 3), ("rows", 5), ("many", 4), ("blocks", 3), ("long", 2), ("odd", 64)])
+@pytest.mark.parametrize("name,K", [("one", 1), ("odd", 3), ("rows", 5), ("many", 4), ("blocks", 3), ("long", 2), ("odd", 64),
+                                    ("64 tiles", 5), ("64 of one", 3), ("63 and 300", 9), ("65 tiles", 4), ("65 of one", 3), ("65 of one", 64)])
 def test_clip_in_place(name, K, storage):
     r = Rig(K, LISTS[name], storage)
     try:
@@ -272,7 +278,8 @@ def test_what_is_not_finite(bad, place, storage):
 @pytest.mark.parametrize("name,K,tuning", [("one", 1, {}), ("odd", 3, {}), ("rows", 5, dict(nontemporal=3)), ("many", 4, {}), ("blocks", 3, dict(nontemporal=3)),
                                            ("long", 2, dict(nontemporal=3)), ("odd", 64, {}), ("odd", 64, dict(nontemporal=3)),
                                            ("odd", 6, dict(vec=4, kper_step=2, waves_per_block=4, max_blocks=3)), ("odd", 6, dict(vec=2, waves_per_block=2)),
-                                           ("long", 3, {})])
+                                           ("long", 3, {}), ("64 tiles", 5, {}), ("64 tiles", 64, dict(vec=4)), ("64 of one", 3, {}),
+                                           ("63 and 300", 9, dict(nontemporal=3)), ("65 tiles", 4, dict(vec=2)), ("65 of one", 7, {}), ("65 of one", 64, dict(kper_step=5))])
 def test_local_steps(name, K, tuning, storage):
     r = Rig(K, LISTS[name], storage)
     try:
@@ -303,7 +310,8 @@ def test_local_steps(name, K, tuning, storage):
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("K,numels,tuning,side", [(3, LISTS["odd"], {}, True), (5, LISTS["rows"], dict(nontemporal=3), True), (2, LISTS["long"], {}, True),
                                                   (4, LISTS["many"], {}, False), (4, (700_001, 3, 256), {}, True), (4, (700_001, 3, 256), dict(nontemporal=3), True),
-                                                  (6, LISTS["odd"], dict(kper_merge=6, waves_per_block=2, vec=2), True)])
+                                                  (6, LISTS["odd"], dict(kper_merge=6, waves_per_block=2, vec=2), True), (5, LISTS["63 and 300"], {}, True),
+                                                  (7, LISTS["64 tiles"], dict(vec=4), True), (7, LISTS["65 of one"], dict(vec=4, kper_merge=3), True), (4, LISTS["65 tiles"], {}, False)])
 def test_global_updates(K, numels, tuning, side, storage):
     """Steps and updates in turn; masks of the step, of the update, and a replica that is not finite and takes the update all the same.
     The lists with 700,001 elements hold a bf16 model in one place after an update."""
@@ -478,7 +486,7 @@ def test_unclipped_sgd_all_reduce_after_a_clipped_one():
         r.close()
 
 
-@pytest.mark.parametrize("storage,n", [("f32", 5000), ("bf16", 5000), ("bf16", 700_001)])
+@pytest.mark.parametrize("storage,n", [("f32", 5000), ("f32", 50_000), ("bf16", 5000), ("bf16", 700_001)])
 def test_graphs(storage, n):
     """The first clipped calls of a context are recorded: a cycle, clipping in place and an All-Reduce step; replays with new gradients, with
     eager calls and other work between them."""
@@ -529,9 +537,10 @@ def test_graphs(storage, n):
         r.close()
 
 
-def test_eager_calls_come_before_the_first_replay():
+@pytest.mark.parametrize("name", ["odd", "blocks"])
+def test_eager_calls_come_before_the_first_replay(name):
     """Recorded first, replayed late: eager calls in between find what they need."""
-    r = Rig(3, LISTS["odd"], side_stream=False)
+    r = Rig(3, LISTS[name], side_stream=False)
     try:
         graph = torch.cuda.CUDAGraph()
         r.ctx.sync()
@@ -640,5 +649,142 @@ def test_refusals():
         e.clip_grads(1.0)                                       # needs no master
         e.close()
         c.close()
+    finally:
+        r.close()
+
+
+# ---- the torch class ------------------------------------------------------------------------------------------------
+def _modules(K, dtype=torch.float32):
+    torch.manual_seed(0)
+    base = torch.nn.Sequential(torch.nn.Linear(20, 33), torch.nn.ReLU(), torch.nn.Linear(33, 5)).to("cuda:0", dtype)
+    return base, [copy.deepcopy(base) for _ in range(K)]
+
+
+def _flat(tensors):
+    return np.concatenate([t.detach().float().cpu().numpy().ravel() for t in tensors])
+
+
+def _backward(replicas, step, dtype=torch.float32):
+    for k, model in enumerate(replicas):
+        g = torch.Generator(device="cuda:0")
+        g.manual_seed(1000 * step + k)
+        x = torch.randn(16, 20, generator=g, device="cuda:0").to(dtype)
+        y = torch.randn(16, 5, generator=g, device="cuda:0").to(dtype)
+        torch.nn.functional.mse_loss(model(x), y).mul((1.0, 20.0, 0.05)[k % 3]).backward()
+
+
+@pytest.mark.parametrize("m", [1, 3])
+@pytest.mark.parametrize("skip", [False, True])
+def test_modules_train_with_clipped_gradients(m, skip):
+    """The whole use: backward, clipped step, now and then an overflow in one replica's backward pass."""
+    from paper_2203_13085_amd.torch_api import LASGD
+    K, lr, mu, wd, most = 3, 0.05, 0.9, 1e-3, 0.5
+    base, replicas = _modules(K)
+    opt = LASGD(replicas, lr=lr, momentum=mu, nesterov=True, weight_decay=wd, m=m, max_grad_norm=most, skip_nonfinite=skip)
+    ps = list(base.parameters())
+    orc = O32.Oracle(K, [p.numel() for p in ps], mu, True, [wd] * len(ps))
+    orc.set_model(_flat(ps))
+    clipped = 0
+    try:
+        tau, started = 0, False
+        for step in range(8):
+            opt.zero_grad()
+            _backward(replicas, step)
+            if skip and step in (2, 5):
+                list(replicas[step % K].parameters())[1].grad[4] = INF
+            torch.cuda.synchronize()
+            grads = [_flat([p.grad for p in r.parameters()]) for r in replicas]
+            norms = [norm64(g) for g in grads]
+            live = sum(1 << k for k in range(K) if np.isfinite(norms[k]))
+            clipped += sum(n > most for n in norms)
+            opt.step()
+            check_norms(opt.grad_norms.cpu().numpy().astype(np.float64), norms)
+            with np.errstate(invalid="ignore"):
+                orc.local_step([coefficient(n, most) * g for n, g in zip(norms, grads)], [lr] * K, mask=live)
+            tau += 1
+            if not started:
+                orc.snapshot(); orc.average(); started, tau = True, 0
+            elif tau == m:
+                orc.merge(True); orc.average(); tau = 0
+            torch.cuda.synchronize()
+            for k, r in enumerate(replicas):
+                assert_close(_flat(list(r.parameters())), orc.x[k], f"step {step} replica {k}")
+        assert 0 < clipped < 8 * K
+    finally:
+        opt.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_clip_grad_norm_in_place(dtype):
+    """Against torch's own, replica by replica; the version counters notice; the caller's stream need not be waited for by hand."""
+    from paper_2203_13085_amd.torch_api import LASGD
+    K, most = 3, 0.5
+    _, replicas = _modules(K, dtype)
+    opt = LASGD(replicas, lr=0.1)
+    try:
+        opt.zero_grad()
+        _backward(replicas, 0, dtype)
+        torch.cuda.synchronize()
+        before = [[p.grad.detach().clone() for p in r.parameters()] for r in replicas]
+        versions = [p.grad._version for p in opt._flat]
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            norms = opt.clip_grad_norm_(most)
+            after = [[p.grad.clone() for p in r.parameters()] for r in replicas]        # on s, right behind it
+        s.synchronize()
+        for k in range(K):
+            n = norm64(_flat(before[k]))
+            check_norms([float(norms[k])], [n])
+            for a, b in zip(after[k], before[k]):
+                want = torch.from_numpy(coefficient(n, most) * b.float().cpu().numpy()).to(dtype)
+                assert torch.equal(a.cpu(), want)
+        assert all(p.grad._version > v for p, v in zip(opt._flat, versions))
+        # another tensor in a gradient's place is not what the library is bound to
+        keep = opt._flat[1].grad
+        opt._flat[1].grad = keep.clone()
+        with pytest.raises(AssertionError, match="not the buffer"):
+            opt.clip_grad_norm_(most)
+        opt._flat[1].grad = None
+        with pytest.raises(AssertionError, match="dropped"):
+            opt.clip_grad_norm_(most)
+        opt._flat[1].grad = keep
+        opt.clip_grad_norm_(most)
+    finally:
+        opt.close()
+    with pytest.raises(AssertionError, match="closed"):
+        opt.clip_grad_norm_(most)
+
+
+def test_class_arguments():
+    from paper_2203_13085_amd.torch_api import LASGD
+    _, replicas = _modules(1)
+    for kw in (dict(max_grad_norm=-1.0), dict(max_grad_norm=float("nan")), dict(skip_nonfinite=True)):
+        with pytest.raises(AssertionError):
+            LASGD(replicas, lr=0.1, **kw)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_driver_loop(storage):
+    """The fixed-cadence loop of the driver, clipped, fused and in two calls, against the oracle."""
+    r = Rig(4, (70_000, 5, 1024), storage)
+    try:
+        g = r.grads(0)
+        r.load(g)
+        most = r.max_norm(g)
+        r.dev.prologue(r.w.lr, most)
+        r.orc.local_step(r.clipped(g, most), r.w.lr)
+        r.orc.snapshot()
+        r.orc.average()
+        tau = 0
+        for step in range(1, 5):
+            g = r.grads(step)
+            r.load(g)
+            tau = r.dev.iteration(r.w.lr, tau, 2, fused=step < 3, max_norm=most)
+            r.orc.local_step(r.clipped(g, most), r.w.lr)
+            if tau == 0:
+                r.orc.merge(True)
+                r.orc.average()
+            r.same(f"step {step}")
     finally:
         r.close()
