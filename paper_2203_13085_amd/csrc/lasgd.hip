@@ -59,7 +59,7 @@ struct lasgd_ctx {
     float *gbar = nullptr;           // mean gradient [npad] of an SGD All-Reduce step in two kernels, see reserve_mean_grad
     bool gbar_tried = false;         // asked for; without it the step always takes one kernel
     char *norm_mem = nullptr;        // what the clipped calls keep between their kernels, see reserve_norms
-    double *norm_part = nullptr;     // [K][kNormParts], or kMeanParts of the mean gradient
+    double *norm_part = nullptr;     // [K][kNormParts]
     Clip *clip = nullptr;            // [K]
     uint32_t *arrived = nullptr;     // [K][kArriveStride], zero between calls
     bool arrived_clear = false;      // it has been cleared, on the main stream and not in a recording
@@ -837,19 +837,30 @@ lasgd_status check_ready_to_step(lasgd_ctx *c, float lr)
 
 // What the kernels of a call hand on: the parts of each sum, and what comes of each norm.  For those alone that make the calls it is for; the
 // first of them asks, before it enqueues anything, also while it is being recorded.
-constexpr uint32_t kNormParts = 768;      // see grad_norm_kernel
-// us at 512 / 1024 / 2048 / 8192 workgroups, all calls: ResNet-50 list K = 8 691 / 692 / 695 / 697, ResNet-18 K = 8 315 / 316 / 316 / 321, MobileNetV2
-// K = 4 48.3 / 51.4 / 54.0 / 62.2, one vector of 2^20, K = 4 15.7 / 18.6 / 18.5 / 18.5.
-constexpr uint32_t kMeanParts = 512;
-uint32_t norm_groups(uint32_t ntiles, uint32_t replicas)      // workgroups for each of them
+// Workgroups of sixteen waves, for all replicas of a call together: as many as have 64 KiB of loads in flight a CU.  us at 128 / 192 / 256 / 384 /
+// 512, three states in turn on one stream: ResNet-50 list K = 8 168 / 127 / 125 / 139 / 130 (6.5 TB/s), ResNet-18 K = 8 78 / 63 / 61 / 66 / 63, MobileNetV2 K = 16
+// 53 / 41 / 38.5 / 41 / 39, one vector of 30,000,001 26.3 / 21.4 / 21.7 / 23.4 / 24.8; bf16 ResNet-50 K = 32 388 / 284 / 247 / 255 / 242 (6.8 TB/s), MobileNetV2 K = 16
+// 40 / 31 / 24.8 / 24.3 / 23.5.  With workgroups of four waves, at their best number for each list (768 to 2048): 125, 60, 37, 26.7 (2048 of them 42), 242, 23.4;
+// one vector of 2^20, K = 4 7.0, with these 6.1.
+constexpr uint32_t kNormParts = 512;
+uint32_t norm_groups(bool bf16, uint32_t ntiles, uint32_t replicas)      // for each of them
 {
-    const uint32_t runs = (ntiles + kNormRun - 1u) / kNormRun, most = kNormParts / replicas;
+    const uint32_t runs = (ntiles + kNormRun - 1u) / kNormRun, most = (bf16 ? 512u : 256u) / replicas;
     return runs < most ? runs : most;
+}
+// The mean gradient's: us at 64 / 128 / 192 / 256 / 384 / 512, whole calls: ResNet-50 list K = 8 797 / 693 / 674 / 668 / 678 / 671, bf16 ResNet-18 K = 20
+// 855 / 773 / 749 / 740 / 753 / 746, MobileNetV2 K = 4 66 / 58 / 54.7 / 54.8 / 58.5 / 58.3, one vector of 2^20, K = 4 20.8 / 20.2 / 20.7 / 21.2 / 21.2 / 21.2.  Workgroups of
+// four waves, at their best: 656, 744, 58.3, 21.9.
+constexpr uint32_t kMeanParts = 256;
+uint32_t mean_norm_groups(uint32_t ntiles)                    // whole rows of XCDs
+{
+    const uint32_t all = ((ntiles + kNormWaves - 1u) / kNormWaves + 7u) & ~7u;
+    return all < kMeanParts ? all : kMeanParts;
 }
 lasgd_status reserve_norms(lasgd_ctx *c)
 {
     if (c->norm_mem) return LASGD_OK;
-    const size_t parts = ((size_t)c->K * kNormParts > kMeanParts ? (size_t)c->K * kNormParts : kMeanParts) * sizeof(double);
+    const size_t parts = (size_t)c->K * kNormParts * sizeof(double);      // more than kMeanParts
     hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;        // allowed while a stream of this thread is being recorded, and not recorded
     (void)hipThreadExchangeStreamCaptureMode(&mode);
     const hipError_t e = hipMalloc((void **)&c->norm_mem, parts + (size_t)c->K * (sizeof(Clip) + kArriveStride * sizeof(uint32_t)));
@@ -884,12 +895,6 @@ hipError_t clear_arrived(lasgd_ctx *c)
     return e;
 }
 
-uint32_t mean_norm_groups(uint32_t ntiles)                    // of four waves, each with a tile at a time; whole rows of XCDs
-{
-    const uint32_t all = ((ntiles + 3u) / 4u + 7u) & ~7u;
-    return all < kMeanParts ? all : kMeanParts;
-}
-
 NormArgs norm_args(const lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, uint32_t ntiles)
 {
     NormArgs n{};
@@ -898,7 +903,7 @@ NormArgs norm_args(const lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, ui
     n.stride = kNormParts;
     n.mask = mask;
     n.count = (uint32_t)__builtin_popcountll(mask);
-    n.parts = norm_groups(ntiles, n.count);
+    n.parts = norm_groups(c->storage == LASGD_BF16, ntiles, n.count);
     n.clip = c->clip;
     n.norms = clip.norms;
     n.max_norm = clip.max_norm;
@@ -908,21 +913,21 @@ NormArgs norm_args(const lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, ui
 
 uint64_t grad_bytes(const lasgd_ctx *c, uint32_t replicas) { return replicas * c->packed * (c->storage == LASGD_BF16 ? 2u : 4u); }
 
-// Gradients are read for their norm and then again.  So many replicas are taken at a time as leave their gradients in the 256 MB memory-side
-// cache until then: from 104 MiB of gradients on two batches or more of one length.  us at so many MB of gradients a batch, all at once last (three
-// states in turn; the unclipped step): ResNet-18 list K = 8 47 342, 94 329, 140 334, 187 353, 374 357 (293); ResNet-50 K = 8 102 736, 204 774, 818 812
-// (631), bf16 K = 32 51 2693, 102 2633, 204 2675, 409 2832, 1636 2891 (2600); MobileNetV2 K = 16 28 215, 56 197, 84 200, 98 201, 112 209, 224 209
-// (172), bf16 K = 32 28 to 112 370, 224 384; six vectors of 20,000,001 80 420, 160 434, 480 454 (373).  In place, everything scaled: ResNet-50 K = 8
-// 102 265, 818 294.  A global update reads z for all replicas of a tile, and in batches it reads z again: ResNet-18 K = 8, with its mean, 94 MB
-// 566, all at once 547, bf16 K = 16 845, 803.  So it takes the norms of all first.
+// Gradients are read for their norm and then again, and the 256 MB memory-side cache keeps part of them between.  bf16 steps, and clipping in
+// place, take so many replicas at a time that it keeps more of them than the further launches cost: batches of one length, up to 400 MiB of gradients each.  us at so
+// many MB of gradients a batch, all at once last (three states in turn on one stream): bf16 step ResNet-50 list K = 32 204 2749, 307 2650, 409 2641, 613 2659, 818
+// 2678, 1636 2724, K = 8 204 686, 409 673, ResNet-18 K = 16 187 609, 374 605; in place, everything scaled, ResNet-50 K = 8 204 516, 409 414, 818 418, bf16
+// K = 32 409 805, 818 844, 1636 870, ResNet-18 K = 16 187 191, 374 180.  fp32 steps, which write more than they read of gradients, gain nothing: ResNet-50
+// K = 8 102 845, 204 773, 409 774, 818 770, ResNet-18 K = 8 187 388, 374 346.  (With each state on a stream of its own batches overlap with other states' and
+// the smallest are best; that is not how a context is used.)  A global update reads z once for all replicas of a tile, and in batches again: it takes all at once.
 //
-// A read for the norm goes without the hint where the second one follows soon enough, us without / with: step, MobileNetV2 K = 4 48.8 / 51.6, K = 8
-// 100.9 / 102.1, bf16 K = 16 185 / 197; step + update, with its mean, MobileNetV2 K = 8 (112 MB) 161 / 168, bf16 K = 16 246 / 252, K = 32 (224 MB) 479 / 483, fp32
-// K = 16 (224 MB) 326 / 321, ResNet-18 K = 8 558 / 547, bf16 K = 12 (280 MB) 607 / 595.  The norms alone: MobileNetV2 bf16 K = 16 17.5 / 16.8, ResNet-50 K = 8
-// 134 / 117.5.
-constexpr uint64_t kNormBytes = 104ull << 20, kNormHintFrom = 160ull << 20;
-uint32_t norm_batch(const lasgd_ctx *c, uint32_t replicas)
+// The read for a norm goes without the streaming hint where a second read follows, us without / with: step ResNet-50 bf16 K = 8 673 / 693, ResNet-18 bf16 K = 16
+// 605 / 631, fp32 K = 8 346 / 345, MobileNetV2 K = 8 107 / 109, K = 4 72 / 73; step + update, with its mean, ResNet-50 K = 8 1189 / 1209, ResNet-18 K = 8 551 / 556,
+// MobileNetV2 K = 16 327 / 325, bf16 253 / 258.  The norms alone: ResNet-50 K = 8 141 / 125, MobileNetV2 bf16 K = 16 25.1 / 23.5.
+constexpr uint64_t kNormBytes = 400ull << 20;
+uint32_t norm_batch(const lasgd_ctx *c, uint32_t replicas, bool in_place)
 {
+    if (!in_place && c->storage != LASGD_BF16) return replicas;
     const uint64_t batches = (grad_bytes(c, replicas) + kNormBytes - 1) / kNormBytes;
     return batches >= replicas ? 1u : (uint32_t)((replicas + batches - 1) / batches);
 }
@@ -947,7 +952,7 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
     if (!clips) n.clip = nullptr;
     hipError_t e = clear_arrived(c);
     if (e == hipSuccess) {
-        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 1) != 0 : !clips || grad_bytes(c, n.count) >= kNormHintFrom;
+        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 1) != 0 : !clips;
         const dim3 grid(n.parts, n.count), bs(kNormThreads);
         if (c->storage == LASGD_BF16) {
             if (hint) hipLaunchKernelGGL((grad_norm_kernel<true, 1>), grid, bs, 0, c->main, a, n);
@@ -962,14 +967,11 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
     return LASGD_OK;
 }
 
-// Lists this short take one launch for norm and update (small_step_kernel): the host is what bounds two of them.  us, two launches / one, three
-// states in turn: step, 300 to 16384 elements, K = 3 to 64 7.1-8.0 / 4.0-4.9; in place 5.4-6.8 / 3.2-3.9; step + update, with its mean, 300 elements
-// K = 3 9.2 / 7.1, 16384 K = 16 12.6 / 10.1; 9000 K = 64 12.8 / 11.3, but 16384 K = 64 (4096 tiles in 64 workgroups) 13.8 / 14.3.
-bool one_launch(const lasgd_ctx *c, int op, uint32_t replicas)
-{
-    const uint32_t ntiles = c->tables_by_vec[0].ntiles;
-    return ntiles <= 4u * kSmallWaves && (op != OP_STEP_MERGE || ntiles * replicas <= 3072u);
-}
+// Lists this short take one launch for the norm and what follows (small_step_kernel): two of them are bound by the host, one of long lists by its one
+// workgroup a replica.  us, two launches / one, three states in turn on one stream: step, 300 elements K = 3 to 64 5.9-6.0 / 3.3-3.4, 4000 5.9-6.1 / 3.7-4.1,
+// 9000 5.9-9.0 / 4.5-5.7, 12288 K = 3 7.9 / 5.5, K = 64 8.2 / 6.5, bf16 6.6-8.3 / 6.0-7.0, 16384 K = 3 5.9 / 5.8, bf16 5.8 / 6.6; step + update, with its mean, 300 K = 3
+// 10.7 / 9.2, 9000 15 / 12.6, 12288 K = 16 14.6 / 13.7, K = 64 16.5 / 16.6, 16384 13.7 / 14.8; in place 16384 K = 3 5.9 / 3.3, K = 64 7.8 / 4.3.
+bool one_launch(const lasgd_ctx *c, bool in_place) { return c->tables_by_vec[0].ntiles <= (in_place ? 4u : 3u) * kSmallWaves; }
 
 lasgd_status launch_small(lasgd_ctx *c, ApplyPlan &p, const lasgd_clip &clip)
 {
@@ -979,11 +981,11 @@ lasgd_status launch_small(lasgd_ctx *c, ApplyPlan &p, const lasgd_clip &clip)
     const NormArgs n = norm_args(c, taking, clip, p.a.ntiles);
     const dim3 grid(n.count), bs(64u * kSmallWaves);
     if (p.op == OP_STEP) {
-        if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_step_kernel<OP_STEP, true>), grid, bs, 0, c->main, p.a, p.ext, n);
-        else hipLaunchKernelGGL((small_step_kernel<OP_STEP, false>), grid, bs, 0, c->main, p.a, p.ext, n);
+        if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_step_kernel<true>), grid, bs, 0, c->main, p.a, p.ext, n);
+        else hipLaunchKernelGGL((small_step_kernel<false>), grid, bs, 0, c->main, p.a, p.ext, n);
     } else {
-        if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_step_kernel<OP_STEP_MERGE, true>), grid, bs, 0, c->main, p.a, p.ext, n);
-        else hipLaunchKernelGGL((small_step_kernel<OP_STEP_MERGE, false>), grid, bs, 0, c->main, p.a, p.ext, n);
+        if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_update_kernel<true>), grid, bs, 0, c->main, p.a, p.ext, n);
+        else hipLaunchKernelGGL((small_update_kernel<false>), grid, bs, 0, c->main, p.a, p.ext, n);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
@@ -1207,9 +1209,9 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
     const bool uniform = fill_ext(c, x, lr_k, mask, 0);
     if (clip) {
         ApplyPlan p;
-        if (one_launch(c, OP_STEP, (uint32_t)__builtin_popcountll(mask))) return (st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK ? st : launch_small(c, p, *clip);
+        if (one_launch(c, false)) return (st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK ? st : launch_small(c, p, *clip);
         if ((st = reserve_norms(c)) != LASGD_OK) return st;
-        const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking);
+        const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking, false);
         const bool plain = uniform && mask == c->all && batch == taking;
         if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, true)) != LASGD_OK) return st;
         if (batch == taking) return (st = enqueue_norms(c, mask, *clip)) != LASGD_OK ? st : launch_apply(c, p);
@@ -1299,7 +1301,7 @@ static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, 
     const bool plain = merge_mask == c->all && c->alpha == 1.f &&
                        (op == OP_MERGE || (step_mask == c->all && uniform));
     ApplyPlan p;
-    const bool small = clip && one_launch(c, op, (uint32_t)__builtin_popcountll(step_mask | merge_mask));
+    const bool small = clip && one_launch(c, false);
     if (clip && !small && (st = reserve_norms(c)) != LASGD_OK) return st;
     if (plain && !small) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0, nullptr, clip != nullptr);
     else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, clip != nullptr);
@@ -1488,7 +1490,7 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
     ApplyArgs a{};
     fill_common(c, a);
     fill_fine(c, a);
-    if (one_launch(c, OP_STEP, (uint32_t)c->K)) {
+    if (one_launch(c, true)) {
         const NormArgs n = norm_args(c, mask, *clip, a.ntiles);
         if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_scale_kernel<true>), dim3(n.count), dim3(64u * kSmallWaves), 0, c->main, a, n);
         else hipLaunchKernelGGL((small_scale_kernel<false>), dim3(n.count), dim3(64u * kSmallWaves), 0, c->main, a, n);
@@ -1496,11 +1498,12 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
         return e == hipSuccess ? LASGD_OK : fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
     }
     if ((st = reserve_norms(c)) != LASGD_OK) return st;
-    for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask)); mask;) {
+    for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask), true); mask;) {
         const uint64_t now = take_replicas(mask, batch);
         if ((st = enqueue_norms(c, now, *clip)) != LASGD_OK) return st;
-        const NormArgs n = norm_args(c, now, *clip, a.ntiles);
-        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 3) != 0 : grad_bytes(c, (uint32_t)c->K) >= kNormBytes;
+        NormArgs n = norm_args(c, now, *clip, a.ntiles);
+        n.parts = norm_groups(true, a.ntiles, n.count);
+        const bool hint = (hint_of(c, USE_CYCLE) & 3) != 0;
         const dim3 grid(n.parts, n.count), bs(kNormThreads);
         if (c->storage == LASGD_BF16) {
             if (hint) hipLaunchKernelGGL((scale_grads_kernel<true, 3>), grid, bs, 0, c->main, a, n);

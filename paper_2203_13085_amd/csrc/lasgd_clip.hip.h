@@ -12,8 +12,8 @@
 
 namespace lasgd {
 
-constexpr uint32_t kNormThreads = 256;
-constexpr uint32_t kNormRun = 16;              // tiles a workgroup takes at a time
+constexpr uint32_t kNormThreads = 1024, kNormWaves = kNormThreads / 64u;
+constexpr uint32_t kNormRun = 4u * kNormWaves;      // tiles a workgroup takes at a time, four a wave
 constexpr uint32_t kArriveStride = 32;          // words: 128 bytes
 
 struct NormArgs {
@@ -87,7 +87,7 @@ __device__ __forceinline__ void join_norm(const NormArgs &n, uint32_t k, uint32_
 {
     __shared__ uint32_t last;
     double *part = n.part + (size_t)k * n.stride;
-    acc = block_sum<kNormThreads / 64u>(acc);
+    acc = block_sum<kNormWaves>(acc);
     if (groups == 1u) {
         if (threadIdx.x == 0u) finish_norm(n, k, acc);
         return;
@@ -101,7 +101,7 @@ __device__ __forceinline__ void join_norm(const NormArgs &n, uint32_t k, uint32_
     if (!last) return;
     acc = 0.0;
     for (uint32_t i = threadIdx.x; i < groups; i += kNormThreads) acc += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    acc = block_sum<kNormThreads / 64u>(acc);
+    acc = block_sum<kNormWaves>(acc);
     if (threadIdx.x != 0u) return;
     __hip_atomic_store(n.arrived + k * kArriveStride, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     finish_norm(n, k, acc);
@@ -180,14 +180,12 @@ __device__ __forceinline__ void load_four(FourTiles &f, const ApplyArgs &a, uint
 
 // Sums of squares of one replica's gradients (blockIdx.y: of which).
 //
-// Few workgroups that go on (norm_groups in the host code): a share, and its arrival, is one atomic each at the memory all XCDs see. us, 768
-// workgroups / 1024 / 1536 / 2048: ResNet-50 list K = 8 117.5 / 117.7 / 121.5 / 125.5 (6.96 TB/s), ResNet-18 K = 8 53.4 / 54.7 / 57.2 / 58.6,
-// MobileNetV2 bf16 K = 16 16.8 / 16.8 / 17.2 / 17.5, one vector of 30,000,001 17.9 / 19.0 / 20.5 / 25.7; ResNet-50 bf16 K = 32 is 227 to 229 with all. Three
-// of them a CU have 48 KiB of fp32 loads in flight.  Runs of 64 tiles, at their best number of workgroups: 127, 54.8, 18.2, 17.5, 225.
+// Few and large workgroups that go on: a share and its arrival are an atomic each at the memory all XCDs see, and arrivals at one
+// counter come one after the other, 10 ns each.  norm_groups in the host code holds their number and what it measured.
 template <bool BF16, int NT>
-__global__ __launch_bounds__(256) void grad_norm_kernel(const ApplyArgs a, const NormArgs n)
+__global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(const ApplyArgs a, const NormArgs n)
 {
-    constexpr uint32_t ROUNDS = kNormRun * 256u * (BF16 ? 2u : 4u) / (256u * 16u);          // of 16 bytes a thread
+    constexpr uint32_t ROUNDS = kNormRun * 256u * (BF16 ? 2u : 4u) / (kNormThreads * 16u);          // of 16 bytes a thread
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t k = n.count == a.K ? blockIdx.y : nth_bit(n.mask, blockIdx.y);
     const uint32_t runs = (a.ntiles + kNormRun - 1u) / kNormRun;
@@ -197,7 +195,7 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const ApplyArgs a, const
         if (const char *p = whole_run<BF16>(a, k, first, entry)) {
             u32x4_t v[ROUNDS];
 #pragma unroll
-            for (uint32_t u = 0; u < ROUNDS; ++u) v[u] = ld_u4<NT>(p + threadIdx.x * 16u + u * 4096u);
+            for (uint32_t u = 0; u < ROUNDS; ++u) v[u] = ld_u4<NT>(p + threadIdx.x * 16u + u * kNormThreads * 16u);
 #pragma unroll
             for (uint32_t u = 0; u < ROUNDS; ++u) add_squares<BF16>(a0, a1, v[u]);
             continue;
@@ -205,7 +203,7 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const ApplyArgs a, const
         const uint32_t t0 = entry & ~kMoreInBlock, starts = later_starts(a, t0);
         const uint32_t end = first + kNormRun < a.ntiles ? first + kNormRun : a.ntiles;
         FourTiles f;
-        load_four<BF16, 4>(f, a, k, t0, starts, first + w, end);
+        load_four<BF16, kNormWaves>(f, a, k, t0, starts, first + w, end);
 #pragma unroll
         for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, f.v[u]);
     }
@@ -214,11 +212,11 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const ApplyArgs a, const
 
 // The mean gradient of all replicas (mean_grad_tile) and its norm in one pass.  A wave's tiles stay on its XCD, where the step looks for them.
 template <bool BF16, int NT>
-__global__ __launch_bounds__(256) void mean_grad_norm_kernel(const ApplyArgs a, const NormArgs n)
+__global__ __launch_bounds__(kNormThreads) void mean_grad_norm_kernel(const ApplyArgs a, const NormArgs n)
 {
     const uint32_t lane = threadIdx.x & 63u, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     double acc = 0.0;
-    for (uint32_t tile = w * n.parts + blockIdx.x; tile < a.ntiles; tile += 4u * n.parts) {
+    for (uint32_t tile = w * n.parts + blockIdx.x; tile < a.ntiles; tile += kNormWaves * n.parts) {
         const uint32_t tensor = tensor_of(a, tile);
         const Tile t = locate(a, load_record(a, 0, tensor), tile, tensor, 256u);
         // the lanes beyond a tensor's end have a mean of zero
@@ -246,9 +244,9 @@ __device__ __forceinline__ void store_grad(char *g, uint32_t e, uint32_t n, floa
 
 // Clipping in place: gradients times c, rounded once to the storage type, where c is not 1.
 template <bool BF16, int NT>
-__global__ __launch_bounds__(256) void scale_grads_kernel(const ApplyArgs a, const NormArgs n)
+__global__ __launch_bounds__(kNormThreads) void scale_grads_kernel(const ApplyArgs a, const NormArgs n)
 {
-    constexpr uint32_t ROUNDS = kNormRun * 256u * (BF16 ? 2u : 4u) / (256u * 16u);
+    constexpr uint32_t ROUNDS = kNormRun * 256u * (BF16 ? 2u : 4u) / (kNormThreads * 16u);
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = (threadIdx.x & 63u) * 4u;
     const uint32_t k = n.count == a.K ? blockIdx.y : nth_bit(n.mask, blockIdx.y);
     const Clip cl = load_clip(n.clip, k);
@@ -259,7 +257,7 @@ __global__ __launch_bounds__(256) void scale_grads_kernel(const ApplyArgs a, con
         if (char *p = whole_run<BF16>(a, k, first, entry)) {
             u32x4_t v[ROUNDS];
 #pragma unroll
-            for (uint32_t u = 0; u < ROUNDS; ++u) v[u] = ld_u4<NT>(p + threadIdx.x * 16u + u * 4096u);
+            for (uint32_t u = 0; u < ROUNDS; ++u) v[u] = ld_u4<NT>(p + threadIdx.x * 16u + u * kNormThreads * 16u);
 #pragma unroll
             for (uint32_t u = 0; u < ROUNDS; ++u) {
                 if constexpr (BF16) {
@@ -269,14 +267,14 @@ __global__ __launch_bounds__(256) void scale_grads_kernel(const ApplyArgs a, con
                     const float4 t = times(make_float4(__uint_as_float(v[u].x), __uint_as_float(v[u].y), __uint_as_float(v[u].z), __uint_as_float(v[u].w)), cl.c);
                     v[u] = u32x4_t{__float_as_uint(t.x), __float_as_uint(t.y), __float_as_uint(t.z), __float_as_uint(t.w)};
                 }
-                st_u4<NT>(p + threadIdx.x * 16u + u * 4096u, v[u]);
+                st_u4<NT>(p + threadIdx.x * 16u + u * kNormThreads * 16u, v[u]);
             }
             continue;
         }
         const uint32_t t0 = entry & ~kMoreInBlock, starts = later_starts(a, t0);
         const uint32_t end = first + kNormRun < a.ntiles ? first + kNormRun : a.ntiles;
         FourTiles f;
-        load_four<BF16, 4>(f, a, k, t0, starts, first + w, end);
+        load_four<BF16, kNormWaves>(f, a, k, t0, starts, first + w, end);
 #pragma unroll
         for (uint32_t u = 0; u < 4u; ++u) store_grad<BF16>(f.g[u], e, f.n[u], times(f.v[u], cl.c));
     }
@@ -284,7 +282,8 @@ __global__ __launch_bounds__(256) void scale_grads_kernel(const ApplyArgs a, con
 
 // ---- short lists ---------------------------------------------------------------
 // Replicas of at most 64 tiles, the first block of the lookup table: a workgroup of sixteen waves takes one, a wave at most four of its tiles.  Their
-// gradients wait in registers for the norm, and everything is one launch.  Bound by latency.
+// gradients wait in registers for the norm, and everything is one launch.  Bound by latency: 4.8 us a step of the list of 5,453 elements in six tensors,
+// K = 3, in two launches 8.4.  one_launch in the host code holds the line.
 constexpr uint32_t kSmallWaves = 16;
 
 // The gradients of replica k, in f, and what comes of their norm, in all threads.
@@ -314,9 +313,62 @@ __global__ __launch_bounds__(1024) void small_scale_kernel(const ApplyArgs a, co
     for (uint32_t u = 0; u < 4u; ++u) store_grad<BF16>(f.g[u], e, f.n[u], times(f.v[u], cl.c));
 }
 
-// A local step, or one with the global update, of the replicas in the masks.  bf16 models this short are never in s alone.
-template <int OP, bool BF16>
+// A local step of the replicas in the mask.  Model and momentum are asked for with the gradients and wait in registers too.
+// bf16 models this short are never in s alone.
+template <bool BF16>
 __global__ __launch_bounds__(1024) void small_step_kernel(const ApplyArgs a, const ExtArgs xa, const NormArgs n)
+{
+    __shared__ Clip shared;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = (threadIdx.x & 63u) * 4u;
+    const uint32_t k = replica_at<true>(a, &xa, blockIdx.x), starts = later_starts(a, 0u);
+    float4 g[4], x[4], v[4];
+    char *xu[4];
+    float *vp[4], *xm[4], wd[4];
+    uint32_t m[4];
+    double acc = 0.0;
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u) {
+        const uint32_t tile = w + u * kSmallWaves;
+        m[u] = 0;
+        g[u] = x[u] = v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (tile < a.ntiles) {
+            const uint32_t tensor = (uint32_t)__popcll(__ballot(starts <= tile));
+            const Record rec = load_record(a, k, tensor);
+            const Tile t = locate(a, rec, tile, tensor, 256u);
+            const size_t ao = (size_t)k * a.npad + t.aoff;
+            m[u] = lane_elems<false>(e, t.count);
+            wd[u] = t.wd;
+            xu[u] = reinterpret_cast<char *>(rec.x) + t.toff * (BF16 ? 2u : 4u);
+            vp[u] = a.v + ao;
+            xm[u] = BF16 ? a.x32 + ao : reinterpret_cast<float *>(xu[u]);
+            if (m[u]) {
+                g[u] = grad_at<BF16>(reinterpret_cast<const char *>(rec.g) + t.toff * (BF16 ? 2u : 4u), e, m[u]);
+                x[u] = grad_at<false>(reinterpret_cast<const char *>(xm[u]), e, m[u]);
+                v[u] = ld4<0>(vp[u] + e);                          // the arenas are padded to whole rows
+            }
+        }
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, g[u]);
+    acc = block_sum<kSmallWaves>(acc);
+    if (threadIdx.x == 0u) shared = clip_of(n, k, acc);
+    __syncthreads();
+    const Clip cl = shared;
+    if (cl.skip) return;
+    const float neg_lr = xa.neg_lr_k[k];
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u) {
+        if (!m[u]) continue;
+        LASGD_FOR4(step_elem(comp(x[u], c), comp(v[u], c), cl.c * compv(g[u], c), wd[u], a.mu, neg_lr, a.nesterov);)
+        store_grad<false>(reinterpret_cast<char *>(vp[u]), e, m[u], v[u]);
+        store_grad<false>(reinterpret_cast<char *>(xm[u]), e, m[u], x[u]);
+        if constexpr (BF16) store_grad<true>(xu[u], e, m[u], x[u]);
+    }
+}
+
+// The same with the global update, of the replicas in the masks.
+template <bool BF16>
+__global__ __launch_bounds__(1024) void small_update_kernel(const ApplyArgs a, const ExtArgs xa, const NormArgs n)
 {
     const uint32_t lane = threadIdx.x & 63u, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t k = replica_at<true>(a, &xa, blockIdx.x);
@@ -329,15 +381,14 @@ __global__ __launch_bounds__(1024) void small_step_kernel(const ApplyArgs a, con
         const uint32_t tensor = (uint32_t)__popcll(__ballot(starts <= tile));
         const Record rec = load_record(a, k, tensor);
         const Tile t = locate(a, rec, tile, tensor, 256u);
-        float4 zt[1] = {make_float4(0.f, 0.f, 0.f, 0.f)};
-        if constexpr (OP == OP_STEP_MERGE) zt[0] = ld4<0>(a.z + t.aoff + lane * 4u);
+        const float4 zt[1] = {ld4<0>(a.z + t.aoff + lane * 4u)};
         char *xu = reinterpret_cast<char *>(rec.x) + t.toff * (BF16 ? 2u : 4u);
         const char *gu = reinterpret_cast<const char *>(rec.g) + t.toff * (BF16 ? 2u : 4u);
         const size_t ao = (size_t)k * a.npad + t.aoff;
         float *xm = BF16 ? a.x32 + ao : nullptr;
         const float nlr = xa.neg_lr_k[k];
 #define LASGD_SMALL(OPX) apply_tile<1, OPX, BF16, 0, false, true, false, false, true>(a, xu, gu, xm, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, nlr, xa.alpha, cl)
-        if (OP == OP_STEP || !in_merge) LASGD_SMALL(OP_STEP);
+        if (!in_merge) LASGD_SMALL(OP_STEP);
         else if (in_step) LASGD_SMALL(OP_STEP_MERGE);
         else LASGD_SMALL(OP_MERGE);
 #undef LASGD_SMALL

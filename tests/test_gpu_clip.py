@@ -114,6 +114,9 @@ LISTS = {
     "many": tuple(1 + (37 * i) % 300 for i in range(150)),              # several tensors in every block of tiles, more than sixteen in some
     "blocks": (64 * 256, 64 * 256 - 1, 64 * 256 + 1, 5, 3 * 64 * 256 + 77),
     "long": (1_300_001, 3, 70_000),
+    "48 tiles": (12_288,),
+    "48 of many": (3, 700, 256) + (1,) * 43,
+    "49 tiles": (12_289,),
     "64 tiles": (16_384,),
     "64 of one": (1,) * 64,
     "63 and 300": (1,) * 62 + (300,),
@@ -279,7 +282,7 @@ def test_what_is_not_finite(bad, place, storage):
                                            ("long", 2, dict(nontemporal=3)), ("odd", 64, {}), ("odd", 64, dict(nontemporal=3)),
                                            ("odd", 6, dict(vec=4, kper_step=2, waves_per_block=4, max_blocks=3)), ("odd", 6, dict(vec=2, waves_per_block=2)),
                                            ("long", 3, {}), ("64 tiles", 5, {}), ("64 tiles", 64, dict(vec=4)), ("64 of one", 3, {}),
-                                           ("63 and 300", 9, dict(nontemporal=3)), ("65 tiles", 4, dict(vec=2)), ("65 of one", 7, {}), ("65 of one", 64, dict(kper_step=5))])
+                                           ("63 and 300", 9, dict(nontemporal=3)), ("48 tiles", 6, dict(vec=4)), ("48 of many", 64, {}), ("49 tiles", 4, dict(vec=2)), ("65 tiles", 4, dict(vec=2)), ("65 of one", 7, {}), ("65 of one", 64, dict(kper_step=5))])
 def test_local_steps(name, K, tuning, storage):
     r = Rig(K, LISTS[name], storage)
     try:
@@ -311,7 +314,7 @@ def test_local_steps(name, K, tuning, storage):
 @pytest.mark.parametrize("K,numels,tuning,side", [(3, LISTS["odd"], {}, True), (5, LISTS["rows"], dict(nontemporal=3), True), (2, LISTS["long"], {}, True),
                                                   (4, LISTS["many"], {}, False), (4, (700_001, 3, 256), {}, True), (4, (700_001, 3, 256), dict(nontemporal=3), True),
                                                   (6, LISTS["odd"], dict(kper_merge=6, waves_per_block=2, vec=2), True), (5, LISTS["63 and 300"], {}, True),
-                                                  (7, LISTS["64 tiles"], dict(vec=4), True), (7, LISTS["65 of one"], dict(vec=4, kper_merge=3), True), (4, LISTS["65 tiles"], {}, False)])
+                                                  (7, LISTS["48 tiles"], dict(vec=4), True), (6, LISTS["48 of many"], {}, True), (7, LISTS["64 tiles"], dict(vec=4), True), (7, LISTS["65 of one"], dict(vec=4, kper_merge=3), True), (4, LISTS["65 tiles"], {}, False)])
 def test_global_updates(K, numels, tuning, side, storage):
     """Steps and updates in turn; masks of the step, of the update, and a replica that is not finite and takes the update all the same.
     The lists with 700,001 elements hold a bf16 model in one place after an update."""
