@@ -34,7 +34,8 @@
  *   on a global update that re-sends leaves the model in s alone until the next
  *   step, "kept once" below; once a call that reads or writes the models has been
  *   recorded into a graph, in both for good), and the lookup tables; from the first lasgd_sgd_ar_step on that takes two kernels, the mean
- *   gradient between them (one array of one replica's length).
+ *   gradient between them (one array of one replica's length), from the first lasgd_sgd_ar_step_clip on too; from the first call
+ *   that takes gradient norms on, but for clipped steps of short lists, 4 KiB a replica for them.
  *
  * Paper <-> calls.  Prologue (steps 1-5): lasgd_local_step(eta_0),
  *   lasgd_snapshot, lasgd_average.  Loop iteration without global update
@@ -91,7 +92,7 @@ typedef struct {
 /* Launch-shape knobs; results never depend on them.  Zero in any field keeps
  * the built-in default for that field. */
 typedef struct {
-    int32_t vec;           /* 128-bit vectors per lane per tile: 1, 2 or 4 (tile = 256*vec elements) */
+    int32_t vec;           /* 128-bit vectors per lane per tile: 1, 2 or 4 (tile = 256*vec elements; clipped calls: 1) */
     int32_t kper_step;     /* replicas one wave handles back to back in local_step (1..K)            */
     int32_t kper_merge;    /* same for merge / step_merge, and the step of an sgd_ar_step in two kernels;
                               K keeps each z tile in registers                                        */
@@ -315,9 +316,9 @@ lasgd_status lasgd_sgd_ar_step(lasgd_ctx *ctx, float lr);
  * c_k is 0 (and 0 times infinity NaN), after a NaN it is NaN.
  *
  * All of it runs on the main stream, also the norms; ordering against the stream the gradients were made on is the caller's,
- * as for every step.  The first of these calls asks for a little device memory that it needs between its kernels (8 KiB a replica),
- * lasgd_sgd_ar_step_clip also for the mean gradient's array; a call that finds none returns ALLOC and enqueues nothing.  The clipped updates
- * take tiles of 256 elements whatever lasgd_tuning.vec says.
+ * as for every step.  The first of these calls asks for a little device memory that it
+ * needs between its kernels (4 KiB a replica), lasgd_sgd_ar_step_clip also for the mean gradient's array if no lasgd_sgd_ar_step has; a call that finds none
+ * returns ALLOC and enqueues nothing.  The clipped calls take tiles of 256 elements whatever lasgd_tuning.vec says.
  */
 #define LASGD_CLIP_EPS 1e-6
 

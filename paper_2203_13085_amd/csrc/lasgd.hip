@@ -921,10 +921,14 @@ uint64_t grad_bytes(const lasgd_ctx *c, uint32_t replicas) { return replicas * c
 // K = 8 102 845, 204 773, 409 774, 818 770, ResNet-18 K = 8 187 388, 374 346.  (With each state on a stream of its own batches overlap with other states' and
 // the smallest are best; that is not how a context is used.)  A global update reads z once for all replicas of a tile, and in batches again: it takes all at once.
 //
-// The read for a norm goes without the streaming hint where a second read follows, us without / with: step ResNet-50 bf16 K = 8 673 / 693, ResNet-18 bf16 K = 16
-// 605 / 631, fp32 K = 8 346 / 345, MobileNetV2 K = 8 107 / 109, K = 4 72 / 73; step + update, with its mean, ResNet-50 K = 8 1189 / 1209, ResNet-18 K = 8 551 / 556,
-// MobileNetV2 K = 16 327 / 325, bf16 253 / 258.  The norms alone: ResNet-50 K = 8 141 / 125, MobileNetV2 bf16 K = 16 25.1 / 23.5.
-constexpr uint64_t kNormBytes = 400ull << 20;
+// The read for a norm goes without the streaming hint where enough of it is still there for the second one; us without / with, one state | three in turn.
+// fp32 updates take it from 256 MiB of gradients on: step, ResNet-50 K = 8 758 / 716 | 753 / 757, K = 4 376 / 363 | 376 / 368, ResNet-18 K = 8 341 / 331 | 344 / 334,
+// K = 6 (281 MB) 247 / 248 | 256 / 250, K = 4 167 / 169 | 170 / 170, MobileNetV2 K = 16 (224 MB) 200 / 201 | 208 / 203, K = 8 105 / 106 | 106 / 107; step + update,
+// with its mean, ResNet-50 K = 8 1190 / 1187 | 1174 / 1190, ResNet-18 K = 8 546 / 537 | 549 / 548, K = 6 400 / 405 | 416 / 412, K = 4 273 / 279 | 285 / 283, MobileNetV2
+// K = 16 312 / 322 | 326 / 323.  bf16, whose gradients are a ninth of what a step moves and not a fifth, never: ResNet-50 K = 16 1316 / 1383 | 1320 / 1380,
+// ResNet-18 K = 8 309 / 317 | 306 / 317, with its update 410 / 418 | 412 / 416.  Nor does clipping in place: ResNet-50 K = 8 414 / 449, ResNet-18 K = 8 180 / 192.
+// The norms alone always do: ResNet-50 K = 8 141 / 125, MobileNetV2 bf16 K = 16 25.1 / 23.5.
+constexpr uint64_t kNormBytes = 400ull << 20, kNormHintFrom = 256ull << 20;
 uint32_t norm_batch(const lasgd_ctx *c, uint32_t replicas, bool in_place)
 {
     if (!in_place && c->storage != LASGD_BF16) return replicas;
@@ -942,17 +946,19 @@ uint64_t take_replicas(uint64_t &left, uint32_t count)
     return taken;
 }
 
-// Norms of the replicas in `mask`, and (clips) what comes of them, on the main stream.
-lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, bool clips = true)
+// Norms of the replicas in `mask`, and what comes of them for what follows, on the main stream.
+enum Next { NEXT_NOTHING, NEXT_UPDATE, NEXT_SCALE };
+lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, Next next)
 {
     ApplyArgs a{};
     fill_common(c, a);
     fill_fine(c, a);
     NormArgs n = norm_args(c, mask, clip, a.ntiles);
-    if (!clips) n.clip = nullptr;
+    if (next == NEXT_NOTHING) n.clip = nullptr;
     hipError_t e = clear_arrived(c);
     if (e == hipSuccess) {
-        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 1) != 0 : !clips;
+        const bool streams = next == NEXT_NOTHING || (next == NEXT_UPDATE && c->storage != LASGD_BF16 && grad_bytes(c, n.count) >= kNormHintFrom);
+        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 1) != 0 : streams;
         const dim3 grid(n.parts, n.count), bs(kNormThreads);
         if (c->storage == LASGD_BF16) {
             if (hint) hipLaunchKernelGGL((grad_norm_kernel<true, 1>), grid, bs, 0, c->main, a, n);
@@ -1214,12 +1220,12 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
         const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking, false);
         const bool plain = uniform && mask == c->all && batch == taking;
         if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, true)) != LASGD_OK) return st;
-        if (batch == taking) return (st = enqueue_norms(c, mask, *clip)) != LASGD_OK ? st : launch_apply(c, p);
+        if (batch == taking) return (st = enqueue_norms(c, mask, *clip, NEXT_UPDATE)) != LASGD_OK ? st : launch_apply(c, p);
         while (mask) {
             x.step_mask = take_replicas(mask, batch);
             ApplyPlan q;               // of fewer replicas than p, which was not refused
             if ((st = plan_apply(c, q, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK) return st;
-            if ((st = enqueue_norms(c, x.step_mask, *clip)) != LASGD_OK) return st;
+            if ((st = enqueue_norms(c, x.step_mask, *clip, NEXT_UPDATE)) != LASGD_OK) return st;
             if ((st = launch_apply(c, q)) != LASGD_OK) return st;
         }
         return LASGD_OK;
@@ -1307,7 +1313,7 @@ static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, 
     else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, clip != nullptr);
     if (st != LASGD_OK) return st;
     // the norms need no z: they are taken while the mean may still be on its way
-    if (clip && !small && step_mask && (st = enqueue_norms(c, step_mask, *clip)) != LASGD_OK) return st;
+    if (clip && !small && step_mask && (st = enqueue_norms(c, step_mask, *clip, NEXT_UPDATE)) != LASGD_OK) return st;
     // nothing can be refused any more: now the main stream waits for z (unless z is made on this very stream)
     if (!c->z_on_main) LASGD_HIP(c, hipStreamWaitEvent(c->main, c->evZ, 0));
     st = small ? launch_small(c, p, *clip) : launch_apply(c, p);
@@ -1477,7 +1483,7 @@ lasgd_status lasgd_grad_norms(lasgd_ctx *c, uint64_t mask, float *norms)
     if ((st = check_mask(c, mask, false, "mask")) != LASGD_OK) return st;
     if (c->n_bound != c->K) return fail(c, LASGD_ERR_STATE, "%d of %d replicas are bound", c->n_bound, c->K);
     if ((st = reserve_norms(c)) != LASGD_OK) return st;
-    return enqueue_norms(c, mask, clip, false);
+    return enqueue_norms(c, mask, clip, NEXT_NOTHING);
 }
 
 lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *clip)
@@ -1500,9 +1506,9 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
     if ((st = reserve_norms(c)) != LASGD_OK) return st;
     for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask), true); mask;) {
         const uint64_t now = take_replicas(mask, batch);
-        if ((st = enqueue_norms(c, now, *clip)) != LASGD_OK) return st;
+        if ((st = enqueue_norms(c, now, *clip, NEXT_SCALE)) != LASGD_OK) return st;
         NormArgs n = norm_args(c, now, *clip, a.ntiles);
-        n.parts = norm_groups(true, a.ntiles, n.count);
+        n.parts = norm_groups(true, a.ntiles, n.count);          // reads and writes: us at 256 / 512 / 1024, bf16 ResNet-50 K = 32 884 / 788 / 867, fp32 K = 8 424 / 426 / 423
         const bool hint = (hint_of(c, USE_CYCLE) & 3) != 0;
         const dim3 grid(n.parts, n.count), bs(kNormThreads);
         if (c->storage == LASGD_BF16) {

@@ -9,6 +9,7 @@
 // Bound by HBM: 2 flop per 2 or 4 bytes; the vector units do 64-bit additions ten times as fast as the elements arrive.
 #pragma once
 #include "lasgd_kernels.hip.h"
+#include "../../include/lasgd.h"
 
 namespace lasgd {
 
@@ -56,7 +57,7 @@ __device__ __forceinline__ Clip clip_of(const NormArgs &n, uint32_t k, double su
 {
     const double norm = __builtin_sqrt(sum);
     if (n.norms) *as_global<float>(n.norms + k) = (float)norm;
-    const double c = (double)n.max_norm / (norm + 1e-6);
+    const double c = (double)n.max_norm / (norm + LASGD_CLIP_EPS);
     const bool finite = norm <= 1.7976931348623157e308;
     return Clip{c >= 1.0 ? 1.f : (float)c, n.skip_nonfinite && !finite ? 1u : 0u};          // a NaN stays one
 }

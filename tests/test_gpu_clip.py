@@ -395,8 +395,7 @@ def test_no_limit_is_the_unclipped_call_to_the_bit(K, numels, storage):
 
 @pytest.mark.parametrize("storage,K,n", [("f32", 9, 3_100_003), ("bf16", 20, 2_800_003)])
 def test_more_gradients_than_a_cache_holds(storage, K, n):
-    """From 104 MiB of gradients on a step, and clipping in place, take some replicas at a time: plain and masked, after updates that
-    leave a bf16 model in one place, and recorded."""
+    """Plain and masked steps, after updates that leave a bf16 model in one place, and recorded."""
     r = Rig(K, (n, 33, 256), storage, side_stream=False)
     full, part = (1 << K) - 1, ((1 << K) - 1) & 0xFFEB7
     try:
@@ -429,6 +428,68 @@ def test_more_gradients_than_a_cache_holds(storage, K, n):
             np.testing.assert_array_equal(r.device_grads(k), W.bf16_bits_to_f32(W.to_bf16_bits(want)) if r.bf16 else want)
     finally:
         r.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_batches(dtype):
+    """From 400 MiB of gradients on bf16 steps, and clipping in place, take some replicas at a time; another context takes them one by one,
+    in calls too small for that.  Recorded too, with the models in s alone before."""
+    bf16 = dtype == torch.bfloat16
+    K, n = (7, 36_000_003) if bf16 else (3, 50_000_003)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    st = torch.cuda.Stream()
+    x0 = torch.randn(n, generator=gen, device="cuda").to(dtype)
+    rows = (n + 255) // 256 * 256
+    g = torch.zeros(K, rows, device="cuda", dtype=dtype)
+    for k in range(K):
+        g[k, :n] = torch.randn(n, generator=gen, device="cuda") * (0.3 + 0.3 * k)
+    want = [float(torch.linalg.vector_norm(g[k, :n].double())) for k in range(K)]
+    most = float(np.float32(0.5 * (want[0] + want[-1])))
+    sides = []
+    for _ in range(2):
+        x = torch.zeros(K, rows, device="cuda", dtype=dtype)
+        x[:, :n] = x0
+        c = B.Context(K, [n], storage=B.BF16 if bf16 else B.F32, main_stream=st.cuda_stream, side_stream=st.cuda_stream, wd_scalar=1e-4)
+        for k in range(K):
+            c.bind(k, [x[k].data_ptr()], [g[k].data_ptr()])
+        torch.cuda.synchronize()
+        if bf16:
+            c.init_master()
+        c.snapshot()
+        c.average()
+        c.step_merge(0.1, True)                          # a bf16 model is in s alone now
+        sides.append((x, c))
+    (xa, a), (xb, b) = sides
+    norms = torch.zeros(K, device="cuda")
+    try:
+        graph = torch.cuda.CUDAGraph()
+        a.sync()
+        with torch.cuda.graph(graph, stream=st):
+            a.local_step_clip(0.1, most, norms=norms.data_ptr())
+        with torch.cuda.stream(st):
+            graph.replay()
+        a.local_step_clip(0.1, most, (1 << K) - 2)
+        a.local_step_clip(0.1, most)
+        for mask in ((1 << K) - 1, (1 << K) - 2, (1 << K) - 1):
+            for k in range(K):
+                if (mask >> k) & 1:
+                    b.local_step_clip(0.1, most, 1 << k)
+        a.sync()
+        assert torch.equal(xa, xb)
+        check_norms(norms.cpu().numpy().astype(np.float64), want)
+        before = g[:, :n].clone()
+        torch.cuda.synchronize()                         # the copy reads what the call is about to write, on another stream
+        a.clip_grads(most, (1 << K) - 2)
+        a.sync()
+        assert torch.equal(g[0, :n], before[0])
+        for k in range(1, K):
+            assert torch.equal(g[k, :n], (before[k].float() * float(coefficient(want[k], most))).to(dtype)), k
+    finally:
+        a.close()
+        b.close()
+        del xa, xb, g, sides
+        torch.cuda.empty_cache()
 
 
 def mean_gradient(g):
@@ -601,6 +662,40 @@ def test_tensors_on_16_bytes(dtype):
             assert bool(torch.isnan(g[k][~inside]).all())
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_tensor_beyond_four_gigabytes(dtype):
+    """2^31 - 2^21 elements, so that offsets pass 32 bits, with values at the beginning, around 2^31 bytes, 2^30 elements and at the odd end."""
+    n = (1 << 31) - (1 << 21) - 3 if dtype == torch.bfloat16 else (1 << 30) + 1027
+    x, g = torch.zeros(n, device="cuda", dtype=dtype), torch.zeros(n, device="cuda", dtype=dtype)
+    at = sorted({0, 1, (1 << 29) - 1, 1 << 29, (1 << 30) - 1, (1 << 30) + 5, n - 2, n - 1})
+    for i, j in enumerate(at):
+        g[j] = float(i + 1)
+    want = float(sum((i + 1) ** 2 for i in range(len(at)))) ** 0.5
+    norms = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    c = B.Context(1, [n], storage=B.BF16 if dtype == torch.bfloat16 else B.F32, momentum=0.0, nesterov=False, main_stream=st.cuda_stream, side_stream=st.cuda_stream)
+    try:
+        c.bind(0, [x.data_ptr()], [g.data_ptr()])
+        if dtype == torch.bfloat16:
+            c.init_master()
+        c.grad_norms(norms.data_ptr())
+        c.sync()
+        check_norms([float(norms)], [want])
+        c.local_step_clip(1.0, 1.0)
+        c.clip_grads(1.0)
+        c.sync()
+        cl = coefficient(want, 1.0)
+        for i, j in enumerate(at):
+            scaled = torch.tensor(float(cl * np.float32(i + 1)))
+            assert float(g[j]) == float(scaled.to(dtype)) and float(x[j]) == float((-scaled).to(dtype)), j
+        assert int(torch.count_nonzero(g)) == len(at) and int(torch.count_nonzero(x)) == len(at)
+    finally:
+        c.close()
+        del x, g
+        torch.cuda.empty_cache()
 
 
 def test_refusals():
