@@ -307,7 +307,7 @@ lasgd_status lasgd_sgd_ar_step(lasgd_ctx *ctx, float lr);
  * Every replica is a worker with gradients of its own, so each has a norm of its own over its whole parameter list,
  *     n_k = sqrt(sum over all tensors and elements of g[k]^2),
  * and clipping to max_norm scales its gradients by c_k = min(1, max_norm / (n_k + LASGD_CLIP_EPS)).  Norms are summed in
- * fp64 from the elements on, in a fixed order (the same gradients give the same bits), and rounded to fp32 once.  c_k is rounded to
+ * fp64 from the elements on, in an order that the call fixes (the same call on the same gradients gives the same bits), and rounded to fp32 once.  c_k is rounded to
  * fp32 once, and so is c_k g (in place: to the storage type).  c_k = 1 leaves every bit as it is.
  *
  * A norm is not finite exactly when one of the gradients is an infinity or a NaN.  With skip_nonfinite such a replica

@@ -895,6 +895,10 @@ hipError_t clear_arrived(lasgd_ctx *c)
     return e;
 }
 
+// us at 256 / 512 / 1024 / 1536, with the copy of new gradients in front, about half of the replicas scaled: ResNet-50 list K = 8 598 / 594 / 592 / 591, bf16
+// K = 32 1300 / 1277 / 1272 / 1276, ResNet-18 K = 8 271 / 270 / 266 / 266, MobileNetV2 bf16 K = 16 79.8 / 77.5 / 76.8 / 76.5.
+constexpr uint32_t kScaleParts = 1024;
+
 NormArgs norm_args(const lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, uint32_t ntiles)
 {
     NormArgs n{};
@@ -913,25 +917,25 @@ NormArgs norm_args(const lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, ui
 
 uint64_t grad_bytes(const lasgd_ctx *c, uint32_t replicas) { return replicas * c->packed * (c->storage == LASGD_BF16 ? 2u : 4u); }
 
-// Gradients are read for their norm and then again, and the 256 MB memory-side cache keeps part of them between.  bf16 steps, and clipping in
+// Gradients are read for their norm and then again, and the 256 MB memory-side cache keeps part of them between.  bf16 steps, and clipping bf16 gradients in
 // place, take so many replicas at a time that it keeps more of them than the further launches cost: batches of one length, up to 400 MiB of gradients each.  us at so
 // many MB of gradients a batch, all at once last (three states in turn on one stream): bf16 step ResNet-50 list K = 32 204 2749, 307 2650, 409 2641, 613 2659, 818
-// 2678, 1636 2724, K = 8 204 686, 409 673, ResNet-18 K = 16 187 609, 374 605; in place, everything scaled, ResNet-50 K = 8 204 516, 409 414, 818 418, bf16
-// K = 32 409 805, 818 844, 1636 870, ResNet-18 K = 16 187 191, 374 180.  fp32 steps, which write more than they read of gradients, gain nothing: ResNet-50
-// K = 8 102 845, 204 773, 409 774, 818 770, ResNet-18 K = 8 187 388, 374 346.  (With each state on a stream of its own batches overlap with other states' and
-// the smallest are best; that is not how a context is used.)  A global update reads z once for all replicas of a tile, and in batches again: it takes all at once.
+// 2678, 1636 2724, K = 8 204 686, 409 673, ResNet-18 K = 16 187 609, 374 605; in place, with a copy in front, ResNet-50 K = 32 409 1277, 818 1293, 1636 1314.  fp32
+// gains nothing: step ResNet-50 K = 8 102 845, 204 773, 409 774, 818 770, ResNet-18 K = 8 187 388, 374 346; in place ResNet-50 K = 8 409 594, 818 595, ResNet-18
+// 187 281, 374 268.  (With each state on a stream of its own batches overlap with other states' and the smallest are best; that is not how a context is
+// used.)  A global update reads z once for all replicas of a tile, and in batches again: it takes all at once.
 //
 // The read for a norm goes without the streaming hint where enough of it is still there for the second one; us without / with, one state | three in turn.
 // fp32 updates take it from 256 MiB of gradients on: step, ResNet-50 K = 8 758 / 716 | 753 / 757, K = 4 376 / 363 | 376 / 368, ResNet-18 K = 8 341 / 331 | 344 / 334,
 // K = 6 (281 MB) 247 / 248 | 256 / 250, K = 4 167 / 169 | 170 / 170, MobileNetV2 K = 16 (224 MB) 200 / 201 | 208 / 203, K = 8 105 / 106 | 106 / 107; step + update,
 // with its mean, ResNet-50 K = 8 1190 / 1187 | 1174 / 1190, ResNet-18 K = 8 546 / 537 | 549 / 548, K = 6 400 / 405 | 416 / 412, K = 4 273 / 279 | 285 / 283, MobileNetV2
 // K = 16 312 / 322 | 326 / 323.  bf16, whose gradients are a ninth of what a step moves and not a fifth, never: ResNet-50 K = 16 1316 / 1383 | 1320 / 1380,
-// ResNet-18 K = 8 309 / 317 | 306 / 317, with its update 410 / 418 | 412 / 416.  Nor does clipping in place: ResNet-50 K = 8 414 / 449, ResNet-18 K = 8 180 / 192.
+// ResNet-18 K = 8 309 / 317 | 306 / 317, with its update 410 / 418 | 412 / 416.  Nor does clipping in place: with the copy in front ResNet-50 K = 8 595 / 589, K = 32 bf16 1277 / 1329, ResNet-18 K = 8 268 / 268, MobileNetV2 bf16 K = 16 77.5 / 85.6.
 // The norms alone always do: ResNet-50 K = 8 141 / 125, MobileNetV2 bf16 K = 16 25.1 / 23.5.
 constexpr uint64_t kNormBytes = 400ull << 20, kNormHintFrom = 256ull << 20;
-uint32_t norm_batch(const lasgd_ctx *c, uint32_t replicas, bool in_place)
+uint32_t norm_batch(const lasgd_ctx *c, uint32_t replicas)
 {
-    if (!in_place && c->storage != LASGD_BF16) return replicas;
+    if (c->storage != LASGD_BF16) return replicas;
     const uint64_t batches = (grad_bytes(c, replicas) + kNormBytes - 1) / kNormBytes;
     return batches >= replicas ? 1u : (uint32_t)((replicas + batches - 1) / batches);
 }
@@ -1217,7 +1221,7 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
         ApplyPlan p;
         if (one_launch(c, false)) return (st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK ? st : launch_small(c, p, *clip);
         if ((st = reserve_norms(c)) != LASGD_OK) return st;
-        const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking, false);
+        const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking);
         const bool plain = uniform && mask == c->all && batch == taking;
         if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, true)) != LASGD_OK) return st;
         if (batch == taking) return (st = enqueue_norms(c, mask, *clip, NEXT_UPDATE)) != LASGD_OK ? st : launch_apply(c, p);
@@ -1504,13 +1508,15 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
         return e == hipSuccess ? LASGD_OK : fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
     }
     if ((st = reserve_norms(c)) != LASGD_OK) return st;
-    for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask), true); mask;) {
+    for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask)); mask;) {
         const uint64_t now = take_replicas(mask, batch);
         if ((st = enqueue_norms(c, now, *clip, NEXT_SCALE)) != LASGD_OK) return st;
         NormArgs n = norm_args(c, now, *clip, a.ntiles);
-        n.parts = norm_groups(true, a.ntiles, n.count);          // reads and writes: us at 256 / 512 / 1024, bf16 ResNet-50 K = 32 884 / 788 / 867, fp32 K = 8 424 / 426 / 423
+        const uint32_t runs = (a.ntiles + kNormRun - 1u) / kNormRun;
+        n.by_runs = make_div(runs);
+        n.parts = n.count * runs < kScaleParts ? n.count * runs : kScaleParts;
         const bool hint = (hint_of(c, USE_CYCLE) & 3) != 0;
-        const dim3 grid(n.parts, n.count), bs(kNormThreads);
+        const dim3 grid(n.parts), bs(kNormThreads);
         if (c->storage == LASGD_BF16) {
             if (hint) hipLaunchKernelGGL((scale_grads_kernel<true, 3>), grid, bs, 0, c->main, a, n);
             else hipLaunchKernelGGL((scale_grads_kernel<true, 0>), grid, bs, 0, c->main, a, n);

@@ -432,7 +432,7 @@ def test_more_gradients_than_a_cache_holds(storage, K, n):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_batches(dtype):
-    """From 400 MiB of gradients on bf16 steps, and clipping in place, take some replicas at a time; another context takes them one by one,
+    """From 400 MiB of bf16 gradients on steps, and clipping in place, take some replicas at a time; another context takes them one by one,
     in calls too small for that.  Recorded too, with the models in s alone before."""
     bf16 = dtype == torch.bfloat16
     K, n = (7, 36_000_003) if bf16 else (3, 50_000_003)
