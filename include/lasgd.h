@@ -34,8 +34,7 @@
  *   on a global update that re-sends leaves the model in s alone until the next
  *   step, "kept once" below; once a call that reads or writes the models has been
  *   recorded into a graph, in both for good), and the lookup tables; from the first lasgd_sgd_ar_step on that takes two kernels, the mean
- *   gradient between them (one array of one replica's length), from the first lasgd_sgd_ar_step_clip on too; from the first call
- *   that takes gradient norms on, but for clipped steps of short lists, 4 KiB a replica for them.
+ *   gradient between them (one array of one replica's length), from the first lasgd_sgd_ar_step_clip on too.
  *
  * Paper <-> calls.  Prologue (steps 1-5): lasgd_local_step(eta_0),
  *   lasgd_snapshot, lasgd_average.  Loop iteration without global update
@@ -316,9 +315,7 @@ lasgd_status lasgd_sgd_ar_step(lasgd_ctx *ctx, float lr);
  * c_k is 0 (and 0 times infinity NaN), after a NaN it is NaN.
  *
  * All of it runs on the main stream, also the norms; ordering against the stream the gradients were made on is the caller's,
- * as for every step.  The first of these calls asks for a little device memory that it
- * needs between its kernels (4 KiB a replica), lasgd_sgd_ar_step_clip also for the mean gradient's array if no lasgd_sgd_ar_step has; a call that finds none
- * returns ALLOC and enqueues nothing.  The clipped calls take tiles of 256 elements whatever lasgd_tuning.vec says.
+ * as for every step.  The clipped calls take tiles of 256 elements whatever lasgd_tuning.vec says.
  */
 #define LASGD_CLIP_EPS 1e-6
 
@@ -330,7 +327,7 @@ typedef struct {
 } lasgd_clip;
 
 /* norms[k] <- n_k for the replicas in `mask` (non-empty); norms: device [K].  The parameters and the state are not touched.
- * Errors: INVALID (NULL, misaligned, bad mask), STATE (a replica is unbound), ALLOC, HIP. */
+ * Errors: INVALID (NULL, misaligned, bad mask), STATE (a replica is unbound), HIP. */
 lasgd_status lasgd_grad_norms(lasgd_ctx *ctx, uint64_t mask, float *norms);
 
 /* g[k] <- c_k g[k], in place, for the replicas in `mask` (non-empty), for callers whose update is not one of this library's or who want to
@@ -340,17 +337,17 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *ctx, uint64_t mask, const lasgd_clip *c
 
 /* lasgd_local_step_ex with c_k g[k] in the place of g[k]; the gradients are only read.  fp32 storage: exactly lasgd_clip_grads and
  * lasgd_local_step_ex, same roundings; bf16 storage: c_k g[k] stays in fp32.
- * Errors: as lasgd_local_step_ex, plus INVALID as lasgd_clip_grads, and ALLOC. */
+ * Errors: as lasgd_local_step_ex, plus INVALID as lasgd_clip_grads. */
 lasgd_status lasgd_local_step_clip(lasgd_ctx *ctx, const float *lr, uint64_t mask, const lasgd_clip *clip);
 
 /* lasgd_step_merge_ex with clipped gradients in the local update of the replicas in step_mask.
- * Errors: as lasgd_step_merge_ex, plus INVALID as lasgd_clip_grads, and ALLOC. */
+ * Errors: as lasgd_step_merge_ex, plus INVALID as lasgd_clip_grads. */
 lasgd_status lasgd_step_merge_clip(lasgd_ctx *ctx, const float *lr, uint64_t step_mask, uint64_t merge_mask,
                                    int32_t resnapshot, const lasgd_clip *clip);
 
 /* lasgd_sgd_ar_step with the mean gradient clipped: one norm, that of the mean gradient, one c, and (skip_nonfinite) all replicas
- * sit out together.  norms: device [1].
- * Errors: as lasgd_sgd_ar_step, plus INVALID as lasgd_clip_grads, and ALLOC. */
+ * sit out together.  norms: device [1].  Always two kernels; the first call asks for the mean gradient's array if no lasgd_sgd_ar_step has.
+ * Errors: as lasgd_sgd_ar_step, plus INVALID as lasgd_clip_grads, and ALLOC where there is no memory for the array. */
 lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *ctx, float lr, const lasgd_clip *clip);
 
 /*

@@ -53,16 +53,14 @@ struct lasgd_ctx {
     bool clear_in_graph = false;     // one was recorded: from then on a replay of it may be queued at any time
     int device = 0;
 
-    // device memory: v, s, z and x32 are one allocation, carved up
+    // device memory: v, s, z, x32 and what the gradient norms keep between kernels are one allocation, carved up
     char *arena = nullptr;
     float *v = nullptr, *s = nullptr, *z = nullptr, *x32 = nullptr;
     float *gbar = nullptr;           // mean gradient [npad] of an SGD All-Reduce step in two kernels, see reserve_mean_grad
     bool gbar_tried = false;         // asked for; without it the step always takes one kernel
-    char *norm_mem = nullptr;        // what the clipped calls keep between their kernels, see reserve_norms
     double *norm_part = nullptr;     // [K][kNormParts]
     Clip *clip = nullptr;            // [K]
     uint32_t *arrived = nullptr;     // [K][kArriveStride], zero between calls
-    bool arrived_clear = false;      // it has been cleared, on the main stream and not in a recording
     // one set of lookup tables per tile size ever used (vec = 1, 2, 4), kept until destroy: a graph captured
     // under one tile size still points at its tables after the tile size has been changed
     struct Tables {
@@ -835,8 +833,6 @@ lasgd_status check_ready_to_step(lasgd_ctx *c, float lr)
 
 // ---- gradient norms and clipping -------------------------------------------
 
-// What the kernels of a call hand on: the parts of each sum, and what comes of each norm.  For those alone that make the calls it is for; the
-// first of them asks, before it enqueues anything, also while it is being recorded.
 // Workgroups of sixteen waves, for all replicas of a call together: as many as have 64 KiB of loads in flight a CU.  us at 128 / 192 / 256 / 384 /
 // 512, three states in turn on one stream: ResNet-50 list K = 8 168 / 127 / 125 / 139 / 130 (6.5 TB/s), ResNet-18 K = 8 78 / 63 / 61 / 66 / 63, MobileNetV2 K = 16
 // 53 / 41 / 38.5 / 41 / 39, one vector of 30,000,001 26.3 / 21.4 / 21.7 / 23.4 / 24.8; bf16 ResNet-50 K = 32 388 / 284 / 247 / 255 / 242 (6.8 TB/s), MobileNetV2 K = 16
@@ -857,23 +853,14 @@ uint32_t mean_norm_groups(uint32_t ntiles)                    // whole rows of X
     const uint32_t all = ((ntiles + kNormWaves - 1u) / kNormWaves + 7u) & ~7u;
     return all < kMeanParts ? all : kMeanParts;
 }
-lasgd_status reserve_norms(lasgd_ctx *c)
+// What the kernels of a call hand on, behind the arrays: the shares of each sum (kMeanParts of them at most in all, or kNormParts a replica), counters, which the
+// kernels leave at zero, and what comes of each norm.
+size_t norm_bytes(int32_t K) { return (size_t)K * (kNormParts * sizeof(double) + kArriveStride * sizeof(uint32_t) + sizeof(Clip)); }
+void place_norms(lasgd_ctx *c, char *at)
 {
-    if (c->norm_mem) return LASGD_OK;
-    const size_t parts = (size_t)c->K * kNormParts * sizeof(double);      // more than kMeanParts
-    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;        // allowed while a stream of this thread is being recorded, and not recorded
-    (void)hipThreadExchangeStreamCaptureMode(&mode);
-    const hipError_t e = hipMalloc((void **)&c->norm_mem, parts + (size_t)c->K * (sizeof(Clip) + kArriveStride * sizeof(uint32_t)));
-    (void)hipThreadExchangeStreamCaptureMode(&mode);
-    if (e != hipSuccess) {
-        (void)hipGetLastError();
-        c->norm_mem = nullptr;
-        return fail(c, LASGD_ERR_ALLOC, "no memory for the gradient norms: %s", hipGetErrorString(e));
-    }
-    c->norm_part = (double *)c->norm_mem;
-    c->arrived = (uint32_t *)(c->norm_mem + parts);
+    c->norm_part = (double *)at;
+    c->arrived = (uint32_t *)(c->norm_part + (size_t)c->K * kNormParts);
     c->clip = (Clip *)(c->arrived + (size_t)c->K * kArriveStride);
-    return LASGD_OK;
 }
 
 lasgd_status check_clip(lasgd_ctx *c, const lasgd_clip *clip)
@@ -882,17 +869,6 @@ lasgd_status check_clip(lasgd_ctx *c, const lasgd_clip *clip)
     if (!(clip->max_norm >= 0.f)) return fail(c, LASGD_ERR_INVALID, "max_norm must be >= 0 (infinity: no limit)");
     if ((uintptr_t)clip->norms & 3u) return fail(c, LASGD_ERR_INVALID, "norms is not 4-byte aligned");
     return LASGD_OK;
-}
-
-// Before the first kernel that counts.  A recorded clear runs whenever its graph does, so until one has run by itself every
-// call brings its own.
-hipError_t clear_arrived(lasgd_ctx *c)
-{
-    if (c->arrived_clear) return hipSuccess;
-    hipLaunchKernelGGL(clear_kernel, dim3(1), dim3(64), 0, c->main, c->arrived, (uint32_t)c->K * kArriveStride);
-    const hipError_t e = hipGetLastError();
-    if (e == hipSuccess && !is_capturing(c->main)) c->arrived_clear = true;
-    return e;
 }
 
 // us at 256 / 512 / 1024 / 1536, with the copy of new gradients in front, about half of the replicas scaled: ResNet-50 list K = 8 598 / 594 / 592 / 591, bf16
@@ -959,20 +935,17 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
     fill_fine(c, a);
     NormArgs n = norm_args(c, mask, clip, a.ntiles);
     if (next == NEXT_NOTHING) n.clip = nullptr;
-    hipError_t e = clear_arrived(c);
-    if (e == hipSuccess) {
-        const bool streams = next == NEXT_NOTHING || (next == NEXT_UPDATE && c->storage != LASGD_BF16 && grad_bytes(c, n.count) >= kNormHintFrom);
-        const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 1) != 0 : streams;
-        const dim3 grid(n.parts, n.count), bs(kNormThreads);
-        if (c->storage == LASGD_BF16) {
-            if (hint) hipLaunchKernelGGL((grad_norm_kernel<true, 1>), grid, bs, 0, c->main, a, n);
-            else hipLaunchKernelGGL((grad_norm_kernel<true, 0>), grid, bs, 0, c->main, a, n);
-        } else {
-            if (hint) hipLaunchKernelGGL((grad_norm_kernel<false, 1>), grid, bs, 0, c->main, a, n);
-            else hipLaunchKernelGGL((grad_norm_kernel<false, 0>), grid, bs, 0, c->main, a, n);
-        }
-        e = hipGetLastError();
+    const bool streams = next == NEXT_NOTHING || (next == NEXT_UPDATE && c->storage != LASGD_BF16 && grad_bytes(c, n.count) >= kNormHintFrom);
+    const bool hint = c->tune.nontemporal >= 0 ? (c->tune.nontemporal & 1) != 0 : streams;
+    const dim3 grid(n.parts, n.count), bs(kNormThreads);
+    if (c->storage == LASGD_BF16) {
+        if (hint) hipLaunchKernelGGL((grad_norm_kernel<true, 1>), grid, bs, 0, c->main, a, n);
+        else hipLaunchKernelGGL((grad_norm_kernel<true, 0>), grid, bs, 0, c->main, a, n);
+    } else {
+        if (hint) hipLaunchKernelGGL((grad_norm_kernel<false, 1>), grid, bs, 0, c->main, a, n);
+        else hipLaunchKernelGGL((grad_norm_kernel<false, 0>), grid, bs, 0, c->main, a, n);
     }
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
     return LASGD_OK;
 }
@@ -1020,7 +993,6 @@ void release(lasgd_ctx *c)
         if (t.mem) (void)hipFree(t.mem);
     if (c->records) (void)hipFree(c->records);
     if (c->gbar) (void)hipFree(c->gbar);
-    if (c->norm_mem) (void)hipFree(c->norm_mem);
     if (c->evA) (void)hipEventDestroy(c->evA);
     if (c->evZ) (void)hipEventDestroy(c->evZ);
     delete c;
@@ -1084,7 +1056,8 @@ static lasgd_status create_impl(const lasgd_config *cfg, lasgd_ctx **out)
     const uint64_t per = c->npad * sizeof(float);
     c->both_places = !bf16 || c->K * per < kOneCopyFrom;
     const uint64_t n_arrays = (uint64_t)c->K * (bf16 ? 3 : 2) + 1;       // v, s (, x32), z
-    const uint64_t bytes = n_arrays * per + (bf16 ? kSettleWords * sizeof(uint32_t) : 0u);
+    const uint64_t norms_at = round_up(n_arrays * per + (bf16 ? kSettleWords * sizeof(uint32_t) : 0u), 256);
+    const uint64_t bytes = norms_at + norm_bytes(c->K);
     CREATE_HIP(hipMalloc((void **)&c->arena, bytes));
     CREATE_HIP(hipMemsetAsync(c->arena, 0, bytes, c->main));
     c->v = (float *)c->arena;
@@ -1092,6 +1065,7 @@ static lasgd_status create_impl(const lasgd_config *cfg, lasgd_ctx **out)
     c->z = c->s + (uint64_t)c->K * c->npad;
     c->x32 = bf16 ? c->z + c->npad : nullptr;
     c->settle = bf16 ? (uint32_t *)(c->x32 + (uint64_t)c->K * c->npad) : nullptr;
+    place_norms(c, c->arena + norms_at);
     const size_t tab = (size_t)c->K * c->n_tensors * sizeof(Record);
     CREATE_HIP(hipMalloc((void **)&c->records, tab));
     CREATE_HIP(hipMemset(c->records, 0, tab));
@@ -1220,7 +1194,6 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
     if (clip) {
         ApplyPlan p;
         if (one_launch(c, false)) return (st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK ? st : launch_small(c, p, *clip);
-        if ((st = reserve_norms(c)) != LASGD_OK) return st;
         const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking);
         const bool plain = uniform && mask == c->all && batch == taking;
         if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, true)) != LASGD_OK) return st;
@@ -1312,7 +1285,6 @@ static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, 
                        (op == OP_MERGE || (step_mask == c->all && uniform));
     ApplyPlan p;
     const bool small = clip && one_launch(c, false);
-    if (clip && !small && (st = reserve_norms(c)) != LASGD_OK) return st;
     if (plain && !small) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0, nullptr, clip != nullptr);
     else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, clip != nullptr);
     if (st != LASGD_OK) return st;
@@ -1486,7 +1458,6 @@ lasgd_status lasgd_grad_norms(lasgd_ctx *c, uint64_t mask, float *norms)
     if (st != LASGD_OK) return st;
     if ((st = check_mask(c, mask, false, "mask")) != LASGD_OK) return st;
     if (c->n_bound != c->K) return fail(c, LASGD_ERR_STATE, "%d of %d replicas are bound", c->n_bound, c->K);
-    if ((st = reserve_norms(c)) != LASGD_OK) return st;
     return enqueue_norms(c, mask, clip, NEXT_NOTHING);
 }
 
@@ -1507,7 +1478,6 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
         const hipError_t e = hipGetLastError();
         return e == hipSuccess ? LASGD_OK : fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
     }
-    if ((st = reserve_norms(c)) != LASGD_OK) return st;
     for (const uint32_t batch = norm_batch(c, (uint32_t)__builtin_popcountll(mask)); mask;) {
         const uint64_t now = take_replicas(mask, batch);
         if ((st = enqueue_norms(c, now, *clip, NEXT_SCALE)) != LASGD_OK) return st;
@@ -1557,25 +1527,21 @@ lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *c, float lr, const lasgd_clip *cl
     if ((st = check_ready_to_step(c, lr)) != LASGD_OK) return st;
     if (!c->gbar) reserve_mean_grad(c);
     if (!c->gbar) return fail(c, LASGD_ERR_ALLOC, "no memory for the mean gradient");
-    if ((st = reserve_norms(c)) != LASGD_OK) return st;
     ApplyPlan p;
     if ((st = plan_apply(c, p, OP_STEP_MEAN, lr, 0, nullptr, true)) != LASGD_OK) return st;
     p.a.z = c->gbar;
     NormArgs n = norm_args(c, 1u, *clip, p.a.ntiles);
     n.parts = mean_norm_groups(p.a.ntiles);
     const bool nt = (hint_of(c, USE_SGD_AR) & 1) != 0;
-    hipError_t e = clear_arrived(c);
-    if (e == hipSuccess) {
-        const dim3 grid(n.parts), bs(kNormThreads);
-        if (c->storage == LASGD_BF16) {
-            if (nt) hipLaunchKernelGGL((mean_grad_norm_kernel<true, 3>), grid, bs, 0, c->main, p.a, n);
-            else hipLaunchKernelGGL((mean_grad_norm_kernel<true, 0>), grid, bs, 0, c->main, p.a, n);
-        } else {
-            if (nt) hipLaunchKernelGGL((mean_grad_norm_kernel<false, 3>), grid, bs, 0, c->main, p.a, n);
-            else hipLaunchKernelGGL((mean_grad_norm_kernel<false, 0>), grid, bs, 0, c->main, p.a, n);
-        }
-        e = hipGetLastError();
+    const dim3 grid(n.parts), bs(kNormThreads);
+    if (c->storage == LASGD_BF16) {
+        if (nt) hipLaunchKernelGGL((mean_grad_norm_kernel<true, 3>), grid, bs, 0, c->main, p.a, n);
+        else hipLaunchKernelGGL((mean_grad_norm_kernel<true, 0>), grid, bs, 0, c->main, p.a, n);
+    } else {
+        if (nt) hipLaunchKernelGGL((mean_grad_norm_kernel<false, 3>), grid, bs, 0, c->main, p.a, n);
+        else hipLaunchKernelGGL((mean_grad_norm_kernel<false, 0>), grid, bs, 0, c->main, p.a, n);
     }
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
     return launch_apply(c, p);
 }

@@ -38,12 +38,19 @@ __device__ __forceinline__ void add_squares(double &acc, float4 g)
     acc = __builtin_fma((double)g.w, (double)g.w, acc);
 }
 
+// The sum over a wave, in its first lane.
+__device__ __forceinline__ double wave_sum(double acc)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) acc += __shfl_down(acc, d, 64);
+    return acc;
+}
+
 // The sum over a workgroup of W waves, in thread 0.
 template <uint32_t W> __device__ __forceinline__ double block_sum(double acc)
 {
     __shared__ double wave[W];
-#pragma unroll
-    for (int d = 32; d; d >>= 1) acc += __shfl_down(acc, d, 64);
+    acc = wave_sum(acc);
     if ((threadIdx.x & 63u) == 0u) wave[threadIdx.x >> 6] = acc;
     __syncthreads();
     if (threadIdx.x == 0u) {
@@ -87,31 +94,32 @@ __device__ __forceinline__ float4 grad_at(const char *g, uint32_t e, uint32_t n)
 // 1863 us in place of 280.)  Counters of different replicas lie on lines of their own, kArriveStride apart.
 __device__ __forceinline__ void join_norm(const NormArgs &n, uint32_t k, uint32_t group, uint32_t groups, double acc)
 {
-    __shared__ uint32_t last;
     double *part = n.part + (size_t)k * n.stride;
     acc = block_sum<kNormWaves>(acc);
-    if (groups == 1u) {
-        if (threadIdx.x == 0u) finish_norm(n, k, acc);
-        return;
+    if (threadIdx.x >= 64u) return;               // the first wave does the rest
+    if (groups > 1u) {
+        uint32_t before = 0;
+        if (threadIdx.x == 0u) {
+            __hip_atomic_store(part + group, acc, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            before = __hip_atomic_fetch_add(n.arrived + k * kArriveStride, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        if (__builtin_amdgcn_readfirstlane(before) + 1u != groups) return;
+        acc = 0.0;
+        for (uint32_t i = threadIdx.x; i < groups; i += 256u) {
+            double share[4];                      // asked for together
+#pragma unroll
+            for (uint32_t u = 0; u < 4u; ++u) {
+                const uint32_t j = i + u * 64u;
+                share[u] = __hip_atomic_load(part + (j < groups ? j : i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 4u; ++u) acc += i + u * 64u < groups ? share[u] : 0.0;
+        }
+        acc = wave_sum(acc);
+        if (threadIdx.x == 0u) __hip_atomic_store(n.arrived + k * kArriveStride, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (threadIdx.x == 0u) {
-        __hip_atomic_store(part + group, acc, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        last = __hip_atomic_fetch_add(n.arrived + k * kArriveStride, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == groups;
-    }
-    __syncthreads();
-    if (!last) return;
-    acc = 0.0;
-    for (uint32_t i = threadIdx.x; i < groups; i += kNormThreads) acc += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    acc = block_sum<kNormWaves>(acc);
-    if (threadIdx.x != 0u) return;
-    __hip_atomic_store(n.arrived + k * kArriveStride, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    finish_norm(n, k, acc);
-}
-
-__global__ void clear_kernel(uint32_t *p, uint32_t n)
-{
-    for (uint32_t i = threadIdx.x; i < n; i += 64u) p[i] = 0u;
+    if (threadIdx.x == 0u) finish_norm(n, k, acc);
 }
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
