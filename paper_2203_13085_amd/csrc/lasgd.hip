@@ -950,11 +950,17 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
     return LASGD_OK;
 }
 
-// Lists this short take one launch for the norm and what follows (small_step_kernel): two of them are bound by the host, one of long lists by its one
-// workgroup a replica.  us, two launches / one, three states in turn on one stream: step, 300 elements K = 3 to 64 5.9-6.0 / 3.3-3.4, 4000 5.9-6.1 / 3.7-4.1,
-// 9000 5.9-9.0 / 4.5-5.7, 12288 K = 3 7.9 / 5.5, K = 64 8.2 / 6.5, bf16 6.6-8.3 / 6.0-7.0, 16384 K = 3 5.9 / 5.8, bf16 5.8 / 6.6; step + update, with its mean, 300 K = 3
-// 10.7 / 9.2, 9000 15 / 12.6, 12288 K = 16 14.6 / 13.7, K = 64 16.5 / 16.6, 16384 13.7 / 14.8; in place 16384 K = 3 5.9 / 3.3, K = 64 7.8 / 4.3.
-bool one_launch(const lasgd_ctx *c, bool in_place) { return c->tables_by_vec[0].ntiles <= (in_place ? 4u : 3u) * kSmallWaves; }
+// Lists this short take one launch for the norm and what follows (small_step_kernel): two of them are bound by the host, one by its workgroups, each of
+// which reads all gradients of its replica (in place, where that cannot be, a workgroup has a replica to itself).  us, two launches / one, three states in turn
+// on one stream, hosts of unlike speed: step, 300 elements K = 64 8.1 / 4.4, 9000 K = 3 to 64 5.8-9.1 / 4.5-5.6, 16384 K = 16 5.8 / 4.9, K = 64 10.2 / 7.0, 32768 K = 3
+// 7.6 / 6.3, K = 64 13.7 / 12.9, 49152 K = 16 9.5 / 8.7, K = 64 16.3 / 21.6; step + update, with its mean, 300 K = 3 10.7 / 9.3, 9000 14.3-16.2 / 11.2-13.7, 16384 K = 3
+// 14.0 / 11.4, K = 64 16.5 / 15.4, 24576 K = 3 11.8 / 12.1, K = 16 13.1 / 12.6, 32768 K = 16 13.9 / 14.6; in place 16384 K = 3 5.9 / 3.3, K = 64 7.8 / 4.3.
+bool one_launch(const lasgd_ctx *c, Next next, int op = OP_STEP)
+{
+    const uint32_t most = next == NEXT_UPDATE && op == OP_STEP ? 128u : 4u * kSmallWaves;
+    // bf16 models of this size may be in s alone (place_models), where these kernels do not look
+    return c->tables_by_vec[0].ntiles <= most && (c->storage != LASGD_BF16 || array_bytes(c) < kOneCopyFrom);
+}
 
 lasgd_status launch_small(lasgd_ctx *c, ApplyPlan &p, const lasgd_clip &clip)
 {
@@ -962,7 +968,7 @@ lasgd_status launch_small(lasgd_ctx *c, ApplyPlan &p, const lasgd_clip &clip)
     const lasgd_status st = place_models(c, &p.a, taking);
     if (st != LASGD_OK) return st;
     const NormArgs n = norm_args(c, taking, clip, p.a.ntiles);
-    const dim3 grid(n.count), bs(64u * kSmallWaves);
+    const dim3 grid(n.count, (p.a.ntiles + kSmallWaves - 1u) / kSmallWaves), bs(64u * kSmallWaves);
     if (p.op == OP_STEP) {
         if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_step_kernel<true>), grid, bs, 0, c->main, p.a, p.ext, n);
         else hipLaunchKernelGGL((small_step_kernel<false>), grid, bs, 0, c->main, p.a, p.ext, n);
@@ -1193,7 +1199,7 @@ static lasgd_status do_local_step(lasgd_ctx *c, const float *lr_k, float lr, uin
     const bool uniform = fill_ext(c, x, lr_k, mask, 0);
     if (clip) {
         ApplyPlan p;
-        if (one_launch(c, false)) return (st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK ? st : launch_small(c, p, *clip);
+        if (one_launch(c, NEXT_UPDATE)) return (st = plan_apply(c, p, OP_STEP, 0.f, 0, &x, true)) != LASGD_OK ? st : launch_small(c, p, *clip);
         const uint32_t taking = (uint32_t)__builtin_popcountll(mask), batch = norm_batch(c, taking);
         const bool plain = uniform && mask == c->all && batch == taking;
         if ((st = plan_apply(c, p, OP_STEP, plain ? lr_k[0] : 0.f, 0, plain ? nullptr : &x, true)) != LASGD_OK) return st;
@@ -1284,7 +1290,7 @@ static lasgd_status do_merge(lasgd_ctx *c, int op, const float *lr_k, float lr, 
     const bool plain = merge_mask == c->all && c->alpha == 1.f &&
                        (op == OP_MERGE || (step_mask == c->all && uniform));
     ApplyPlan p;
-    const bool small = clip && one_launch(c, false);
+    const bool small = clip && one_launch(c, NEXT_UPDATE, op);
     if (plain && !small) st = plan_apply(c, p, op, lr_k ? lr_k[0] : lr, resnapshot ? 1 : 0, nullptr, clip != nullptr);
     else st = plan_apply(c, p, op, 0.f, resnapshot ? 1 : 0, &x, clip != nullptr);
     if (st != LASGD_OK) return st;
@@ -1471,7 +1477,7 @@ lasgd_status lasgd_clip_grads(lasgd_ctx *c, uint64_t mask, const lasgd_clip *cli
     ApplyArgs a{};
     fill_common(c, a);
     fill_fine(c, a);
-    if (one_launch(c, true)) {
+    if (one_launch(c, NEXT_SCALE)) {
         const NormArgs n = norm_args(c, mask, *clip, a.ntiles);
         if (c->storage == LASGD_BF16) hipLaunchKernelGGL((small_scale_kernel<true>), dim3(n.count), dim3(64u * kSmallWaves), 0, c->main, a, n);
         else hipLaunchKernelGGL((small_scale_kernel<false>), dim3(n.count), dim3(64u * kSmallWaves), 0, c->main, a, n);

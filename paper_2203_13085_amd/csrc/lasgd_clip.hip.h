@@ -298,89 +298,93 @@ __global__ __launch_bounds__(kNormThreads) void scale_grads_kernel(const ApplyAr
 }
 
 // ---- short lists ---------------------------------------------------------------
-// Replicas of at most 64 tiles, the first block of the lookup table: a workgroup of sixteen waves takes one, a wave at most four of its tiles.  Their
-// gradients wait in registers for the norm, and everything is one launch.  Bound by latency: 4.8 us a step of the list of 5,453 elements in six tensors,
-// K = 3, in two launches 8.4.  one_launch in the host code holds the line.
+// Norm and what follows in one launch of workgroups of sixteen waves, bound by latency: 4.7 us a step of the list of 5,453 elements in six tensors, K = 3,
+// in two launches 9.4.  one_launch in the host code holds the lines.
 constexpr uint32_t kSmallWaves = 16;
 
-// The gradients of replica k, in f, and what comes of their norm, in all threads.
-template <bool BF16>
-__device__ __forceinline__ Clip small_norm(FourTiles &f, const ApplyArgs &a, const NormArgs &n, uint32_t k, uint32_t starts, uint32_t w)
+// What comes of a replica's sum of squares, in all threads; `says`: this workgroup is the one to write the norm.
+__device__ __forceinline__ Clip small_clip(const NormArgs &n, uint32_t k, double acc, bool says)
 {
     __shared__ Clip shared;
-    load_four<BF16, kSmallWaves>(f, a, k, 0u, starts, w, a.ntiles);
-    double acc = 0.0;
-#pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, f.v[u]);
     acc = block_sum<kSmallWaves>(acc);
-    if (threadIdx.x == 0u) shared = clip_of(n, k, acc);
+    if (threadIdx.x == 0u) {
+        NormArgs m = n;
+        if (!says) m.norms = nullptr;
+        shared = clip_of(m, k, acc);
+    }
     __syncthreads();
     return shared;
 }
 
+// The same of all of replica k, block by block of the lookup table: always in one order, so that every workgroup that takes it gets the same bits.
+template <bool BF16>
+__device__ __forceinline__ Clip whole_clip(const ApplyArgs &a, const NormArgs &n, uint32_t k, uint32_t w, bool says)
+{
+    constexpr uint32_t kBlock = 1u << kBlockShift;
+    double acc = 0.0;
+    for (uint32_t first = 0; first < a.ntiles; first += kBlock) {
+        const uint32_t t0 = as_const(a.blocks)[first >> kBlockShift] & ~kMoreInBlock;
+        FourTiles f;
+        load_four<BF16, kSmallWaves>(f, a, k, t0, later_starts(a, t0), first + w, first + kBlock < a.ntiles ? first + kBlock : a.ntiles);
+#pragma unroll
+        for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, f.v[u]);
+    }
+    return small_clip(n, k, acc, says);
+}
+
+// Clipping in place, lists of one block: a workgroup a replica, whose gradients wait in registers for the norm.
 template <bool BF16>
 __global__ __launch_bounds__(1024) void small_scale_kernel(const ApplyArgs a, const NormArgs n)
 {
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = (threadIdx.x & 63u) * 4u;
     const uint32_t k = n.count == a.K ? blockIdx.x : nth_bit(n.mask, blockIdx.x);
     FourTiles f;
-    const Clip cl = small_norm<BF16>(f, a, n, k, later_starts(a, 0u), w);
+    load_four<BF16, kSmallWaves>(f, a, k, 0u, later_starts(a, 0u), w, a.ntiles);
+    double acc = 0.0;
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, f.v[u]);
+    const Clip cl = small_clip(n, k, acc, true);
     if (cl.skip || cl.c == 1.f) return;
 #pragma unroll
     for (uint32_t u = 0; u < 4u; ++u) store_grad<BF16>(f.g[u], e, f.n[u], times(f.v[u], cl.c));
 }
 
-// A local step of the replicas in the mask.  Model and momentum are asked for with the gradients and wait in registers too.
-// bf16 models this short are never in s alone.
+// A local step of the replicas in the mask.  Sixteen tiles of a replica to a workgroup (blockIdx.y: which), one a wave; each workgroup takes the norm
+// of the whole replica by itself rather than wait for the others: gradients are only read here.  A wave asks for its tile's gradients, model and
+// momentum first.  bf16: one_launch sees to it that the models are in the master copies.
 template <bool BF16>
 __global__ __launch_bounds__(1024) void small_step_kernel(const ApplyArgs a, const ExtArgs xa, const NormArgs n)
 {
-    __shared__ Clip shared;
+    constexpr uint32_t ESZ = BF16 ? 2u : 4u;
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = (threadIdx.x & 63u) * 4u;
-    const uint32_t k = replica_at<true>(a, &xa, blockIdx.x), starts = later_starts(a, 0u);
-    float4 g[4], x[4], v[4];
-    char *xu[4];
-    float *vp[4], *xm[4], wd[4];
-    uint32_t m[4];
-    double acc = 0.0;
-#pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u) {
-        const uint32_t tile = w + u * kSmallWaves;
-        m[u] = 0;
-        g[u] = x[u] = v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (tile < a.ntiles) {
-            const uint32_t tensor = (uint32_t)__popcll(__ballot(starts <= tile));
-            const Record rec = load_record(a, k, tensor);
-            const Tile t = locate(a, rec, tile, tensor, 256u);
-            const size_t ao = (size_t)k * a.npad + t.aoff;
-            m[u] = lane_elems<false>(e, t.count);
-            wd[u] = t.wd;
-            xu[u] = reinterpret_cast<char *>(rec.x) + t.toff * (BF16 ? 2u : 4u);
-            vp[u] = a.v + ao;
-            xm[u] = BF16 ? a.x32 + ao : reinterpret_cast<float *>(xu[u]);
-            if (m[u]) {
-                g[u] = grad_at<BF16>(reinterpret_cast<const char *>(rec.g) + t.toff * (BF16 ? 2u : 4u), e, m[u]);
-                x[u] = grad_at<false>(reinterpret_cast<const char *>(xm[u]), e, m[u]);
-                v[u] = ld4<0>(vp[u] + e);                          // the arenas are padded to whole rows
-            }
+    const uint32_t k = replica_at<true>(a, &xa, blockIdx.x), tile = blockIdx.y * kSmallWaves + w;
+    float4 g = make_float4(0.f, 0.f, 0.f, 0.f), x = g, v = g;
+    char *xu = nullptr;
+    float *vp = nullptr, *xm = nullptr, wd = 0.f;
+    uint32_t m = 0;
+    if (tile < a.ntiles) {
+        const uint32_t tensor = tensor_of(a, tile);
+        const Record rec = load_record(a, k, tensor);
+        const Tile t = locate(a, rec, tile, tensor, 256u);
+        const size_t ao = (size_t)k * a.npad + t.aoff;
+        m = lane_elems<false>(e, t.count);
+        wd = t.wd;
+        xu = reinterpret_cast<char *>(rec.x) + t.toff * ESZ;
+        vp = a.v + ao;
+        xm = BF16 ? a.x32 + ao : reinterpret_cast<float *>(xu);
+        if (m) {
+            g = grad_at<BF16>(reinterpret_cast<const char *>(rec.g) + t.toff * ESZ, e, m);
+            x = grad_at<false>(reinterpret_cast<const char *>(xm), e, m);
+            v = ld4<0>(vp + e);                          // the arenas are padded to whole rows
         }
     }
-#pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, g[u]);
-    acc = block_sum<kSmallWaves>(acc);
-    if (threadIdx.x == 0u) shared = clip_of(n, k, acc);
-    __syncthreads();
-    const Clip cl = shared;
-    if (cl.skip) return;
+    const Clip cl = whole_clip<BF16>(a, n, k, w, blockIdx.y == 0u);
+    if (cl.skip || !m) return;
     const float neg_lr = xa.neg_lr_k[k];
-#pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u) {
-        if (!m[u]) continue;
-        LASGD_FOR4(step_elem(comp(x[u], c), comp(v[u], c), cl.c * compv(g[u], c), wd[u], a.mu, neg_lr, a.nesterov);)
-        store_grad<false>(reinterpret_cast<char *>(vp[u]), e, m[u], v[u]);
-        store_grad<false>(reinterpret_cast<char *>(xm[u]), e, m[u], x[u]);
-        if constexpr (BF16) store_grad<true>(xu[u], e, m[u], x[u]);
-    }
+    LASGD_FOR4(step_elem(comp(x, c), comp(v, c), cl.c * compv(g, c), wd, a.mu, neg_lr, a.nesterov);)
+    store_grad<false>(reinterpret_cast<char *>(vp), e, m, v);
+    store_grad<false>(reinterpret_cast<char *>(xm), e, m, x);
+    if constexpr (BF16) store_grad<true>(xu, e, m, x);
 }
 
 // The same with the global update, of the replicas in the masks.
@@ -388,28 +392,25 @@ template <bool BF16>
 __global__ __launch_bounds__(1024) void small_update_kernel(const ApplyArgs a, const ExtArgs xa, const NormArgs n)
 {
     const uint32_t lane = threadIdx.x & 63u, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t k = replica_at<true>(a, &xa, blockIdx.x);
+    const uint32_t k = replica_at<true>(a, &xa, blockIdx.x), tile = blockIdx.y * kSmallWaves + w;
     const bool in_step = (xa.step_mask >> k) & 1ull, in_merge = (xa.merge_mask >> k) & 1ull;
-    const uint32_t starts = later_starts(a, 0u);
     Clip cl{1.f, 0u};
-    FourTiles f;
-    if (in_step) cl = small_norm<BF16>(f, a, n, k, starts, w);
-    for (uint32_t tile = w; tile < a.ntiles; tile += kSmallWaves) {
-        const uint32_t tensor = (uint32_t)__popcll(__ballot(starts <= tile));
-        const Record rec = load_record(a, k, tensor);
-        const Tile t = locate(a, rec, tile, tensor, 256u);
-        const float4 zt[1] = {ld4<0>(a.z + t.aoff + lane * 4u)};
-        char *xu = reinterpret_cast<char *>(rec.x) + t.toff * (BF16 ? 2u : 4u);
-        const char *gu = reinterpret_cast<const char *>(rec.g) + t.toff * (BF16 ? 2u : 4u);
-        const size_t ao = (size_t)k * a.npad + t.aoff;
-        float *xm = BF16 ? a.x32 + ao : nullptr;
-        const float nlr = xa.neg_lr_k[k];
+    if (in_step) cl = whole_clip<BF16>(a, n, k, w, blockIdx.y == 0u);
+    if (tile >= a.ntiles) return;
+    const uint32_t tensor = tensor_of(a, tile);
+    const Record rec = load_record(a, k, tensor);
+    const Tile t = locate(a, rec, tile, tensor, 256u);
+    const float4 zt[1] = {ld4<0>(a.z + t.aoff + lane * 4u)};
+    char *xu = reinterpret_cast<char *>(rec.x) + t.toff * (BF16 ? 2u : 4u);
+    const char *gu = reinterpret_cast<const char *>(rec.g) + t.toff * (BF16 ? 2u : 4u);
+    const size_t ao = (size_t)k * a.npad + t.aoff;
+    float *xm = BF16 ? a.x32 + ao : nullptr;
+    const float nlr = xa.neg_lr_k[k];
 #define LASGD_SMALL(OPX) apply_tile<1, OPX, BF16, 0, false, true, false, false, true>(a, xu, gu, xm, xm, a.v + ao, a.s + ao, zt, t.wd, t.count, lane, nlr, xa.alpha, cl)
-        if (!in_merge) LASGD_SMALL(OP_STEP);
-        else if (in_step) LASGD_SMALL(OP_STEP_MERGE);
-        else LASGD_SMALL(OP_MERGE);
+    if (!in_merge) LASGD_SMALL(OP_STEP);
+    else if (in_step) LASGD_SMALL(OP_STEP_MERGE);
+    else LASGD_SMALL(OP_MERGE);
 #undef LASGD_SMALL
-    }
 }
 
 } // namespace lasgd

@@ -122,6 +122,9 @@ LISTS = {
     "63 and 300": (1,) * 62 + (300,),
     "65 tiles": (16_385,),
     "65 of one": (1,) * 65,
+    "128 tiles": (32_768,),
+    "127 of many": (300, 1, 20_000, 700) + (1,) * 40 + (257,) + (3,) * 1,
+    "129 tiles": (32_769,),
 }
 
 
@@ -282,7 +285,7 @@ def test_what_is_not_finite(bad, place, storage):
                                            ("long", 2, dict(nontemporal=3)), ("odd", 64, {}), ("odd", 64, dict(nontemporal=3)),
                                            ("odd", 6, dict(vec=4, kper_step=2, waves_per_block=4, max_blocks=3)), ("odd", 6, dict(vec=2, waves_per_block=2)),
                                            ("long", 3, {}), ("64 tiles", 5, {}), ("64 tiles", 64, dict(vec=4)), ("64 of one", 3, {}),
-                                           ("63 and 300", 9, dict(nontemporal=3)), ("48 tiles", 6, dict(vec=4)), ("48 of many", 64, {}), ("49 tiles", 4, dict(vec=2)), ("65 tiles", 4, dict(vec=2)), ("65 of one", 7, {}), ("65 of one", 64, dict(kper_step=5))])
+                                           ("63 and 300", 9, dict(nontemporal=3)), ("128 tiles", 5, {}), ("128 tiles", 64, {}), ("128 tiles", 62, dict(vec=2)), ("127 of many", 9, {}), ("129 tiles", 5, {}), ("48 tiles", 6, dict(vec=4)), ("48 of many", 64, {}), ("49 tiles", 4, dict(vec=2)), ("65 tiles", 4, dict(vec=2)), ("65 of one", 7, {}), ("65 of one", 64, dict(kper_step=5))])
 def test_local_steps(name, K, tuning, storage):
     r = Rig(K, LISTS[name], storage)
     try:
@@ -314,7 +317,7 @@ def test_local_steps(name, K, tuning, storage):
 @pytest.mark.parametrize("K,numels,tuning,side", [(3, LISTS["odd"], {}, True), (5, LISTS["rows"], dict(nontemporal=3), True), (2, LISTS["long"], {}, True),
                                                   (4, LISTS["many"], {}, False), (4, (700_001, 3, 256), {}, True), (4, (700_001, 3, 256), dict(nontemporal=3), True),
                                                   (6, LISTS["odd"], dict(kper_merge=6, waves_per_block=2, vec=2), True), (5, LISTS["63 and 300"], {}, True),
-                                                  (7, LISTS["48 tiles"], dict(vec=4), True), (6, LISTS["48 of many"], {}, True), (7, LISTS["64 tiles"], dict(vec=4), True), (7, LISTS["65 of one"], dict(vec=4, kper_merge=3), True), (4, LISTS["65 tiles"], {}, False)])
+                                                  (64, LISTS["128 tiles"], {}, True), (62, LISTS["128 tiles"], {}, False), (64, LISTS["64 tiles"], {}, True), (9, LISTS["127 of many"], {}, True), (7, LISTS["48 tiles"], dict(vec=4), True), (6, LISTS["48 of many"], {}, True), (7, LISTS["64 tiles"], dict(vec=4), True), (7, LISTS["65 of one"], dict(vec=4, kper_merge=3), True), (4, LISTS["65 tiles"], {}, False)])
 def test_global_updates(K, numels, tuning, side, storage):
     """Steps and updates in turn; masks of the step, of the update, and a replica that is not finite and takes the update all the same.
     The lists with 700,001 elements hold a bf16 model in one place after an update."""
