@@ -312,7 +312,7 @@ lasgd_status lasgd_sgd_ar_step(lasgd_ctx *ctx, float lr);
  * A norm is not finite exactly when one of the gradients is an infinity or a NaN.  With skip_nonfinite such a replica
  * sits out what the call does with its gradients: clip_grads leaves them as they are, a step leaves x and v as they are (it
  * still takes part in a global update of the same call).  Without, the formulas above are followed as they stand: after an infinity
- * c_k is 0 (and 0 times infinity NaN), after a NaN it is NaN.
+ * c_k is 0 (and 0 times infinity NaN), after a NaN it is NaN.  An infinite max_norm is no limit: c_k is 1 whatever n_k is.
  *
  * All of it runs on the main stream, also the norms; ordering against the stream the gradients were made on is the caller's,
  * as for every step.  The clipped calls take tiles of 256 elements whatever lasgd_tuning.vec says.

@@ -1,7 +1,7 @@
 // Gradient norms and clipping: device code.
 //
 // Each replica (the paper's worker) has a norm of its own over its whole parameter list,
-//     n_k = sqrt(sum_t sum_i g[k][t][i]^2),    c_k = min(1, max_norm / (n_k + 1e-6)),
+//     n_k = sqrt(sum_t sum_i g[k][t][i]^2),    c_k = min(1, max_norm / (n_k + 1e-6)), 1 where max_norm is infinite,
 // and its gradients count times c_k.  Squares and sums are in fp64 from the elements on: 1e30 or 1e-30 neither overflows nor
 // vanishes in its square, and the sum is finite exactly when every element is.  Everything is added in an order that the launch shape fixes, so
 // the same call on the same gradients gives the same bits.
@@ -65,7 +65,8 @@ __device__ __forceinline__ Clip clip_of(const NormArgs &n, uint32_t k, double su
 {
     const double norm = __builtin_sqrt(sum);
     if (n.norms) *as_global<float>(n.norms + k) = (float)norm;
-    const double c = (double)n.max_norm / (norm + LASGD_CLIP_EPS);
+    // no limit: nothing is scaled, whatever the norm is (the quotient would make a NaN of an infinite one)
+    const double c = __builtin_isinf(n.max_norm) ? 1.0 : (double)n.max_norm / (norm + LASGD_CLIP_EPS);
     const bool finite = norm <= 1.7976931348623157e308;
     return Clip{c >= 1.0 ? 1.f : (float)c, n.skip_nonfinite && !finite ? 1u : 0u};          // a NaN stays one
 }
