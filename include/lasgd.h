@@ -335,8 +335,9 @@ lasgd_status lasgd_grad_norms(lasgd_ctx *ctx, uint64_t mask, float *norms);
  * Errors: as lasgd_grad_norms, plus INVALID for a NULL clip or a max_norm that is negative or NaN. */
 lasgd_status lasgd_clip_grads(lasgd_ctx *ctx, uint64_t mask, const lasgd_clip *clip);
 
-/* lasgd_local_step_ex with c_k g[k] in the place of g[k]; the gradients are only read.  fp32 storage: exactly lasgd_clip_grads and
- * lasgd_local_step_ex, same roundings; bf16 storage: c_k g[k] stays in fp32.
+/* lasgd_local_step_ex with c_k g[k] in the place of g[k]; the gradients are only read.  fp32 storage: exactly lasgd_clip_grads with the same mask and
+ * then lasgd_local_step_ex of the replicas that do not sit out, the same norms and roundings; bf16 storage: c_k g[k] stays in fp32, and
+ * n_k may be summed in another order.
  * Errors: as lasgd_local_step_ex, plus INVALID as lasgd_clip_grads. */
 lasgd_status lasgd_local_step_clip(lasgd_ctx *ctx, const float *lr, uint64_t mask, const lasgd_clip *clip);
 

@@ -957,7 +957,7 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
 // 14.0 / 11.4, K = 64 16.5 / 15.4, 24576 K = 3 11.8 / 12.1, K = 16 13.1 / 12.6, 32768 K = 16 13.9 / 14.6; in place 16384 K = 3 5.9 / 3.3, K = 64 7.8 / 4.3.
 bool one_launch(const lasgd_ctx *c, Next next, int op = OP_STEP)
 {
-    const uint32_t most = next == NEXT_UPDATE && op == OP_STEP ? 128u : 4u * kSmallWaves;
+    const uint32_t most = next == NEXT_UPDATE && op == OP_STEP ? kSmallBlocks << kBlockShift : 1u << kBlockShift;
     // bf16 models of this size may be in s alone (place_models), where these kernels do not look
     return c->tables_by_vec[0].ntiles <= most && (c->storage != LASGD_BF16 || array_bytes(c) < kOneCopyFrom);
 }

@@ -15,6 +15,7 @@ namespace lasgd {
 
 constexpr uint32_t kNormThreads = 1024, kNormWaves = kNormThreads / 64u;
 constexpr uint32_t kNormRun = 4u * kNormWaves;      // tiles a workgroup takes at a time, four a wave
+static_assert(kNormRun == 1u << kBlockShift, "a run is a block of the lookup table: one entry says what is in it");
 constexpr uint32_t kArriveStride = 32;          // words: 128 bytes
 
 struct NormArgs {
@@ -36,6 +37,15 @@ __device__ __forceinline__ void add_squares(double &acc, float4 g)
     acc = __builtin_fma((double)g.y, (double)g.y, acc);
     acc = __builtin_fma((double)g.z, (double)g.z, acc);
     acc = __builtin_fma((double)g.w, (double)g.w, acc);
+}
+
+// Into two sums, as in a run of one tensor (fp32).
+__device__ __forceinline__ void add_squares(double &a0, double &a1, float4 g)
+{
+    a0 = __builtin_fma((double)g.x, (double)g.x, a0);
+    a1 = __builtin_fma((double)g.y, (double)g.y, a1);
+    a0 = __builtin_fma((double)g.z, (double)g.z, a0);
+    a1 = __builtin_fma((double)g.w, (double)g.w, a1);
 }
 
 // The sum over a wave, in its first lane.
@@ -140,15 +150,11 @@ template <bool BF16> __device__ __forceinline__ void add_squares(double &a0, dou
     if constexpr (BF16) {
         add_squares(a0, widen4(make_uint2(v.x, v.y)));
         add_squares(a1, widen4(make_uint2(v.z, v.w)));
-    } else {
-        a0 = __builtin_fma((double)__uint_as_float(v.x), (double)__uint_as_float(v.x), a0);
-        a1 = __builtin_fma((double)__uint_as_float(v.y), (double)__uint_as_float(v.y), a1);
-        a0 = __builtin_fma((double)__uint_as_float(v.z), (double)__uint_as_float(v.z), a0);
-        a1 = __builtin_fma((double)__uint_as_float(v.w), (double)__uint_as_float(v.w), a1);
-    }
+    } else
+        add_squares(a0, a1, make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)));
 }
 
-// A workgroup's runs of 16 tiles, a quarter of a block of the lookup table.  A run inside one tensor, as nearly all of a long list are,
+// A workgroup's runs are blocks of the lookup table, 64 tiles.  A run inside one tensor, as nearly all of a long list are,
 // takes one lookup: its address, or NULL where several tensors meet in it or the list ends.
 template <bool BF16>
 __device__ __forceinline__ char *whole_run(const ApplyArgs &a, uint32_t k, uint32_t first, uint32_t entry)
@@ -159,7 +165,8 @@ __device__ __forceinline__ char *whole_run(const ApplyArgs &a, uint32_t k, uint3
     return rec.numel - off >= kNormRun * 256u ? reinterpret_cast<char *>(rec.g) + (uint64_t)off * (BF16 ? 2u : 4u) : nullptr;
 }
 
-// Any run, tile by tile: four of a wave's tiles from `tile` on, every W-th one.
+// Any run, tile by tile: four of a wave's tiles from `tile` on, every W-th one.  With sixteen waves a lane has the elements that it has in a run of one
+// tensor in fp32.
 struct FourTiles {
     char *g[4];             // the tensor's gradient from the tile on
     uint32_t n[4];          // how many of the lane's four elements there are
@@ -216,7 +223,7 @@ __global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(const ApplyArgs
         FourTiles f;
         load_four<BF16, kNormWaves>(f, a, k, t0, starts, first + w, end);
 #pragma unroll
-        for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, f.v[u]);
+        for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, a1, f.v[u]);
     }
     join_norm(n, k, blockIdx.x, n.parts, a0 + a1);
 }
@@ -301,14 +308,34 @@ __global__ __launch_bounds__(kNormThreads) void scale_grads_kernel(const ApplyAr
 // ---- short lists ---------------------------------------------------------------
 // Norm and what follows in one launch of workgroups of sixteen waves, bound by latency: 4.7 us a step of the list of 5,453 elements in six tensors, K = 3,
 // in two launches 9.4.  one_launch in the host code holds the lines.
-constexpr uint32_t kSmallWaves = 16;
+//
+// fp32 sums come to the same bits as grad_norm_kernel's, in which a list of two blocks has two workgroups: a clipped step is to be
+// clipping in place and a step, whichever of them takes one launch.  Each block's sum is made in the same order, and then they are added.
+constexpr uint32_t kSmallWaves = 16, kSmallBlocks = 2;           // at most
+static_assert(kSmallWaves == kNormWaves, "a lane's elements of a block are those it has in grad_norm_kernel");
 
-// What comes of a replica's sum of squares, in all threads; `says`: this workgroup is the one to write the norm.
-__device__ __forceinline__ Clip small_clip(const NormArgs &n, uint32_t k, double acc, bool says)
+// What comes of a replica's sum of squares, in all threads; `says`: this workgroup is the one to write the norm.  before: the sum of the block before the last, if
+// there is one.
+__device__ __forceinline__ Clip small_clip(const NormArgs &n, uint32_t k, bool two, double before, double acc, bool says)
 {
+    __shared__ double wave[kSmallBlocks][kSmallWaves];
     __shared__ Clip shared;
-    acc = block_sum<kSmallWaves>(acc);
+    const uint32_t w = threadIdx.x >> 6;
+    acc = wave_sum(acc);
+    if (two) before = wave_sum(before);
+    if ((threadIdx.x & 63u) == 0u) {
+        wave[0][w] = acc;
+        if (two) wave[1][w] = before;
+    }
+    __syncthreads();
     if (threadIdx.x == 0u) {
+#pragma unroll
+        for (uint32_t v = 1; v < kSmallWaves; ++v) acc += wave[0][v];
+        if (two) {
+#pragma unroll
+            for (uint32_t v = 1; v < kSmallWaves; ++v) before += wave[1][v];
+            acc = before + acc;
+        }
         NormArgs m = n;
         if (!says) m.norms = nullptr;
         shared = clip_of(m, k, acc);
@@ -317,20 +344,24 @@ __device__ __forceinline__ Clip small_clip(const NormArgs &n, uint32_t k, double
     return shared;
 }
 
-// The same of all of replica k, block by block of the lookup table: always in one order, so that every workgroup that takes it gets the same bits.
+// The same of all of replica k: always in one order, so that every workgroup that takes it gets the same bits.
 template <bool BF16>
 __device__ __forceinline__ Clip whole_clip(const ApplyArgs &a, const NormArgs &n, uint32_t k, uint32_t w, bool says)
 {
     constexpr uint32_t kBlock = 1u << kBlockShift;
-    double acc = 0.0;
+    double before = 0.0, acc = 0.0;
+#pragma unroll 1
     for (uint32_t first = 0; first < a.ntiles; first += kBlock) {
         const uint32_t t0 = as_const(a.blocks)[first >> kBlockShift] & ~kMoreInBlock;
         FourTiles f;
         load_four<BF16, kSmallWaves>(f, a, k, t0, later_starts(a, t0), first + w, first + kBlock < a.ntiles ? first + kBlock : a.ntiles);
+        double a0 = 0.0, a1 = 0.0;
 #pragma unroll
-        for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, f.v[u]);
+        for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, a1, f.v[u]);
+        before = acc;
+        acc = a0 + a1;
     }
-    return small_clip(n, k, acc, says);
+    return small_clip(n, k, a.ntiles > kBlock, before, acc, says);
 }
 
 // Clipping in place, lists of one block: a workgroup a replica, whose gradients wait in registers for the norm.
@@ -341,10 +372,10 @@ __global__ __launch_bounds__(1024) void small_scale_kernel(const ApplyArgs a, co
     const uint32_t k = n.count == a.K ? blockIdx.x : nth_bit(n.mask, blockIdx.x);
     FourTiles f;
     load_four<BF16, kSmallWaves>(f, a, k, 0u, later_starts(a, 0u), w, a.ntiles);
-    double acc = 0.0;
+    double a0 = 0.0, a1 = 0.0;
 #pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u) add_squares(acc, f.v[u]);
-    const Clip cl = small_clip(n, k, acc, true);
+    for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, a1, f.v[u]);
+    const Clip cl = small_clip(n, k, false, 0.0, a0 + a1, true);
     if (cl.skip || cl.c == 1.f) return;
 #pragma unroll
     for (uint32_t u = 0; u < 4u; ++u) store_grad<BF16>(f.g[u], e, f.n[u], times(f.v[u], cl.c));

@@ -1,4 +1,5 @@
-"""Gradient norms and clipping where a promise is easily broken: no limit next to what is not finite.
+"""Gradient norms and clipping where a promise is easily broken: no limit next to what is not finite, and one norm for calls that are to
+give the same bits.
 
 No tolerances: everything here is the other call's result, bit by bit, or a value that is rounded once."""
 import numpy as np
@@ -138,3 +139,64 @@ def test_class_without_a_limit_takes_the_norms_only():
     finally:
         p.close()
         q.close()
+
+
+# ---- one norm ------------------------------------------------------------------------------------------------------------
+def straddling(numels, big, tiny):
+    """`big` in the first of a lane's four elements in the first sixteen tiles, `tiny` elsewhere: tiny^2 is just under half an ulp of big^2's binade, so it is
+    lost where it is added to big^2 and counts where it meets its like first, and the 64-bit sum tells the order it was made in."""
+    out, tile = [], 0
+    for n in numels:
+        i = np.arange(n)
+        out.append(np.where((i % 4 == 0) & (tile + i // 256 < 16), np.float32(big), np.float32(tiny)).astype(np.float32))
+        tile += (n + 255) // 256
+    return np.concatenate(out)
+
+
+@pytest.mark.parametrize("numels,big,most", [((32_768,), "0x1.2ca558p+0", "0x1.8f7026p+4"),                # whole runs of one tensor
+                                             ((3, 20_000, 12_000), "0x1.624e48p+0", "0x1.4cac20p+5")])     # several tensors in a run
+def test_a_clipped_step_is_clipping_and_a_step(numels, big, most):
+    """fp32, lists of two blocks of tiles: the step takes one launch and clipping in place two, and both have to come to one coefficient.  The limits were
+    found by search: sums that differ by a few ulps on either side of where the coefficient rounds to its neighbour."""
+    tiny, most = float.fromhex("0x1.69db8cp-27"), float.fromhex(most)
+    a, b = Rig(1, numels), Rig(1, numels)
+    g = straddling(numels, float.fromhex(big), tiny)
+    try:
+        for r in (a, b):
+            r.load([g])
+        a.ctx.local_step_clip(0.05, most, norms=a.norms.data_ptr())
+        b.ctx.clip_grads(most, norms=b.norms.data_ptr())
+        b.ctx.local_step_ex([0.05], 1)
+        same_state(a, b, 1, "step")
+        assert a.read_norms().tolist() == b.read_norms().tolist()
+    finally:
+        a.close()
+        b.close()
+
+
+@pytest.mark.parametrize("K", [1, 5, 64])
+@pytest.mark.parametrize("name", ["odd", "64 tiles", "65 tiles", "128 tiles", "127 of many", "129 tiles", "blocks"])
+def test_a_clipped_step_is_clipping_and_a_step_on_every_route(name, K):
+    if K == 64:
+        name = {"blocks": "rows"}.get(name, name)
+    a, b = Rig(K, LISTS[name]), Rig(K, LISTS[name])
+    full, part = (1 << K) - 1, ((1 << K) - 1) & 0x5555555555555555
+    lrs = [0.05 * (1.0 + 0.01 * k) for k in range(K)]
+    try:
+        for r in (a, b):
+            r.ctx.snapshot()
+        for step, mask in enumerate((full, part, full)):
+            g = a.grads(step)
+            most = a.max_norm(g)
+            for r in (a, b):
+                r.load(g)
+                r.ctx.average()
+            a.ctx.local_step_clip(lrs, most, mask)
+            a.ctx.step_merge_clip(lrs, most, mask, full, True)
+            b.ctx.clip_grads(most, mask)
+            b.ctx.local_step_ex(lrs, mask)
+            b.ctx.step_merge_ex(lrs, mask, full, True)
+            same_state(a, b, K, f"step {step}")
+    finally:
+        a.close()
+        b.close()
