@@ -119,6 +119,8 @@ class LASGD:
         """Scale every replica's gradients in place to a norm of at most `max_norm`, on the current stream's time line.
         Returns the K norms before clipping, on the GPU.  skip_nonfinite: gradients with an infinity or a NaN stay as they are."""
         self._check_in_place()
+        if not self._unwatched():
+            return self._clip_by_torch(float(max_norm), skip_nonfinite)
         norms = torch.empty_like(self.grad_norms)
         cur = torch.cuda.current_stream(self.device)
         self.main.wait_stream(cur)                  # also with the memory of `norms`, which cur may have used before
@@ -126,6 +128,23 @@ class LASGD:
         cur.wait_stream(self.main)
         torch.autograd.graph.increment_version([p.grad for p in self._flat])
         return norms
+
+    @torch.no_grad()
+    def _clip_by_torch(self, max_norm: float, skip_nonfinite: bool) -> torch.Tensor:
+        # clip_grad_norm_ in torch's operations, for whoever watches them: the library's roundings, and sums in 64 bits as it makes them
+        if not max_norm >= 0.0:
+            raise B.LasgdError(B.ERR_INVALID, "max_norm must be >= 0 (infinity: no limit)")
+        most, norms = float(np.float32(max_norm)), []
+        for ps in self.params:
+            grads = [p.grad for p in ps]
+            norm = torch.linalg.vector_norm(torch.stack([torch.linalg.vector_norm(g, dtype=torch.float64) for g in grads]))
+            norms.append(norm.float())
+            c = most / (norm + 1e-6) if most < float("inf") else torch.ones_like(norm)
+            c = torch.where(c >= 1.0, torch.ones_like(c), c).float()
+            stays = (c == 1.0) | ~torch.isfinite(norm) if skip_nonfinite else c == 1.0
+            for g in grads:
+                g.copy_(torch.where(stays, g, (g.float() * c).to(g.dtype)))
+        return torch.stack(norms)
 
     def _check_in_place(self) -> None:
         # the library scales the buffers it is bound to: each gradient has to be the one that was bound, plain
@@ -139,12 +158,15 @@ class LASGD:
             assert (p.grad.data_ptr() == at and p.grad.is_contiguous() and p.grad.dtype == p.dtype
                     and p.grad.numel() * p.grad.element_size() == size), "a gradient is not the buffer that was bound"
 
-    def _eager(self) -> bool:
-        # the library's tables are there, nobody watches torch's operations, and no graph is recorded that could outlive the tables
+    def _unwatched(self) -> bool:
+        # nobody watches torch's operations, and kernels go to the replicas' device
         return (torch._C._len_torch_dispatch_stack() == 0 and torch._C._len_torch_function_stack() == 0
                 and torch._C._functorch.peek_interpreter_stack() is None and not torch.compiler.is_compiling()
-                and self.ctx.is_open and torch.cuda.current_device() == self.device.index
-                and not torch.cuda.is_current_stream_capturing())
+                and torch.cuda.current_device() == self.device.index)
+
+    def _eager(self) -> bool:
+        # the library's tables are there, nobody watches torch's operations, and no graph is recorded that could outlive the tables
+        return self._unwatched() and self.ctx.is_open and not torch.cuda.is_current_stream_capturing()
 
     def _check_bound(self) -> None:
         # a dropped or replaced .grad would leave the library reading a stale buffer

@@ -1,5 +1,5 @@
-"""Gradient norms and clipping where a promise is easily broken: no limit next to what is not finite, and one norm for calls that are to
-give the same bits.
+"""Gradient norms and clipping where a promise is easily broken: no limit next to what is not finite, one norm for calls that are to give the
+same bits, and torch watching its operations.
 
 No tolerances: everything here is the other call's result, bit by bit, or a value that is rounded once."""
 import numpy as np
@@ -8,7 +8,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2203_13085_amd import binding as B              # noqa: E402
-from tests.test_gpu_clip import LISTS, Rig, check_norms, norm64, _backward, _flat, _modules      # noqa: E402
+from tests.test_gpu_clip import LISTS, Rig, check_norms, coefficient, norm64, _backward, _flat, _modules      # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -200,3 +200,92 @@ def test_a_clipped_step_is_clipping_and_a_step_on_every_route(name, K):
     finally:
         a.close()
         b.close()
+
+
+# ---- torch watching ------------------------------------------------------------------------------------------------------
+def _watch(kind, seen):
+    """A mode that notes which memory torch's operations write in place."""
+    from torch.overrides import TorchFunctionMode
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    def note(func, args):
+        name = getattr(func, "__name__", str(func)).split(".")[0]
+        if name.endswith("_") and not name.endswith("__"):
+            for t in args[0] if isinstance(args[0], (list, tuple)) else [args[0]]:
+                seen.add(t.data_ptr())
+
+    class Dispatch(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            note(func, args)
+            return func(*args, **(kwargs or {}))
+
+    class Function(TorchFunctionMode):
+        def __torch_function__(self, func, types, args=(), kwargs=None):
+            note(func, args)
+            return func(*args, **(kwargs or {}))
+
+    return Dispatch() if kind == "dispatch" else Function()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", ["dispatch", "function"])
+@pytest.mark.parametrize("most,skip", [(0.5, False), (0.5, True), (INF, False), (1e9, True), (0.0, False)])
+def test_clip_grad_norm_is_seen_by_modes(kind, dtype, most, skip):
+    """While a mode watches torch's operations it sees every gradient written; the result is that of a call nobody watches."""
+    from paper_2203_13085_amd.torch_api import LASGD
+    K = 3
+    _, replicas = _modules(K, dtype)
+    opt = LASGD(replicas, lr=0.1)
+    view = torch.int16 if dtype == torch.bfloat16 else torch.int32
+    try:
+        opt.zero_grad()
+        _backward(replicas, 0, dtype)
+        list(replicas[2].parameters())[1].grad[4] = INF
+        torch.cuda.synchronize()
+        fresh = [p.grad.detach().clone() for p in opt._flat]
+        seen = set()
+        with _watch(kind, seen):
+            norms = opt.clip_grad_norm_(most, skip_nonfinite=skip)
+        assert {p.grad.data_ptr() for p in opt._flat} <= seen
+        watched = [p.grad.detach().clone() for p in opt._flat]
+        for p, g in zip(opt._flat, fresh):
+            p.grad.copy_(g)
+        plain = opt.clip_grad_norm_(most, skip_nonfinite=skip)
+        assert norms.dtype == plain.dtype and norms.tolist() == plain.tolist()
+        for w, p in zip(watched, opt._flat):
+            nan = torch.isnan(w)
+            assert torch.equal(nan, torch.isnan(p.grad))
+            assert torch.equal(w.view(view)[~nan], p.grad.view(view)[~nan])
+        with _watch(kind, seen), pytest.raises(B.LasgdError) as err:
+            opt.clip_grad_norm_(-1.0)
+        assert err.value.status == B.ERR_INVALID
+    finally:
+        opt.close()
+
+
+def test_clip_grad_norm_recorded():
+    """Inside a graph the library's own kernels are recorded; replays on new gradients, with eager work between them."""
+    from paper_2203_13085_amd.torch_api import LASGD
+    K, most = 3, 0.5
+    _, replicas = _modules(K)
+    opt = LASGD(replicas, lr=0.1)
+    try:
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            norms = opt.clip_grad_norm_(most)
+        for step in range(3):
+            opt.zero_grad()
+            _backward(replicas, step)
+            torch.cuda.synchronize()
+            before = [[p.grad.detach().clone() for p in r.parameters()] for r in replicas]
+            graph.replay()
+            torch.cuda.synchronize()
+            for k, r in enumerate(replicas):
+                n = norm64(_flat(before[k]))
+                check_norms([float(norms[k])], [n])
+                for p, b in zip(r.parameters(), before[k]):
+                    assert torch.equal(p.grad.cpu(), torch.from_numpy(coefficient(n, most) * b.cpu().numpy()))
+    finally:
+        torch.cuda.synchronize()
+        opt.close()
