@@ -289,3 +289,110 @@ def test_clip_grad_norm_recorded():
     finally:
         torch.cuda.synchronize()
         opt.close()
+
+
+# ---- what the calls' routes leave out elsewhere ----------------------------------------------------------------------------
+def test_streamed_norms_recorded_and_masked():
+    """More than 256 MiB of fp32 gradients, whose norms an update reads with the streaming hint: recorded, with masks, and next to the same calls in
+    pieces that are too small for that."""
+    K, n, st = 3, 25_000_003, torch.cuda.Stream()
+    rows = (n + 255) // 256 * 256
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    g = torch.zeros(K, rows, device="cuda")
+    for k in range(K):
+        g[k, :n] = torch.randn(n, generator=gen, device="cuda") * (1e-3 * (k + 1))
+    x0 = torch.randn(n, generator=gen, device="cuda") * 0.05
+    want = [float(torch.linalg.vector_norm(g[k, :n].double())) for k in range(K)]
+    most, full = float(np.float32(want[1])) * 0.75, (1 << K) - 1
+    sides, norms = [], torch.zeros(2, K, device="cuda")
+    for _ in range(2):
+        x = torch.zeros(K, rows, device="cuda")
+        x[:, :n] = x0
+        c = B.Context(K, [n], main_stream=st.cuda_stream, side_stream=st.cuda_stream, wd_scalar=1e-4)
+        for k in range(K):
+            c.bind(k, [x[k].data_ptr()], [g[k].data_ptr()])
+        sides.append((x, c))
+    torch.cuda.synchronize()
+    (xa, a), (xb, b) = sides
+    try:
+        assert 4 * K * rows > 256 << 20 > 4 * rows
+        a.snapshot()
+        b.snapshot()
+        graph = torch.cuda.CUDAGraph()
+        a.sync()
+        with torch.cuda.graph(graph, stream=st):
+            a.average()
+            a.local_step_clip(0.1, most)
+            a.step_merge_clip(0.1, most, full, full, True, norms=norms[0].data_ptr())
+        for rep in range(3):
+            with torch.cuda.stream(st):
+                graph.replay()
+            b.average()
+            for k in range(K):
+                b.local_step_clip(0.1, most, 1 << k)
+            for k in range(K):
+                b.local_step_clip(0.1, most, 1 << k, norms=norms[1].data_ptr())
+            b.merge(True)
+            a.sync()
+            assert torch.equal(xa, xb), rep
+            check_norms(norms[0].cpu().numpy().astype(np.float64), want)
+            check_norms(norms[1].cpu().numpy().astype(np.float64), want)
+        a.local_step_clip(0.1, most, full)
+        a.local_step_clip(0.1, most, 0b101)
+        for k in (0, 1, 2, 0, 2):
+            b.local_step_clip(0.1, most, 1 << k)
+        a.sync()
+        assert torch.equal(xa, xb)
+    finally:
+        a.close()
+        b.close()
+        del xa, xb, g, sides
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("skip", [False, True])
+def test_bf16_modules_train_with_clipped_gradients(skip):
+    """bf16 modules with fp32 master copies: backward, clipped step, now and then an overflow, against the oracle on the widened gradients."""
+    from oracle import lasgd_oracle as O32
+    from paper_2203_13085_amd import workloads as W
+    from paper_2203_13085_amd.torch_api import LASGD
+    K, m, lr, mu, wd, most = 3, 2, 0.05, 0.9, 1e-3, 0.5
+    base, replicas = _modules(K, torch.bfloat16)
+    opt = LASGD(replicas, lr=lr, momentum=mu, nesterov=True, weight_decay=wd, m=m, max_grad_norm=most, skip_nonfinite=skip)
+    ps = list(base.parameters())
+    orc = O32.Oracle(K, [p.numel() for p in ps], mu, True, [wd] * len(ps))
+    orc.set_model(_flat(ps))
+    clipped = 0
+    try:
+        tau, started = 0, False
+        for step in range(7):
+            opt.zero_grad()
+            _backward(replicas, step, torch.bfloat16)
+            if skip and step in (2, 5):
+                list(replicas[step % K].parameters())[1].grad[4] = INF
+            torch.cuda.synchronize()
+            grads = [_flat([p.grad for p in r.parameters()]) for r in replicas]
+            norms = [norm64(g) for g in grads]
+            live = sum(1 << k for k in range(K) if np.isfinite(norms[k]))
+            clipped += sum(n > most for n in norms)
+            opt.step()
+            check_norms(opt.grad_norms.cpu().numpy().astype(np.float64), norms)
+            with np.errstate(invalid="ignore"):
+                orc.local_step([coefficient(n, most) * g for n, g in zip(norms, grads)], [lr] * K, mask=live)
+            tau += 1
+            if not started:
+                orc.snapshot()
+                orc.average()
+                started, tau = True, 0
+            elif tau == m:
+                orc.merge(True)
+                orc.average()
+                tau = 0
+            torch.cuda.synchronize()
+            for k, r in enumerate(replicas):
+                got = np.concatenate([p.detach().view(torch.int16).cpu().numpy().ravel() for p in r.parameters()]).view(np.uint16)
+                np.testing.assert_array_equal(got, W.to_bf16_bits(orc.x[k]), err_msg=f"step {step} replica {k}")
+        assert 0 < clipped < 7 * K
+    finally:
+        opt.close()
