@@ -309,7 +309,8 @@ lasgd_status lasgd_sgd_ar_step(lasgd_ctx *ctx, float lr);
  * fp64 from the elements on, in an order that the call fixes (the same call on the same gradients gives the same bits), and rounded to fp32 once.  c_k is rounded to
  * fp32 once, and so is c_k g (in place: to the storage type).  c_k = 1 leaves every bit as it is.
  *
- * A norm is not finite exactly when one of the gradients is an infinity or a NaN.  With skip_nonfinite such a replica
+ * The fp64 norm is not finite exactly when one of the gradients is an infinity or a NaN.  (A finite one beyond fp32 is written to `norms` as an
+ * infinity; its replica is clipped like any other.)  With skip_nonfinite a replica whose fp64 norm is not finite
  * sits out what the call does with its gradients: clip_grads leaves them as they are, a step leaves x and v as they are (it
  * still takes part in a global update of the same call).  Without, the formulas above are followed as they stand: after an infinity
  * c_k is 0 (and 0 times infinity NaN), after a NaN it is NaN.  An infinite max_norm is no limit: c_k is 1 whatever n_k is.
@@ -321,7 +322,7 @@ lasgd_status lasgd_sgd_ar_step(lasgd_ctx *ctx, float lr);
 
 typedef struct {
     float max_norm;         /* >= 0; infinity: nothing is scaled, norms are taken and skip_nonfinite holds    */
-    int32_t skip_nonfinite; /* != 0: replicas whose norm is not finite sit out, see above                      */
+    int32_t skip_nonfinite; /* != 0: replicas whose fp64 norm is not finite sit out, see above                */
     float *norms;           /* device [K], 4-byte aligned, or NULL: n_k is written for the replicas that take part,
                                the other entries stay (lasgd_sgd_ar_step_clip: [1])                              */
 } lasgd_clip;

@@ -907,7 +907,7 @@ uint64_t grad_bytes(const lasgd_ctx *c, uint32_t replicas) { return replicas * c
 // with its mean, ResNet-50 K = 8 1190 / 1187 | 1174 / 1190, ResNet-18 K = 8 546 / 537 | 549 / 548, K = 6 400 / 405 | 416 / 412, K = 4 273 / 279 | 285 / 283, MobileNetV2
 // K = 16 312 / 322 | 326 / 323.  bf16, whose gradients are a ninth of what a step moves and not a fifth, never: ResNet-50 K = 16 1316 / 1383 | 1320 / 1380,
 // ResNet-18 K = 8 309 / 317 | 306 / 317, with its update 410 / 418 | 412 / 416.  Nor does clipping in place: with the copy in front ResNet-50 K = 8 595 / 589, K = 32 bf16 1277 / 1329, ResNet-18 K = 8 268 / 268, MobileNetV2 bf16 K = 16 77.5 / 85.6.
-// The norms alone always do: ResNet-50 K = 8 141 / 125, MobileNetV2 bf16 K = 16 25.1 / 23.5.
+// The norms alone always do, by loops of nothing else (no update of the same gradients behind them): ResNet-50 K = 8 141 / 125, MobileNetV2 bf16 K = 16 25.1 / 23.5.
 constexpr uint64_t kNormBytes = 400ull << 20, kNormHintFrom = 256ull << 20;
 uint32_t norm_batch(const lasgd_ctx *c, uint32_t replicas)
 {
@@ -952,9 +952,9 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
 
 // Lists this short take one launch for the norm and what follows (small_step_kernel): two of them are bound by the host, one by its workgroups, each of
 // which reads all gradients of its replica (in place, where that cannot be, a workgroup has a replica to itself).  us, two launches / one, three states in turn
-// on one stream, hosts of unlike speed: step, 300 elements K = 64 8.1 / 4.4, 9000 K = 3 to 64 5.8-9.1 / 4.5-5.6, 16384 K = 16 5.8 / 4.9, K = 64 10.2 / 7.0, 32768 K = 3
-// 7.6 / 6.3, K = 64 13.7 / 12.9, 49152 K = 16 9.5 / 8.7, K = 64 16.3 / 21.6; step + update, with its mean, 300 K = 3 10.7 / 9.3, 9000 14.3-16.2 / 11.2-13.7, 16384 K = 3
-// 14.0 / 11.4, K = 64 16.5 / 15.4, 24576 K = 3 11.8 / 12.1, K = 16 13.1 / 12.6, 32768 K = 16 13.9 / 14.6; in place 16384 K = 3 5.9 / 3.3, K = 64 7.8 / 4.3.
+// on streams of their own, hosts of unlike speed: step, 300 elements K = 64 7.6 / 4.5, 9000 K = 3 7.4 / 4.5, K = 64 6.1 / 3.9, 16384 K = 16 6.1 / 3.9, K = 64 6.2 / 3.9, 32768 K = 3
+// 7.5 / 4.5, K = 16 6.0 / 3.8, K = 64 8.7 / 10.9, bf16 8.6 / 8.3; step + update, with its mean, 300 K = 3 14.3 / 11.3, 9000 K = 16 10.0 / 7.9, 16384 K = 3
+// 10.2 / 8.0, K = 64 12.3 / 12.0; on one stream, step 49152 K = 16 9.5 / 8.7, K = 64 16.3 / 21.6; step + update 24576 K = 3 11.8 / 12.1, K = 16 13.1 / 12.6, 32768 K = 16 13.9 / 14.6; in place 16384 K = 3 5.9 / 3.3, K = 64 7.8 / 4.3.
 bool one_launch(const lasgd_ctx *c, Next next, int op = OP_STEP)
 {
     const uint32_t most = next == NEXT_UPDATE && op == OP_STEP ? kSmallBlocks << kBlockShift : 1u << kBlockShift;

@@ -102,7 +102,7 @@ __device__ __forceinline__ float4 grad_at(const char *g, uint32_t e, uint32_t n)
 // Shares and counter are only ever touched by atomics of device scope, which bypass the XCDs' own L2s, so no cache has to be written back
 // or invalidated for them.  What is needed beyond is that a share is in memory before its arrival is counted: the store is waited
 // for.  (Left to an acquire-release addition, every workgroup writes back and invalidates its L2: norms of ResNet-50 K = 32 bf16
-// 1863 us in place of 280.)  Counters of different replicas lie on lines of their own, kArriveStride apart.
+// 1863 us in place of 242.)  Counters of different replicas lie on lines of their own, kArriveStride apart.
 __device__ __forceinline__ void join_norm(const NormArgs &n, uint32_t k, uint32_t group, uint32_t groups, double acc)
 {
     double *part = n.part + (size_t)k * n.stride;
@@ -306,8 +306,8 @@ __global__ __launch_bounds__(kNormThreads) void scale_grads_kernel(const ApplyAr
 }
 
 // ---- short lists ---------------------------------------------------------------
-// Norm and what follows in one launch of workgroups of sixteen waves, bound by latency: 4.7 us a step of the list of 5,453 elements in six tensors, K = 3,
-// in two launches 9.4.  one_launch in the host code holds the lines.
+// Norm and what follows in one launch of workgroups of sixteen waves, bound by latency: 4.5 us a step of the list of 5,453 elements in six tensors, K = 3,
+// in two launches 6.2 to 8.1.  one_launch in the host code holds the lines.
 //
 // fp32 sums come to the same bits as grad_norm_kernel's, in which a list of two blocks has two workgroups: a clipped step is to be
 // clipping in place and a step, whichever of them takes one launch.  Each block's sum is made in the same order, and then they are added.
