@@ -953,7 +953,7 @@ lasgd_status enqueue_norms(lasgd_ctx *c, uint64_t mask, const lasgd_clip &clip, 
 // Lists this short take one launch for the norm and what follows (small_step_kernel): two of them are bound by the host, one by its workgroups, each of
 // which reads all gradients of its replica (in place, where that cannot be, a workgroup has a replica to itself).  us, two launches / one, three states in turn
 // on streams of their own, hosts of unlike speed: step, 300 elements K = 64 7.6 / 4.5, 9000 K = 3 7.4 / 4.5, K = 64 6.1 / 3.9, 16384 K = 16 6.1 / 3.9, K = 64 6.2 / 3.9, 32768 K = 3
-// 7.5 / 4.5, K = 16 6.0 / 3.8, K = 64 8.7 / 10.9, bf16 8.6 / 8.3; step + update, with its mean, 300 K = 3 14.3 / 11.3, 9000 K = 16 10.0 / 7.9, 16384 K = 3
+// 7.5 / 4.5, K = 16 6.0 / 3.8, K = 64 8.7 / 10.4, bf16 9.1 / 9.1; step + update, with its mean, 300 K = 3 14.3 / 11.3, 9000 K = 16 10.0 / 7.9, 16384 K = 3
 // 10.2 / 8.0, K = 64 12.3 / 12.0; on one stream, step 49152 K = 16 9.5 / 8.7, K = 64 16.3 / 21.6; step + update 24576 K = 3 11.8 / 12.1, K = 16 13.1 / 12.6, 32768 K = 16 13.9 / 14.6; in place 16384 K = 3 5.9 / 3.3, K = 64 7.8 / 4.3.
 bool one_launch(const lasgd_ctx *c, Next next, int op = OP_STEP)
 {

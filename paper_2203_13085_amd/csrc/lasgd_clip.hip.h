@@ -314,54 +314,45 @@ __global__ __launch_bounds__(kNormThreads) void scale_grads_kernel(const ApplyAr
 constexpr uint32_t kSmallWaves = 16, kSmallBlocks = 2;           // at most
 static_assert(kSmallWaves == kNormWaves, "a lane's elements of a block are those it has in grad_norm_kernel");
 
-// What comes of a replica's sum of squares, in all threads; `says`: this workgroup is the one to write the norm.  before: the sum of the block before the last, if
-// there is one.
-__device__ __forceinline__ Clip small_clip(const NormArgs &n, uint32_t k, bool two, double before, double acc, bool says)
+// What comes of a replica's sums of squares, wave[block][its waves], in all threads; `says`: this workgroup is the one to write the norm.
+__device__ __forceinline__ Clip small_clip(const NormArgs &n, uint32_t k, const double (*wave)[kSmallWaves], uint32_t blocks, bool says)
 {
-    __shared__ double wave[kSmallBlocks][kSmallWaves];
     __shared__ Clip shared;
-    const uint32_t w = threadIdx.x >> 6;
-    acc = wave_sum(acc);
-    if (two) before = wave_sum(before);
-    if ((threadIdx.x & 63u) == 0u) {
-        wave[0][w] = acc;
-        if (two) wave[1][w] = before;
-    }
     __syncthreads();
     if (threadIdx.x == 0u) {
+        double sum = 0.0;
+        for (uint32_t b = 0; b < blocks; ++b) {
+            double acc = wave[b][0];
 #pragma unroll
-        for (uint32_t v = 1; v < kSmallWaves; ++v) acc += wave[0][v];
-        if (two) {
-#pragma unroll
-            for (uint32_t v = 1; v < kSmallWaves; ++v) before += wave[1][v];
-            acc = before + acc;
+            for (uint32_t w = 1; w < kSmallWaves; ++w) acc += wave[b][w];
+            sum += acc;
         }
         NormArgs m = n;
         if (!says) m.norms = nullptr;
-        shared = clip_of(m, k, acc);
+        shared = clip_of(m, k, sum);
     }
     __syncthreads();
     return shared;
 }
 
-// The same of all of replica k: always in one order, so that every workgroup that takes it gets the same bits.
+// The same of all of replica k: always in one order, so that every workgroup that takes it gets the same bits.  A block's sums leave the registers before the next
+// one's gradients come: kept until all are there, 64 replicas of 128 tiles take 10.9 us a step in place of 10.4.
 template <bool BF16>
 __device__ __forceinline__ Clip whole_clip(const ApplyArgs &a, const NormArgs &n, uint32_t k, uint32_t w, bool says)
 {
     constexpr uint32_t kBlock = 1u << kBlockShift;
-    double before = 0.0, acc = 0.0;
-#pragma unroll 1
+    __shared__ double wave[kSmallBlocks][kSmallWaves];
     for (uint32_t first = 0; first < a.ntiles; first += kBlock) {
-        const uint32_t t0 = as_const(a.blocks)[first >> kBlockShift] & ~kMoreInBlock;
+        const uint32_t b = first >> kBlockShift, t0 = as_const(a.blocks)[b] & ~kMoreInBlock;
         FourTiles f;
         load_four<BF16, kSmallWaves>(f, a, k, t0, later_starts(a, t0), first + w, first + kBlock < a.ntiles ? first + kBlock : a.ntiles);
         double a0 = 0.0, a1 = 0.0;
 #pragma unroll
         for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, a1, f.v[u]);
-        before = acc;
-        acc = a0 + a1;
+        const double sum = wave_sum(a0 + a1);
+        if ((threadIdx.x & 63u) == 0u) wave[b][w] = sum;
     }
-    return small_clip(n, k, a.ntiles > kBlock, before, acc, says);
+    return small_clip(n, k, wave, (a.ntiles + kBlock - 1u) / kBlock, says);
 }
 
 // Clipping in place, lists of one block: a workgroup a replica, whose gradients wait in registers for the norm.
@@ -375,7 +366,10 @@ __global__ __launch_bounds__(1024) void small_scale_kernel(const ApplyArgs a, co
     double a0 = 0.0, a1 = 0.0;
 #pragma unroll
     for (uint32_t u = 0; u < 4u; ++u) add_squares(a0, a1, f.v[u]);
-    const Clip cl = small_clip(n, k, false, 0.0, a0 + a1, true);
+    __shared__ double wave[1][kSmallWaves];
+    const double sum = wave_sum(a0 + a1);
+    if ((threadIdx.x & 63u) == 0u) wave[0][w] = sum;
+    const Clip cl = small_clip(n, k, wave, 1u, true);
     if (cl.skip || cl.c == 1.f) return;
 #pragma unroll
     for (uint32_t u = 0; u < 4u; ++u) store_grad<BF16>(f.g[u], e, f.n[u], times(f.v[u], cl.c));
