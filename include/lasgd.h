@@ -352,6 +352,101 @@ lasgd_status lasgd_step_merge_clip(lasgd_ctx *ctx, const float *lr, uint64_t ste
  * Errors: as lasgd_sgd_ar_step, plus INVALID as lasgd_clip_grads, and ALLOC where there is no memory for the array. */
 lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *ctx, float lr, const lasgd_clip *clip);
 
+/* ---- layers: operators of the replicas' forward and backward passes -------------------
+ *
+ * What a language model's replicas compute between two updates, for all K replicas in one call: dropout, root-mean-square norms and gated
+ * blocks.  Weights are tensors of the bound parameter list, each replica's own; their gradients go into the bound gradient
+ * buffers, where the update reads them, and autograd's second copy of them is not needed.
+ *
+ * Activations and their gradients are the caller's, of the storage type.  rows: host [K], how many rows (tokens) replica k has; a replica with 0
+ * rows takes no part, and rows behind a replica's last are neither read nor written.  Inputs may have any stride >= 0 (0: every replica, or every row, reads the
+ * same); the rows of an output must not overlap.  An output may be an input of the same call (same address and strides) where the call says so;
+ * otherwise outputs overlap nothing that the call reads or writes.  Pointers are aligned to an element; with 16-byte aligned
+ * addresses and strides, and a multiple of 8 columns, accesses are 16 bytes wide.
+ *
+ * stream: hipStream_t the passes run on (NULL = default stream).  Ordering against the main stream, which writes the parameters and reads the gradients, is
+ * the caller's, as for lasgd_zero_grads.  A call takes the buffers that are bound when it is made, a recorded one those bound
+ * when it was recorded.  No call allocates device memory or changes the context, so calls on different streams may run at the same time; two that
+ * write the same gradient may not.  workspace: device memory of the caller's, 16-byte aligned, as many bytes as the call's _bytes function
+ * says, in use until the call has run: two calls that may run at the same time, and two graphs that may be replayed at the same time, need one each.
+ *
+ * Sums, norms and products are in fp32, results are rounded to the storage type once.  The same call on the same data gives the
+ * same bits.  accumulate: the weights' gradients are added to what their buffers hold (0: they replace it, also
+ * of a replica with 0 rows, which are then 0).
+ * Errors of all: INVALID (NULL, a stride, size or tensor index out of range, misaligned, a workspace that is too small, the context's device not current),
+ * STATE (a replica is unbound), UNSUPPORTED (2^31 rows of all replicas together, or beyond a limit below), HIP.
+ */
+typedef struct {             /* element (k, r, c) is at data[k * replica_stride + r * row_stride + c] */
+    void *data;              /* device */
+    int64_t replica_stride;  /* elements */
+    int64_t row_stride;
+} lasgd_rows;
+
+/*
+ * A dropout mask, which is never stored: of element (k, r, c) of an activation with `cols` columns it is made from its place and from these, and from
+ * nothing else.  Philox 4x32 with ten rounds, key `seed`, counter (i, i >> 32 | k << 16, n, n >> 32) with i = r * ceil(cols / 8) + c / 8 and
+ * n = call + *counter; element c % 8 takes the low (even) or high (odd) half of word c % 8 / 2, and is dropped if that is below round(p * 65536).  What
+ * stays counts 1 / (1 - round(p * 65536) / 65536) times, so the mean is kept exactly; a dropped element counts 0 whatever it holds.
+ * Use another number n for every dropout of a step and every step; the backward pass takes its forward pass's.
+ */
+typedef struct {
+    float p;                 /* 0..1; 0: no dropout, nothing else here is read                       */
+    uint64_t seed, call;
+    const uint64_t *counter; /* device, 8-byte aligned, or NULL (0): for recorded calls, whose `call` is fixed */
+} lasgd_drop;
+
+/*
+ * y = residual + drop(x); residual may be NULL (none), and y may be x or residual.  The backward pass is the same call on dy, without a residual.
+ * Errors: as above, and UNSUPPORTED beyond 2^48 groups of eight columns a replica.
+ */
+lasgd_status lasgd_dropout(lasgd_ctx *ctx, const int64_t *rows, int64_t cols, const lasgd_rows *x, const lasgd_rows *residual,
+                           const lasgd_rows *y, const lasgd_drop *drop, void *stream);
+
+/*
+ * h = residual + drop(x),  y = gain * h / sqrt(mean(h^2) + eps) over a row.  gain: index of a bound tensor, whose length is the number of columns.
+ * residual may be NULL (none), sum too (h is not written; h enters the norm before it is rounded), and drop (no dropout).  scales NULL: y of the
+ * storage type.  Otherwise y is e4m3 (OCP, one byte an element) and scales, fp32, gets scale = max |y| / 448 of each row (at least 2^-126) at
+ * data[k * replica_stride + r * row_stride]; y / scale is rounded to nearest even.  sum may be x or residual, and y, in the storage type, x or residual.
+ * Errors: as above, and UNSUPPORTED beyond LASGD_NORM_MAX_COLS columns.
+ */
+#define LASGD_NORM_MAX_COLS 16384
+lasgd_status lasgd_rms_norm(lasgd_ctx *ctx, int32_t gain, const int64_t *rows, const lasgd_rows *x, const lasgd_rows *residual,
+                            const lasgd_rows *sum, const lasgd_rows *y, const lasgd_rows *scales, float eps, const lasgd_drop *drop, void *stream);
+
+/*
+ * Its backward pass.  h: the sum as it was stored (x, without residual and dropout); dy: gradient of y; dsum: gradient that arrives at h itself, or
+ * NULL.  dresidual = the gradient of h, dx = drop of that; each may be NULL (not wanted), and may be h, dy or dsum.  The gain's gradient goes to its
+ * bound buffer.  (The 8-bit output's gradient is that of y before it was rounded.)
+ */
+lasgd_status lasgd_rms_norm_backward(lasgd_ctx *ctx, int32_t gain, const int64_t *rows, const lasgd_rows *h, const lasgd_rows *dy,
+                                     const lasgd_rows *dsum, const lasgd_rows *dresidual, const lasgd_rows *dx, float eps,
+                                     const lasgd_drop *drop, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream);
+lasgd_status lasgd_rms_norm_backward_bytes(lasgd_ctx *ctx, int32_t gain, const int64_t *rows, int64_t *bytes);
+
+typedef enum {
+    LASGD_SILU = 0,          /* v / (1 + exp(-v))                                                  */
+    LASGD_GELU = 1,          /* v (1 + erf(v / sqrt(2))) / 2                                       */
+    LASGD_GELU_TANH = 2,     /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2                  */
+    LASGD_RELU = 3           /* v if v > 0, else 0                                                 */
+} lasgd_activation;
+
+/*
+ * g = x Wg^T,  u = x Wu^T,  a = f(g) u.  gate, up: indices of bound tensors, [wide][cols] row by row, wide = their length / cols; one index for both: a
+ * tensor [2][wide][cols] that holds the two.  x has `cols` columns; a, g and u have `wide`.  g and u, which the backward pass reads, are both given or both NULL.
+ * a is made from g and u before these are rounded.
+ */
+lasgd_status lasgd_gated(lasgd_ctx *ctx, int32_t gate, int32_t up, const int64_t *rows, int64_t cols, const lasgd_rows *x, const lasgd_rows *g,
+                         const lasgd_rows *u, const lasgd_rows *a, lasgd_activation activation, void *stream);
+
+/*
+ * Its backward pass, from da, the gradient of a: dg = da u f'(g) and du = da f(g), rounded to the storage type (in the workspace), then
+ * dx = dg Wg + du Wu (dx may be NULL: not wanted) and the weights' gradients dg^T x and du^T x into their bound buffers.
+ */
+lasgd_status lasgd_gated_backward(lasgd_ctx *ctx, int32_t gate, int32_t up, const int64_t *rows, int64_t cols, const lasgd_rows *x,
+                                  const lasgd_rows *g, const lasgd_rows *u, const lasgd_rows *da, const lasgd_rows *dx,
+                                  lasgd_activation activation, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream);
+lasgd_status lasgd_gated_backward_bytes(lasgd_ctx *ctx, int32_t gate, int32_t up, const int64_t *rows, int64_t cols, int64_t *bytes);
+
 /*
  * Parity probe: wait for both streams, then copy one array to host memory as
  * fp32.  tensor >= 0: that tensor of replica k, n must equal numel[tensor];

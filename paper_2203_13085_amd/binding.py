@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "liblasgd_hip.so")
 OK, ERR_INVALID, ERR_STATE, ERR_ALLOC, ERR_HIP, ERR_UNSUPPORTED = range(6)
 F32, BF16 = 0, 1
 STATE_X, STATE_V, STATE_S, STATE_Z = range(4)
+SILU, GELU, GELU_TANH, RELU = range(4)
 _STATUS_NAMES = ["OK", "ERR_INVALID", "ERR_STATE", "ERR_ALLOC", "ERR_HIP", "ERR_UNSUPPORTED"]
 
 EXPORTS = ["lasgd_create", "lasgd_bind", "lasgd_init_master", "lasgd_local_step", "lasgd_snapshot",
@@ -29,7 +30,9 @@ EXPORTS = ["lasgd_create", "lasgd_bind", "lasgd_init_master", "lasgd_local_step"
            "lasgd_average_ex", "lasgd_merge_ex", "lasgd_step_merge_ex", "lasgd_set_elastic",
            "lasgd_sgd_ar_step", "lasgd_global_update_static", "lasgd_step_merge_average",
            "lasgd_zero_grads", "lasgd_grad_norms", "lasgd_clip_grads", "lasgd_local_step_clip",
-           "lasgd_step_merge_clip", "lasgd_sgd_ar_step_clip"]
+           "lasgd_step_merge_clip", "lasgd_sgd_ar_step_clip", "lasgd_dropout", "lasgd_rms_norm",
+           "lasgd_rms_norm_backward", "lasgd_rms_norm_backward_bytes", "lasgd_gated", "lasgd_gated_backward",
+           "lasgd_gated_backward_bytes"]
 
 
 class LasgdError(RuntimeError):
@@ -48,6 +51,14 @@ class Config(ctypes.Structure):
 
 class Clip(ctypes.Structure):
     _fields_ = [("max_norm", ctypes.c_float), ("skip_nonfinite", ctypes.c_int32), ("norms", ctypes.c_void_p)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("replica_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class Drop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("call", ctypes.c_uint64), ("counter", ctypes.c_void_p)]
 
 
 class Tuning(ctypes.Structure):
@@ -104,6 +115,14 @@ def load() -> ctypes.CDLL:
     L.lasgd_local_step_clip.argtypes = [P, f32p, u64, clip]
     L.lasgd_step_merge_clip.argtypes = [P, f32p, u64, u64, i32, clip]
     L.lasgd_sgd_ar_step_clip.argtypes = [P, f32, clip]
+    rp, ip, drop = ctypes.POINTER(Rows), ctypes.POINTER(i64), ctypes.POINTER(Drop)
+    L.lasgd_dropout.argtypes = [P, ip, i64, rp, rp, rp, drop, P]
+    L.lasgd_rms_norm.argtypes = [P, i32, ip, rp, rp, rp, rp, rp, f32, drop, P]
+    L.lasgd_rms_norm_backward.argtypes = [P, i32, ip, rp, rp, rp, rp, rp, f32, drop, i32, P, i64, P]
+    L.lasgd_rms_norm_backward_bytes.argtypes = [P, i32, ip, ip]
+    L.lasgd_gated.argtypes = [P, i32, i32, ip, i64, rp, rp, rp, rp, ctypes.c_int, P]
+    L.lasgd_gated_backward.argtypes = [P, i32, i32, ip, i64, rp, rp, rp, rp, rp, ctypes.c_int, i32, P, i64, P]
+    L.lasgd_gated_backward_bytes.argtypes = [P, i32, i32, ip, i64, ip]
     L.lasgd_last_error.argtypes = [P]
     L.lasgd_last_error.restype = ctypes.c_char_p
     L.lasgd_destroy.argtypes = [P]
@@ -286,6 +305,59 @@ class Context:
 
     def sgd_ar_step_clip(self, lr: float, max_norm: float, *, skip_nonfinite: bool = False, norms: Optional[int] = None) -> None:
         self._check(self._L.lasgd_sgd_ar_step_clip(self._h, lr, self._clip(max_norm, skip_nonfinite, norms)))
+
+    # -- layers: dropout, root-mean-square norms and gated blocks of all replicas -----------
+    # rows: K counts.  An activation is (address, replica stride, row stride), strides in elements, or None where it may be absent.
+    # The passes run on `stream` (a raw handle; None = the default stream).
+    def _counts(self, rows):
+        assert len(rows) == self.K
+        return (ctypes.c_int64 * self.K)(*rows)
+
+    @staticmethod
+    def _at(a):
+        return None if a is None else ctypes.byref(Rows(a[0], a[1], a[2]))
+
+    def dropout(self, rows, cols: int, x, y, p: float, *, residual=None, seed: int = 0, call: int = 0,
+                counter: Optional[int] = None, stream: Optional[int] = None) -> None:
+        """y = residual + drop(x).  counter: device address of 64 bits that are added to `call`."""
+        self._check(self._L.lasgd_dropout(self._h, self._counts(rows), cols, self._at(x), self._at(residual), self._at(y),
+                                          ctypes.byref(Drop(p, seed, call, counter)), stream or None))
+
+    def rms_norm(self, gain: int, rows, x, y, *, residual=None, sum=None, scales=None, eps: float = 1e-6, p: float = 0.0,
+                 seed: int = 0, call: int = 0, counter: Optional[int] = None, stream: Optional[int] = None) -> None:
+        """sum = residual + drop(x), y = gain * sum / rms(sum); with scales (address, replica stride, row stride) y is e4m3."""
+        self._check(self._L.lasgd_rms_norm(self._h, gain, self._counts(rows), self._at(x), self._at(residual), self._at(sum),
+                                           self._at(y), self._at(scales), eps, ctypes.byref(Drop(p, seed, call, counter)), stream or None))
+
+    def rms_norm_backward_bytes(self, gain: int, rows) -> int:
+        n = ctypes.c_int64(0)
+        self._check(self._L.lasgd_rms_norm_backward_bytes(self._h, gain, self._counts(rows), ctypes.byref(n)))
+        return n.value
+
+    def rms_norm_backward(self, gain: int, rows, h, dy, dx=None, *, dsum=None, dresidual=None, eps: float = 1e-6, p: float = 0.0,
+                          seed: int = 0, call: int = 0, counter: Optional[int] = None, accumulate: bool = True,
+                          workspace: Optional[int] = None, workspace_bytes: int = 0, stream: Optional[int] = None) -> None:
+        self._check(self._L.lasgd_rms_norm_backward(self._h, gain, self._counts(rows), self._at(h), self._at(dy), self._at(dsum),
+                                                    self._at(dresidual), self._at(dx), eps, ctypes.byref(Drop(p, seed, call, counter)),
+                                                    int(bool(accumulate)), workspace or None, workspace_bytes, stream or None))
+
+    def gated(self, gate: int, up: int, rows, cols: int, x, a, *, g=None, u=None, activation: int = SILU,
+              stream: Optional[int] = None) -> None:
+        """a = f(x Wg^T) * (x Wu^T); g and u are the two products, for the backward pass."""
+        self._check(self._L.lasgd_gated(self._h, gate, up, self._counts(rows), cols, self._at(x), self._at(g), self._at(u),
+                                        self._at(a), activation, stream or None))
+
+    def gated_backward_bytes(self, gate: int, up: int, rows, cols: int) -> int:
+        n = ctypes.c_int64(0)
+        self._check(self._L.lasgd_gated_backward_bytes(self._h, gate, up, self._counts(rows), cols, ctypes.byref(n)))
+        return n.value
+
+    def gated_backward(self, gate: int, up: int, rows, cols: int, x, g, u, da, dx=None, *, activation: int = SILU,
+                       accumulate: bool = True, workspace: Optional[int] = None, workspace_bytes: int = 0,
+                       stream: Optional[int] = None) -> None:
+        self._check(self._L.lasgd_gated_backward(self._h, gate, up, self._counts(rows), cols, self._at(x), self._at(g), self._at(u),
+                                                 self._at(da), self._at(dx), activation, int(bool(accumulate)), workspace or None,
+                                                 workspace_bytes, stream or None))
 
     def read_state(self, which: int, k: int = 0, tensor: int = -1) -> np.ndarray:
         # an out-of-range tensor index is the library's to refuse

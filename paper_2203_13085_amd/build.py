@@ -7,6 +7,7 @@ import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "lasgd.hip")
+LAYERS_SRC = os.path.join(HERE, "csrc", "lasgd_layers.hip")
 LIB = os.path.join(HERE, "liblasgd_hip.so")
 WALK_SRC = os.path.join(HERE, "csrc", "grad_walk.cpp")
 WALK_LIB = os.path.join(HERE, "_grad_walk" + sysconfig.get_config_var("EXT_SUFFIX"))     # another Python does not load it
@@ -21,7 +22,7 @@ FLAGS = [
 
 def build_hip(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + ["-o", LIB, SRC]
+    cmd = [hipcc] + FLAGS + ["-parallel-jobs=2", "-o", LIB, SRC, LAYERS_SRC]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)

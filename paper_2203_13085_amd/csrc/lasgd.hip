@@ -12,6 +12,7 @@
 // while the other stream may still read them.
 #include "lasgd_kernels.hip.h"
 #include "lasgd_clip.hip.h"
+#include "lasgd_context.h"
 #include "../../include/lasgd.h"
 
 #include <cmath>
@@ -71,7 +72,7 @@ struct lasgd_ctx {
     Tables tables_by_vec[3];
     const Tables *tables = nullptr;              // those of the current tile size
     Record *records = nullptr;                   // device table [K*n_tensors]
-    std::vector<void *> h_xptr;
+    std::vector<void *> h_xptr, h_gptr;      // [K*n_tensors] as bound
     std::vector<char> bound;
     int32_t n_bound = 0;
 
@@ -103,18 +104,24 @@ struct lasgd_ctx {
 
 namespace {
 
-lasgd_status fail(lasgd_ctx *ctx, lasgd_status st, const char *fmt, ...)
+lasgd_status vfail(lasgd_ctx *ctx, lasgd_status st, const char *fmt, va_list ap)
 {
     char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
     try {
         if (ctx) ctx->err = buf;
         else g_create_error = buf;
     } catch (...) {       // the message is lost, the status is not
     }
+    return st;
+}
+
+lasgd_status fail(lasgd_ctx *ctx, lasgd_status st, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vfail(ctx, st, fmt, ap);
+    va_end(ap);
     return st;
 }
 
@@ -1006,6 +1013,25 @@ void release(lasgd_ctx *c)
 
 } // namespace
 
+// ---- for the other translation units ---------------------------------------
+namespace lasgd {
+
+ContextView view_of(const lasgd_ctx *c)
+{
+    return ContextView{c->K, c->n_tensors, c->device, c->storage == LASGD_BF16, c->n_bound == c->K, c->numel.data(), c->h_xptr.data(), c->h_gptr.data()};
+}
+
+lasgd_status refuse(lasgd_ctx *c, lasgd_status st, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vfail(c, st, fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+} // namespace lasgd
+
 static lasgd_status create_impl(const lasgd_config *cfg, lasgd_ctx **out)
 {
     if (out) *out = nullptr;
@@ -1043,6 +1069,7 @@ static lasgd_status create_impl(const lasgd_config *cfg, lasgd_ctx **out)
     c->ntotal = total;
     c->bound.assign((size_t)c->K, 0);
     c->h_xptr.assign((size_t)c->K * c->n_tensors, nullptr);
+    c->h_gptr.assign((size_t)c->K * c->n_tensors, nullptr);
     c->tune = default_tuning(*c);
 
 #define CREATE_HIP(call)                                                                       \
@@ -1129,6 +1156,7 @@ lasgd_status lasgd_bind(lasgd_ctx *c, int32_t k, void *const *params, void *cons
                          (uint32_t)c->numel[t], c->wd[t], 0u};
     LASGD_HIP(c, hipMemcpy(c->records + base, recs.data(), recs.size() * sizeof(Record), hipMemcpyHostToDevice));
     memcpy(&c->h_xptr[base], params, recs.size() * sizeof(void *));
+    memcpy(&c->h_gptr[base], grads, recs.size() * sizeof(void *));
     if (!c->bound[(size_t)k]) {
         c->bound[(size_t)k] = 1;
         ++c->n_bound;

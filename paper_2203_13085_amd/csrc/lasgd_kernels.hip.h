@@ -11,8 +11,7 @@
 // __builtin_fmaf calls below fuse.  Local update: Algorithm 1 steps 3 and 7
 // with the optimizer of Sec. 5.2; global update: step 9a-b; mean: Sec. 3 Eq. 8.
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "lasgd_memory.hip.h"
 
 namespace lasgd {
 
@@ -122,28 +121,8 @@ struct Clip {
 
 // ---- 128-bit / 64-bit accesses, optionally with the streaming hint --------
 // NT: 1 the hint on loads, 2 on stores; 4 belongs to the kernels that ask for a word of their model before their loads.
-// Every pointer the kernels dereference is device (global) memory.  Pointers
-// that come out of the tables are generic as far as the compiler can tell and
-// would be accessed with FLAT instructions; casting to the global address
-// space makes every access a GLOBAL load or store.
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
-#define LASGD_GLOBAL_AS __attribute__((address_space(1)))
-template <class T> __device__ __forceinline__ const LASGD_GLOBAL_AS T *as_global(const void *p)
-{
-    return reinterpret_cast<const LASGD_GLOBAL_AS T *>(reinterpret_cast<uintptr_t>(p));
-}
-template <class T> __device__ __forceinline__ LASGD_GLOBAL_AS T *as_global(void *p)
-{
-    return reinterpret_cast<LASGD_GLOBAL_AS T *>(reinterpret_cast<uintptr_t>(p));
-}
-
-#define LASGD_CONST_AS __attribute__((address_space(4)))
-template <class T> __device__ __forceinline__ const LASGD_CONST_AS T *as_const(const T *p)
-{
-    return reinterpret_cast<const LASGD_CONST_AS T *>(reinterpret_cast<uintptr_t>(p));
-}
-
 typedef uint32_t u32x16_t __attribute__((ext_vector_type(16), aligned(4)));
 
 // The tensor that tile `tile` (wave-uniform) belongs to.

@@ -1,0 +1,472 @@
+// Host side of the operators of the replicas' forward and backward passes: checks, launch shapes.  Declared in include/lasgd.h.
+#include "lasgd_context.h"
+#include "lasgd_gated.hip.h"
+
+#include <cmath>
+#include <cstring>
+
+using namespace lasgd;
+
+namespace {
+
+constexpr int64_t kMaxRows = 0x7fffffff;             // of all replicas together
+constexpr int64_t kMaxGroups = 1ll << 48;            // of eight columns, a replica's, where a mask's counter names them
+constexpr int64_t kMaxBlocks = 0x7fffffff;           // of a launch, along x
+
+// What a call's rows come to.
+struct Rows {
+    uint32_t n[64], first[64];
+    uint32_t most = 0, total = 0, replicas = 0;      // replicas: with any rows
+};
+
+#define CHECK(cond, st, ...) do { if (!(cond)) return refuse(c, st, __VA_ARGS__); } while (0)
+#define TRY(call) do { const lasgd_status st_ = (call); if (st_ != LASGD_OK) return st_; } while (0)
+
+lasgd_status check_call(lasgd_ctx *c, const ContextView &v, const int64_t *rows, Rows &r)
+{
+    CHECK(rows, LASGD_ERR_INVALID, "NULL rows");
+    int64_t total = 0;
+    for (int32_t k = 0; k < v.K; ++k) {
+        CHECK(rows[k] >= 0, LASGD_ERR_INVALID, "rows[%d] = %lld", k, (long long)rows[k]);
+        CHECK(rows[k] <= kMaxRows - total, LASGD_ERR_UNSUPPORTED, "more than %lld rows", (long long)kMaxRows);
+        r.first[k] = (uint32_t)total;
+        r.n[k] = (uint32_t)rows[k];
+        total += rows[k];
+        if (r.n[k] > r.most) r.most = r.n[k];
+        r.replicas += rows[k] > 0;
+    }
+    r.total = (uint32_t)total;
+    return LASGD_OK;
+}
+
+lasgd_status check_device(lasgd_ctx *c, const ContextView &v)
+{
+    int dev = -1;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        return refuse(c, LASGD_ERR_HIP, "hipGetDevice failed: %s", hipGetErrorString(e));
+    }
+    CHECK(dev == v.device, LASGD_ERR_INVALID, "the context is on device %d, the current device is %d", v.device, dev);
+    return LASGD_OK;
+}
+
+// An activation of `cols` columns.  vec comes out false if accesses of eight elements would not be aligned (es bytes an element).  A stride that
+// nothing is multiplied with does not count.
+lasgd_status check_rows(lasgd_ctx *c, const ContextView &v, const Rows &r, const char *name, const lasgd_rows *a, int64_t cols, int es, bool output,
+                        RowsAt &at, bool &vec)
+{
+    CHECK(a && a->data, LASGD_ERR_INVALID, "NULL %s", name);
+    at = RowsAt{(char *)a->data, v.K > 1 ? a->replica_stride : 0, r.most > 1 ? a->row_stride : 0};
+    CHECK((uintptr_t)a->data % es == 0, LASGD_ERR_INVALID, "%s is not aligned to its elements", name);
+    CHECK(at.rs >= 0 && at.ss >= 0, LASGD_ERR_INVALID, "%s has a negative stride", name);
+    const __int128 end = (__int128)at.rs * (v.K - 1) + (__int128)at.ss * (r.most ? r.most - 1 : 0) + cols;
+    CHECK(end * es < (__int128)1 << 47, LASGD_ERR_INVALID, "%s reaches beyond the address space", name);
+    if (output) {
+        CHECK(r.most <= 1 || at.ss >= cols, LASGD_ERR_INVALID, "the rows of %s overlap: stride %lld, %lld columns", name, (long long)at.ss, (long long)cols);
+        if (r.replicas > 1) {
+            const bool apart = at.rs >= (int64_t)(r.most - 1) * at.ss + cols;
+            const bool turned = at.rs >= cols && (r.most <= 1 || at.ss >= (v.K - 1) * at.rs + cols);
+            CHECK(apart || turned, LASGD_ERR_INVALID, "the replicas of %s overlap: stride %lld", name, (long long)at.rs);
+        }
+    }
+    const int wide = es == 1 ? 8 : 16;
+    if (cols % 8 || (uintptr_t)a->data % wide || at.rs * es % wide || at.ss * es % wide) vec = false;
+    return LASGD_OK;
+}
+
+lasgd_status check_drop(lasgd_ctx *c, const lasgd_drop *d, DropArgs &a)
+{
+    a = DropArgs{};
+    if (!d) return LASGD_OK;
+    CHECK(d->p >= 0.f && d->p <= 1.f, LASGD_ERR_INVALID, "p = %g is no probability", (double)d->p);
+    if (d->p == 0.f) return LASGD_OK;
+    a.below = (uint32_t)std::lrint((double)d->p * 65536.0);
+    a.scale = a.below < 65536u ? (float)(65536.0 / (65536.0 - a.below)) : 0.f;
+    a.seed = d->seed;
+    a.call = d->call;
+    a.counter = d->counter;
+    CHECK((uintptr_t)d->counter % 8 == 0, LASGD_ERR_INVALID, "the counter is not 8-byte aligned");
+    return LASGD_OK;
+}
+
+lasgd_status check_groups(lasgd_ctx *c, const Rows &r, int64_t cols)
+{
+    CHECK((__int128)r.most * ((cols + 7) / 8) < kMaxGroups, LASGD_ERR_UNSUPPORTED, "a mask of more than 2^48 groups of eight columns");
+    return LASGD_OK;
+}
+
+lasgd_status check_tensor(lasgd_ctx *c, const ContextView &v, const char *name, int32_t t)
+{
+    CHECK(t >= 0 && t < v.n_tensors, LASGD_ERR_INVALID, "%s = %d outside 0..%d", name, t, v.n_tensors - 1);
+    return LASGD_OK;
+}
+
+lasgd_status check_workspace(lasgd_ctx *c, const void *p, int64_t have, int64_t need)
+{
+    if (!need) return LASGD_OK;
+    CHECK(p, LASGD_ERR_INVALID, "NULL workspace");
+    CHECK((uintptr_t)p % 16 == 0, LASGD_ERR_INVALID, "the workspace is not 16-byte aligned");
+    CHECK(have >= need, LASGD_ERR_INVALID, "a workspace of %lld bytes, %lld are needed", (long long)have, (long long)need);
+    return LASGD_OK;
+}
+
+lasgd_status launched(lasgd_ctx *c)
+{
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return refuse(c, LASGD_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return LASGD_OK;
+}
+
+template <class T> void copy_rows(T &a, const Rows &r, int32_t K) { memcpy(a.rows, r.n, K * sizeof(uint32_t)); }
+
+uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
+
+// f(std::integral_constant<bool, ...>...) for two flags.
+template <class F> void two_flags(bool a, bool b, F f)
+{
+    if (a) {
+        if (b) f(std::true_type{}, std::true_type{});
+        else f(std::true_type{}, std::false_type{});
+    } else {
+        if (b) f(std::false_type{}, std::true_type{});
+        else f(std::false_type{}, std::false_type{});
+    }
+}
+
+// Threads that share a row of a norm, and groups of eight columns that each of them holds.
+template <int G_, int NV_> struct NormShape { static constexpr int G = G_, NV = NV_; };
+template <class F> void norm_shape(uint32_t groups, F f)
+{
+    if (groups <= 16u) f(NormShape<16, 1>{});
+    else if (groups <= 64u) f(NormShape<64, 1>{});
+    else if (groups <= 128u) f(NormShape<64, 2>{});
+    else if (groups <= 256u) f(NormShape<64, 4>{});
+    else if (groups <= 512u) f(NormShape<256, 2>{});
+    else if (groups <= 1024u) f(NormShape<256, 4>{});
+    else f(NormShape<1024, 2>{});
+}
+
+// Workgroups a replica of a norm's backward pass, and the shares of the gain's gradient that they leave.
+struct Shares {
+    uint32_t parts, shares;
+    int64_t bytes;
+};
+Shares norm_shares(int32_t K, const Rows &r, uint32_t groups)
+{
+    Shares s{};
+    norm_shape(groups, [&](auto shape) {
+        constexpr uint32_t R = norm_threads(shape.G) / shape.G;
+        const uint32_t want = 1024u / (r.replicas ? r.replicas : 1u), have = ceil_div(r.most, R);
+        s.parts = have < want ? have : want;
+        s.shares = s.parts * R;
+    });
+    s.bytes = (int64_t)K * s.shares * groups * 8 * sizeof(float);
+    return s;
+}
+
+lasgd_status check_norm(lasgd_ctx *c, ContextView &v, int32_t gain, const int64_t *rows, Rows &r, int64_t &cols)
+{
+    v = view_of(c);
+    TRY(check_call(c, v, rows, r));
+    TRY(check_tensor(c, v, "gain", gain));
+    cols = v.numel[gain];
+    CHECK(cols <= LASGD_NORM_MAX_COLS, LASGD_ERR_UNSUPPORTED, "%lld columns, LASGD_NORM_MAX_COLS is %d", (long long)cols, LASGD_NORM_MAX_COLS);
+    return LASGD_OK;
+}
+
+lasgd_status check_eps(lasgd_ctx *c, float eps)
+{
+    CHECK(std::isfinite(eps) && eps >= 0.f, LASGD_ERR_INVALID, "eps must be finite and >= 0");
+    return LASGD_OK;
+}
+
+} // namespace
+
+extern "C" lasgd_status lasgd_dropout(lasgd_ctx *c, const int64_t *rows, int64_t cols, const lasgd_rows *x, const lasgd_rows *residual,
+                                      const lasgd_rows *y, const lasgd_drop *drop, void *stream)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    const ContextView v = view_of(c);
+    const int es = v.bf16 ? 2 : 4;
+    Rows r;
+    DropoutArgs a{};
+    bool vec = true;
+    TRY(check_call(c, v, rows, r));
+    CHECK(cols >= 1 && cols <= kMaxRows, LASGD_ERR_INVALID, "cols = %lld", (long long)cols);
+    CHECK(drop, LASGD_ERR_INVALID, "NULL drop");
+    TRY(check_drop(c, drop, a.drop));
+    if (!a.drop.below) a.drop.scale = 1.f;
+    TRY(check_groups(c, r, cols));
+    TRY(check_rows(c, v, r, "x", x, cols, es, false, a.x, vec));
+    if (residual) TRY(check_rows(c, v, r, "residual", residual, cols, es, false, a.residual, vec));
+    TRY(check_rows(c, v, r, "y", y, cols, es, true, a.y, vec));
+    TRY(check_device(c, v));
+    if (!r.most) return LASGD_OK;
+    a.cols = (uint32_t)cols;
+    a.groups = ceil_div(cols, 8);
+    while (a.tx_shift < 8u && (1u << a.tx_shift) < a.groups) ++a.tx_shift;
+    copy_rows(a, r, v.K);
+    const dim3 grid(ceil_div(r.most, (256u >> a.tx_shift) * kDropRows), v.K);
+    two_flags(v.bf16, vec, [&](auto bf16, auto wide) {
+        hipLaunchKernelGGL((dropout_kernel<bf16, wide>), grid, dim3(256), 0, (hipStream_t)stream, a);
+    });
+    return launched(c);
+}
+
+extern "C" lasgd_status lasgd_rms_norm(lasgd_ctx *c, int32_t gain, const int64_t *rows, const lasgd_rows *x, const lasgd_rows *residual,
+                                       const lasgd_rows *sum, const lasgd_rows *y, const lasgd_rows *scales, float eps, const lasgd_drop *drop, void *stream)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    ContextView v;
+    Rows r;
+    int64_t cols;
+    NormRowsArgs a{};
+    bool vec = true, ignored = true;
+    TRY(check_norm(c, v, gain, rows, r, cols));
+    const int es = v.bf16 ? 2 : 4;
+    TRY(check_eps(c, eps));
+    TRY(check_drop(c, drop, a.drop));
+    TRY(check_groups(c, r, cols));
+    TRY(check_rows(c, v, r, "x", x, cols, es, false, a.x, vec));
+    if (residual) TRY(check_rows(c, v, r, "residual", residual, cols, es, false, a.residual, vec));
+    if (sum) TRY(check_rows(c, v, r, "sum", sum, cols, es, true, a.sum, vec));
+    TRY(check_rows(c, v, r, "y", y, cols, scales ? 1 : es, true, a.y, vec));
+    if (scales) TRY(check_rows(c, v, r, "scales", scales, 1, 4, true, a.scales, ignored));
+    CHECK(v.all_bound, LASGD_ERR_STATE, "not every replica is bound");
+    TRY(check_device(c, v));
+    if (!r.most) return LASGD_OK;
+    a.cols = (uint32_t)cols;
+    a.groups = ceil_div(cols, 8);
+    a.eps = eps;
+    a.inv_cols = (float)(1.0 / (double)cols);
+    copy_rows(a, r, v.K);
+    for (int32_t k = 0; k < v.K; ++k) a.gain[k] = (const char *)v.params[(size_t)k * v.n_tensors + gain];
+    norm_shape(a.groups, [&](auto shape) {
+        constexpr int G = decltype(shape)::G, NV = decltype(shape)::NV, T = norm_threads(G);
+        const dim3 grid(ceil_div(r.most, T / G), v.K);
+        two_flags(v.bf16, vec, [&](auto bf16, auto wide) {
+            hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV>), grid, dim3(T), 0, (hipStream_t)stream, a);
+        });
+    });
+    return launched(c);
+}
+
+extern "C" lasgd_status lasgd_rms_norm_backward_bytes(lasgd_ctx *c, int32_t gain, const int64_t *rows, int64_t *bytes)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    ContextView v;
+    Rows r;
+    int64_t cols;
+    CHECK(bytes, LASGD_ERR_INVALID, "NULL bytes");
+    TRY(check_norm(c, v, gain, rows, r, cols));
+    *bytes = norm_shares(v.K, r, ceil_div(cols, 8)).bytes;
+    return LASGD_OK;
+}
+
+extern "C" lasgd_status lasgd_rms_norm_backward(lasgd_ctx *c, int32_t gain, const int64_t *rows, const lasgd_rows *h, const lasgd_rows *dy,
+                                                const lasgd_rows *dsum, const lasgd_rows *dresidual, const lasgd_rows *dx, float eps,
+                                                const lasgd_drop *drop, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    ContextView v;
+    Rows r;
+    int64_t cols;
+    NormBackArgs a{};
+    bool vec = true;
+    TRY(check_norm(c, v, gain, rows, r, cols));
+    const int es = v.bf16 ? 2 : 4;
+    TRY(check_eps(c, eps));
+    TRY(check_drop(c, drop, a.drop));
+    TRY(check_groups(c, r, cols));
+    TRY(check_rows(c, v, r, "h", h, cols, es, false, a.h, vec));
+    TRY(check_rows(c, v, r, "dy", dy, cols, es, false, a.dy, vec));
+    if (dsum) TRY(check_rows(c, v, r, "dsum", dsum, cols, es, false, a.dsum, vec));
+    if (dresidual) TRY(check_rows(c, v, r, "dresidual", dresidual, cols, es, true, a.dresidual, vec));
+    if (dx) TRY(check_rows(c, v, r, "dx", dx, cols, es, true, a.dx, vec));
+    a.groups = ceil_div(cols, 8);
+    const Shares s = norm_shares(v.K, r, a.groups);
+    TRY(check_workspace(c, workspace, workspace_bytes, s.bytes));
+    CHECK(v.all_bound, LASGD_ERR_STATE, "not every replica is bound");
+    TRY(check_device(c, v));
+    if (!r.most && accumulate) return LASGD_OK;
+    a.cols = (uint32_t)cols;
+    a.eps = eps;
+    a.inv_cols = (float)(1.0 / (double)cols);
+    a.parts = s.parts;
+    a.part = (float *)workspace;
+    copy_rows(a, r, v.K);
+    JoinArgs j{(const float *)workspace, s.shares, (uint32_t)cols, a.groups, accumulate, {}};
+    for (int32_t k = 0; k < v.K; ++k) {
+        a.gain[k] = (const char *)v.params[(size_t)k * v.n_tensors + gain];
+        j.grad[k] = (char *)v.grads[(size_t)k * v.n_tensors + gain];
+    }
+    if (r.most) {
+        norm_shape(a.groups, [&](auto shape) {
+            constexpr int G = decltype(shape)::G, NV = decltype(shape)::NV, T = norm_threads(G);
+            two_flags(v.bf16, vec, [&](auto bf16, auto wide) {
+                hipLaunchKernelGGL((rms_norm_backward_kernel<bf16, wide, G, NV>), dim3(s.parts, v.K), dim3(T), 0, (hipStream_t)stream, a);
+            });
+        });
+        TRY(launched(c));
+    }
+    const dim3 grid(ceil_div(cols, 16), v.K);
+    if (v.bf16) hipLaunchKernelGGL((join_gain_kernel<true>), grid, dim3(256), 0, (hipStream_t)stream, j);
+    else hipLaunchKernelGGL((join_gain_kernel<false>), grid, dim3(256), 0, (hipStream_t)stream, j);
+    return launched(c);
+}
+
+// ---- gated blocks ------------------------------------------------------------------------------------------------------------
+namespace {
+
+struct Gated {
+    ContextView v;
+    Rows r;
+    int64_t wide, pitch;
+    int es;
+};
+
+lasgd_status check_gated(lasgd_ctx *c, Gated &d, int32_t gate, int32_t up, const int64_t *rows, int64_t cols)
+{
+    d.v = view_of(c);
+    d.es = d.v.bf16 ? 2 : 4;
+    TRY(check_call(c, d.v, rows, d.r));
+    TRY(check_tensor(c, d.v, "gate", gate));
+    TRY(check_tensor(c, d.v, "up", up));
+    CHECK(cols >= 1, LASGD_ERR_INVALID, "cols = %lld", (long long)cols);
+    const int64_t n = d.v.numel[gate], per = gate == up ? 2 * cols : cols;
+    CHECK(n % per == 0, LASGD_ERR_INVALID, "tensor %d has %lld elements, no multiple of %lld", gate, (long long)n, (long long)per);
+    CHECK(gate == up || d.v.numel[up] == n, LASGD_ERR_INVALID, "gate has %lld elements, up %lld", (long long)n, (long long)d.v.numel[up]);
+    d.wide = n / per;
+    d.pitch = (d.wide + 7) / 8 * 8;
+    const __int128 tiles_w = (d.wide + kTile - 1) / kTile, tiles_c = (cols + kTile - 1) / kTile, tiles_r = (d.r.most + kTile - 1) / kTile;
+    CHECK(tiles_r * tiles_w <= kMaxBlocks && tiles_r * tiles_c <= kMaxBlocks && tiles_w * tiles_c <= kMaxBlocks, LASGD_ERR_UNSUPPORTED, "too many tiles");
+    return LASGD_OK;
+}
+
+lasgd_status check_act(lasgd_ctx *c, lasgd_activation act)
+{
+    CHECK((int)act >= LASGD_SILU && (int)act <= LASGD_RELU, LASGD_ERR_INVALID, "unknown activation %d", (int)act);
+    return LASGD_OK;
+}
+
+ProductArgs product_args(const Gated &d, int64_t cols, lasgd_activation act)
+{
+    ProductArgs a{};
+    a.cols = (uint32_t)cols;
+    a.wide = (uint32_t)d.wide;
+    a.pitch = (uint32_t)d.pitch;
+    a.act = (int32_t)act;
+    copy_rows(a, d.r, d.v.K);
+    memcpy(a.first, d.r.first, d.v.K * sizeof(uint32_t));
+    return a;
+}
+
+void weights(ProductArgs &a, const Gated &d, void *const *of, int32_t gate, int32_t up, int64_t cols)
+{
+    for (int32_t k = 0; k < d.v.K; ++k) {
+        a.gate[k] = (char *)of[(size_t)k * d.v.n_tensors + gate];
+        a.up[k] = (char *)of[(size_t)k * d.v.n_tensors + up] + (gate == up ? d.wide * cols * d.es : 0);
+    }
+}
+
+template <int FORM> void launch_product(const Gated &d, const ProductArgs &a, bool vm, bool vn, hipStream_t st)
+{
+    const uint64_t M = FORM == DW ? d.wide : d.r.most, N = FORM == FWD ? a.wide : a.cols;
+    const dim3 grid(ceil_div(M, kTile) * ceil_div(N, kTile), d.v.K, FORM == DW ? 2 : 1);
+    two_flags(vm, vn, [&](auto m, auto n) {
+        if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((product_kernel<false, FORM, m, n>), grid, dim3(256), 0, st, a);
+    });
+}
+
+int64_t gated_bytes(const Gated &d) { return 2 * (int64_t)d.r.total * d.pitch * d.es; }
+
+} // namespace
+
+extern "C" lasgd_status lasgd_gated(lasgd_ctx *c, int32_t gate, int32_t up, const int64_t *rows, int64_t cols, const lasgd_rows *x, const lasgd_rows *g,
+                                    const lasgd_rows *u, const lasgd_rows *a, lasgd_activation activation, void *stream)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    Gated d;
+    TRY(check_gated(c, d, gate, up, rows, cols));
+    TRY(check_act(c, activation));
+    ProductArgs p = product_args(d, cols, activation);
+    bool vx = true, vo = true;
+    TRY(check_rows(c, d.v, d.r, "x", x, cols, d.es, false, p.x, vx));
+    CHECK(!g == !u, LASGD_ERR_INVALID, "g and u are given together or not at all");
+    if (g) {
+        TRY(check_rows(c, d.v, d.r, "g", g, d.wide, d.es, true, p.g, vo));
+        TRY(check_rows(c, d.v, d.r, "u", u, d.wide, d.es, true, p.u, vo));
+    }
+    TRY(check_rows(c, d.v, d.r, "a", a, d.wide, d.es, true, p.a, vo));
+    CHECK(d.v.all_bound, LASGD_ERR_STATE, "not every replica is bound");
+    TRY(check_device(c, d.v));
+    if (!d.r.most) return LASGD_OK;
+    weights(p, d, d.v.params, gate, up, cols);
+    launch_product<FWD>(d, p, vx, cols % 8 == 0, (hipStream_t)stream);
+    return launched(c);
+}
+
+extern "C" lasgd_status lasgd_gated_backward_bytes(lasgd_ctx *c, int32_t gate, int32_t up, const int64_t *rows, int64_t cols, int64_t *bytes)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    Gated d;
+    CHECK(bytes, LASGD_ERR_INVALID, "NULL bytes");
+    TRY(check_gated(c, d, gate, up, rows, cols));
+    *bytes = gated_bytes(d);
+    return LASGD_OK;
+}
+
+extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t up, const int64_t *rows, int64_t cols, const lasgd_rows *x,
+                                             const lasgd_rows *g, const lasgd_rows *u, const lasgd_rows *da, const lasgd_rows *dx,
+                                             lasgd_activation activation, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!c) return LASGD_ERR_INVALID;
+    Gated d;
+    TRY(check_gated(c, d, gate, up, rows, cols));
+    TRY(check_act(c, activation));
+    ProductArgs p = product_args(d, cols, activation);
+    GatesArgs e{};
+    RowsAt out{};
+    bool vx = true, vg = true, vo = true;
+    TRY(check_rows(c, d.v, d.r, "x", x, cols, d.es, false, p.x, vx));
+    TRY(check_rows(c, d.v, d.r, "g", g, d.wide, d.es, false, e.g, vg));
+    TRY(check_rows(c, d.v, d.r, "u", u, d.wide, d.es, false, e.u, vg));
+    TRY(check_rows(c, d.v, d.r, "da", da, d.wide, d.es, false, e.da, vg));
+    if (dx) TRY(check_rows(c, d.v, d.r, "dx", dx, cols, d.es, true, out, vo));
+    const int64_t need = gated_bytes(d);
+    TRY(check_workspace(c, workspace, workspace_bytes, need));
+    CHECK(d.v.all_bound, LASGD_ERR_STATE, "not every replica is bound");
+    TRY(check_device(c, d.v));
+    if (!d.r.most && accumulate) return LASGD_OK;
+    const hipStream_t st = (hipStream_t)stream;
+    e.dg = (char *)workspace;
+    e.du = e.dg + need / 2;
+    p.dg = e.dg;
+    p.du = e.du;
+    if (d.r.most) {
+        e.wide = (uint32_t)d.wide;
+        e.groups = ceil_div(d.wide, 8);
+        e.pitch = (uint32_t)d.pitch;
+        e.act = (int32_t)activation;
+        copy_rows(e, d.r, d.v.K);
+        memcpy(e.first, d.r.first, d.v.K * sizeof(uint32_t));
+        const dim3 grid(d.r.most < 4096u ? d.r.most : 4096u, d.v.K);
+        two_flags(d.v.bf16, vg, [&](auto bf16, auto wide) {
+            hipLaunchKernelGGL((gates_backward_kernel<bf16, wide>), grid, dim3(256), 0, st, e);
+        });
+        TRY(launched(c));
+    }
+    if (dx && d.r.most) {
+        ProductArgs q = p;
+        q.a = out;
+        weights(q, d, d.v.params, gate, up, cols);
+        launch_product<DX>(d, q, true, cols % 8 == 0, st);
+        TRY(launched(c));
+    }
+    p.accumulate = accumulate;
+    weights(p, d, d.v.grads, gate, up, cols);
+    launch_product<DW>(d, p, true, vx, st);
+    return launched(c);
+}

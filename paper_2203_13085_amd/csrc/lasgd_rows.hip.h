@@ -1,0 +1,445 @@
+// Row-wise operators of the replicas' forward and backward passes: device code of dropout and of root-mean-square norms.
+//
+// Bound by HBM: a handful of operations per element that is read or written once.  A dropout draw is ten rounds of two 32-bit
+// products for eight elements.
+#pragma once
+#include "lasgd_memory.hip.h"
+
+namespace lasgd {
+
+struct RowsAt {             // element (k, r, c) is at p + (k * rs + r * ss + c) elements
+    char *p;
+    int64_t rs, ss;
+};
+
+struct DropArgs {
+    uint64_t seed, call;
+    const uint64_t *counter;     // added to call, or NULL
+    uint32_t below;              // an element is dropped if its 16 bits are below this (0: no dropout; 65536: all are)
+    float scale;                 // of those that stay
+};
+
+// ---- Philox 4x32, ten rounds (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", SC 2011) ------------
+__device__ __forceinline__ uint4 philox(uint4 c, uint2 key)
+{
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t a = (uint64_t)c.x * 0xD2511F53u, b = (uint64_t)c.z * 0xCD9E8D57u;
+        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ key.x, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ key.y, (uint32_t)a);
+        key.x += 0x9E3779B9u;
+        key.y += 0xBB67AE85u;
+    }
+    return c;
+}
+
+// The mask of eight columns: one draw, 16 bits an element, the low half of a word first.  16 bits and not 32: the draws are what
+// a dropout pass would otherwise wait for (p is taken to the nearest 1/65536 and the scale is that number's, so means stay exact).
+// The counter names the place (replica, row, group of eight columns) and the call, so a mask does not depend on the launch shape, on the
+// layout, on how many replicas or rows there are, or on what ran before.
+struct Lots {
+    uint32_t w[4];
+};
+__device__ __forceinline__ Lots draw_lots(const DropArgs &d, uint64_t call, uint32_t k, uint64_t group)
+{
+    const uint4 w = philox(make_uint4((uint32_t)group, (uint32_t)(group >> 32) | k << 16, (uint32_t)call, (uint32_t)(call >> 32)),
+                           make_uint2((uint32_t)d.seed, (uint32_t)(d.seed >> 32)));
+    return Lots{{w.x, w.y, w.z, w.w}};
+}
+__device__ __forceinline__ bool stays(const Lots &l, int j, uint32_t below)
+{
+    const uint32_t lot = j & 1 ? l.w[j >> 1] >> 16 : l.w[j >> 1] & 0xffffu;
+    return lot >= below;
+}
+__device__ __forceinline__ uint64_t call_number(const DropArgs &d)
+{
+    return d.counter ? d.call + *as_global<uint64_t>(d.counter) : d.call;
+}
+
+// ---- eight elements ------------------------------------------------------------------------------------------------------
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float widen_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float widen_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Two to bf16, to nearest, ties to even.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t narrow2(float a, float b)
+{
+    bf16x2 r = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+template <bool BF16> __device__ __forceinline__ float load1(const char *p, int64_t i)
+{
+    if constexpr (BF16) return __uint_as_float((uint32_t)as_global<uint16_t>(p)[i] << 16);
+    else return as_global<float>(p)[i];
+}
+template <bool BF16> __device__ __forceinline__ void store1(char *p, int64_t i, float v)
+{
+    if constexpr (BF16) as_global<uint16_t>(p)[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
+    else as_global<float>(p)[i] = v;
+}
+
+// VEC: 16-byte accesses, and all eight are there; otherwise n of them are.
+template <bool BF16, bool VEC> __device__ __forceinline__ void load8(float (&v)[8], const char *p, int64_t at, uint32_t n)
+{
+    if constexpr (VEC && BF16) {
+        const u32x4 w = *as_global<u32x4>(p + at * 2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[2 * j] = widen_lo(w[j]), v[2 * j + 1] = widen_hi(w[j]);
+    } else if constexpr (VEC) {
+        const u32x4 a = *as_global<u32x4>(p + at * 4), b = *as_global<u32x4>(p + at * 4 + 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(a[j]), v[4 + j] = __uint_as_float(b[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (uint32_t)j < n ? load1<BF16>(p, at + j) : 0.f;
+    }
+}
+template <bool BF16, bool VEC> __device__ __forceinline__ void store8(char *p, int64_t at, uint32_t n, const float (&v)[8])
+{
+    if constexpr (VEC && BF16) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = narrow2(v[2 * j], v[2 * j + 1]);
+        *as_global<u32x4>(p + at * 2) = w;
+    } else if constexpr (VEC) {
+        u32x4 a, b;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(v[j]), b[j] = __float_as_uint(v[4 + j]);
+        *as_global<u32x4>(p + at * 4) = a;
+        *as_global<u32x4>(p + at * 4 + 16) = b;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if ((uint32_t)j < n) store1<BF16>(p, at + j, v[j]);
+    }
+}
+
+// ---- dropout ---------------------------------------------------------------------------------------------------------------
+//     y = residual + m x / (1 - p),      a dropped element counts 0 whatever it holds
+// A thread has eight columns of kDropRows rows at a time; a workgroup is tx threads along a row (a power of two) and 256 / tx rows.
+constexpr uint32_t kDropRows = 4;
+
+struct DropoutArgs {
+    RowsAt x, residual, y;       // residual.p NULL: none
+    DropArgs drop;
+    uint32_t cols, groups;       // groups of eight columns
+    uint32_t tx_shift;           // log2 of tx
+    uint32_t rows[64];
+};
+
+template <bool BF16, bool VEC>
+__global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a)
+{
+    const uint32_t k = blockIdx.y, rows = a.rows[k];
+    const uint32_t ty = 256u >> a.tx_shift;
+    const uint64_t r0 = (uint64_t)blockIdx.x * (ty * kDropRows);
+    if (r0 >= rows) return;
+    const uint32_t tx = threadIdx.x & ((1u << a.tx_shift) - 1u);
+    const uint64_t r1 = r0 + (threadIdx.x >> a.tx_shift);
+    const uint64_t call = call_number(a.drop);
+    for (uint32_t g = tx; g < a.groups; g += 1u << a.tx_shift) {
+        const uint32_t c = g * 8u, n = a.cols - c;
+        float x[kDropRows][8], res[kDropRows][8];
+#pragma unroll
+        for (uint32_t u = 0; u < kDropRows; ++u) {
+            const uint64_t r = r1 + u * ty;
+            if (r < rows) {
+                load8<BF16, VEC>(x[u], a.x.p, k * a.x.rs + (int64_t)r * a.x.ss + c, n);
+                if (a.residual.p) load8<BF16, VEC>(res[u], a.residual.p, k * a.residual.rs + (int64_t)r * a.residual.ss + c, n);
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kDropRows; ++u) {
+            const uint64_t r = r1 + u * ty;
+            if (r >= rows) break;
+            const Lots lots = draw_lots(a.drop, call, k, r * a.groups + g);
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                y[j] = stays(lots, j, a.drop.below) ? x[u][j] * a.drop.scale : 0.f;
+                if (a.residual.p) y[j] = res[u][j] + y[j];
+            }
+            store8<BF16, VEC>(a.y.p, k * a.y.rs + (int64_t)r * a.y.ss + c, n, y);
+        }
+    }
+}
+
+// ---- root-mean-square norm ----------------------------------------------------------------------------------------------------
+//     h = residual + m x / (1 - p),   rho = (mean h^2 + eps)^(-1/2),   y = gain (h rho)
+// G threads hold a row, NV groups of eight columns each, so everything is read once; h is rounded where it is stored, and enters the norm
+// as it was before.  In 8 bits: scale = max |y| / 448, at least the smallest normal number, and y / scale to e4m3.
+constexpr float kE4m3Max = 448.f;
+constexpr float kLeastScale = 1.17549435e-38f;
+
+struct NormRowsArgs {
+    RowsAt x, residual, sum, y, scales;
+    DropArgs drop;
+    uint32_t cols, groups;
+    float eps, inv_cols;
+    uint32_t rows[64];
+    const char *gain[64];
+};
+
+// Sum over the G threads of a row, the same in all of them.  lds: a word a wave.
+template <int G> __device__ __forceinline__ float row_sum(float v, float *lds)
+{
+#pragma unroll
+    for (int d = (G < 64 ? G : 64) / 2; d; d >>= 1) v += __shfl_xor(v, d, 64);
+    if constexpr (G > 64) {
+        __syncthreads();                 // the words of the sum before
+        if ((threadIdx.x & 63u) == 0u) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < G / 64; ++w) v += lds[w];
+    }
+    return v;
+}
+__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }      // a NaN stays
+template <int G> __device__ __forceinline__ float row_max(float v, float *lds)
+{
+#pragma unroll
+    for (int d = (G < 64 ? G : 64) / 2; d; d >>= 1) v = larger(v, __shfl_xor(v, d, 64));
+    if constexpr (G > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63u) == 0u) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = lds[0];
+#pragma unroll
+        for (int w = 1; w < G / 64; ++w) v = larger(v, lds[w]);
+    }
+    return v;
+}
+
+constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
+
+template <bool BF16, bool VEC, int G, int NV>
+__global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRowsArgs a)
+{
+    __shared__ float lds[G > 64 ? G / 64 : 1];
+    constexpr uint32_t R = norm_threads(G) / G;              // rows a workgroup
+    const uint32_t k = blockIdx.y, rows = a.rows[k];
+    const uint64_t r = (uint64_t)blockIdx.x * R + threadIdx.x / G;
+    if ((uint64_t)blockIdx.x * R >= rows) return;
+    if (G <= 64 && r >= rows) return;                        // (with G > 64 a workgroup is one row)
+    const uint32_t t = threadIdx.x % G;
+    const uint64_t call = a.drop.below ? call_number(a.drop) : 0;
+    const char *gain = a.gain[k];
+    float h[NV][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t g = t + i * G, c = g * 8u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[i][j] = 0.f;
+        if (g < a.groups) {
+            load8<BF16, VEC>(h[i], a.x.p, k * a.x.rs + (int64_t)r * a.x.ss + c, a.cols - c);
+        }
+    }
+    if (a.drop.below) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G;
+            if (g < a.groups) {
+                const Lots lots = draw_lots(a.drop, call, k, r * a.groups + g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] = stays(lots, j, a.drop.below) ? h[i][j] * a.drop.scale : 0.f;
+            }
+        }
+    }
+    if (a.residual.p) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G, c = g * 8u;
+            if (g < a.groups) {
+                float res[8];
+                load8<BF16, VEC>(res, a.residual.p, k * a.residual.rs + (int64_t)r * a.residual.ss + c, a.cols - c);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] = res[j] + h[i][j];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(h[i][j], h[i][j], sum);
+    }
+    if (a.sum.p) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G, c = g * 8u;
+            if (g < a.groups) store8<BF16, VEC>(a.sum.p, k * a.sum.rs + (int64_t)r * a.sum.ss + c, a.cols - c, h[i]);
+        }
+    }
+    sum = row_sum<G>(sum, lds);
+    const float rho = 1.f / __builtin_sqrtf(__builtin_fmaf(sum, a.inv_cols, a.eps));
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t g = t + i * G, c = g * 8u;
+        if (g < a.groups) {
+            float w[8];
+            load8<BF16, VEC>(w, gain, c, a.cols - c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                h[i][j] = w[j] * (h[i][j] * rho);
+                most = larger(most, __builtin_fabsf(h[i][j]));
+            }
+            if (!a.scales.p) store8<BF16, VEC>(a.y.p, k * a.y.rs + (int64_t)r * a.y.ss + c, a.cols - c, h[i]);
+        }
+    }
+    if (!a.scales.p) return;
+    most = row_max<G>(most, lds);
+    float scale = most / kE4m3Max;
+    if (scale < kLeastScale) scale = kLeastScale;
+    const float inv = 1.f / scale;
+    if (t == 0u) as_global<float>(a.scales.p)[k * a.scales.rs + (int64_t)r * a.scales.ss] = scale;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t g = t + i * G, c = g * 8u;
+        if (g < a.groups) {
+            uint32_t q[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                int w = 0;
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][4 * j] * inv, h[i][4 * j + 1] * inv, w, false);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][4 * j + 2] * inv, h[i][4 * j + 3] * inv, w, true);
+                q[j] = (uint32_t)w;
+            }
+            char *y = a.y.p + (k * a.y.rs + (int64_t)r * a.y.ss + c);
+            if constexpr (VEC) *as_global<u32x2>(y) = u32x2{q[0], q[1]};
+            else {
+#pragma unroll
+                for (uint32_t j = 0; j < 8u; ++j)
+                    if (c + j < a.cols) *as_global<uint8_t>(y + j) = (uint8_t)(q[j >> 2] >> (8u * (j & 3u)));
+            }
+        }
+    }
+}
+
+// The backward pass, with hhat = h rho:
+//     dh = rho (gain dy - hhat mean(hhat gain dy)) + dsum,   dx = m dh / (1 - p),   dgain = sum over the rows of dy hhat
+// rho is made again from h, which is read anyway.  A workgroup takes rows one after the other and adds up its share of dgain
+// in registers; the shares of a replica's workgroups go to the workspace and are added in their order by join_gain_kernel.
+struct NormBackArgs {
+    RowsAt h, dy, dsum, dresidual, dx;       // dsum, dresidual, dx: may be NULL
+    DropArgs drop;
+    uint32_t cols, groups;
+    float eps, inv_cols;
+    uint32_t parts;              // workgroups a replica
+    float *part;                 // [K][parts * rows a workgroup][groups * 8]
+    uint32_t rows[64];
+    const char *gain[64];
+};
+
+template <bool BF16, bool VEC, int G, int NV>
+__global__ __launch_bounds__(norm_threads(G)) void rms_norm_backward_kernel(const NormBackArgs a)
+{
+    __shared__ float lds[G > 64 ? G / 64 : 1];
+    constexpr uint32_t R = norm_threads(G) / G;
+    const uint32_t k = blockIdx.y, rows = a.rows[k];
+    const uint32_t t = threadIdx.x % G, lane_row = threadIdx.x / G;
+    const uint64_t call = a.drop.below ? call_number(a.drop) : 0;
+    const char *gain = a.gain[k];
+    float acc[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+    }
+    for (uint64_t r = (uint64_t)blockIdx.x * R + lane_row; r < rows; r += (uint64_t)a.parts * R) {
+        float h[NV][8], d[NV][8];
+        float sum = 0.f, dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G, c = g * 8u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[i][j] = d[i][j] = 0.f;
+            if (g < a.groups) {
+                load8<BF16, VEC>(h[i], a.h.p, k * a.h.rs + (int64_t)r * a.h.ss + c, a.cols - c);
+                load8<BF16, VEC>(d[i], a.dy.p, k * a.dy.rs + (int64_t)r * a.dy.ss + c, a.cols - c);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G, c = g * 8u;
+            if (g < a.groups) {
+                float w[8];
+                load8<BF16, VEC>(w, gain, c, a.cols - c);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    sum = __builtin_fmaf(h[i][j], h[i][j], sum);
+                    dot = __builtin_fmaf(h[i][j], w[j] * d[i][j], dot);
+                }
+            }
+        }
+        sum = row_sum<G>(sum, lds);
+        dot = row_sum<G>(dot, lds);
+        const float rho = 1.f / __builtin_sqrtf(__builtin_fmaf(sum, a.inv_cols, a.eps));
+        const float mean = dot * rho * a.inv_cols;           // of hhat gain dy
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G, c = g * 8u;
+            if (g < a.groups) {
+                float w[8], more[8];
+                load8<BF16, VEC>(w, gain, c, a.cols - c);
+                if (a.dsum.p) load8<BF16, VEC>(more, a.dsum.p, k * a.dsum.rs + (int64_t)r * a.dsum.ss + c, a.cols - c);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float hat = h[i][j] * rho;
+                    acc[i][j] = __builtin_fmaf(d[i][j], hat, acc[i][j]);
+                    d[i][j] = rho * __builtin_fmaf(-hat, mean, w[j] * d[i][j]);
+                    if (a.dsum.p) d[i][j] += more[j];
+                }
+                if (a.dresidual.p) store8<BF16, VEC>(a.dresidual.p, k * a.dresidual.rs + (int64_t)r * a.dresidual.ss + c, a.cols - c, d[i]);
+                if (a.dx.p) {
+                    if (a.drop.below) {
+                        const Lots lots = draw_lots(a.drop, call, k, r * a.groups + g);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) d[i][j] = stays(lots, j, a.drop.below) ? d[i][j] * a.drop.scale : 0.f;
+                    }
+                    store8<BF16, VEC>(a.dx.p, k * a.dx.rs + (int64_t)r * a.dx.ss + c, a.cols - c, d[i]);
+                }
+            }
+        }
+    }
+    const uint64_t part = ((uint64_t)k * a.parts + blockIdx.x) * R + lane_row;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t g = t + i * G;
+        if (g < a.groups) store8<false, true>(reinterpret_cast<char *>(a.part), (int64_t)(part * a.groups + g) * 8, 8u, acc[i]);
+    }
+}
+
+struct JoinArgs {
+    const float *part;           // [K][shares][groups * 8]
+    uint32_t shares, cols, groups;
+    int32_t accumulate;
+    char *grad[64];
+};
+
+// The shares of a column, added in their order: 16 threads, one share in 16 each, and then those.
+template <bool BF16>
+__global__ __launch_bounds__(256) void join_gain_kernel(const JoinArgs a)
+{
+    __shared__ float lds[16][17];
+    const uint32_t k = blockIdx.y, x = threadIdx.x & 15u, y = threadIdx.x >> 4;
+    const uint32_t c = blockIdx.x * 16u + x;
+    float sum = 0.f;
+    if (c < a.cols)
+        for (uint32_t s = y; s < a.shares; s += 16u) sum += as_global<float>(a.part)[((uint64_t)k * a.shares + s) * (a.groups * 8u) + c];
+    lds[y][x] = sum;
+    __syncthreads();
+    if (y == 0u && c < a.cols) {
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += lds[i][x];
+        if (a.accumulate) sum += load1<BF16>(a.grad[k], c);
+        store1<BF16>(a.grad[k], c, sum);
+    }
+}
+
+} // namespace lasgd
