@@ -80,6 +80,7 @@ struct ProductArgs {
     const char *dg, *du;         // DX, DW: [rows of all replicas][pitch]
     uint32_t cols, wide, pitch;
     int32_t act, accumulate;
+    int32_t wide_out;            // outputs take accesses of eight elements
     uint32_t rows[64];
     uint32_t first[64];
     char *gate[64], *up[64];     // the weights; DW: their gradients
@@ -217,6 +218,250 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
                 }
             }
         }
+    }
+}
+
+// ---- bf16, aligned, more rows than a few ------------------------------------------------------------------------------------------
+// Bound by the matrix cores.  A workgroup makes TM x TN of C, wave by wave, and takes the contraction kStep at a time through two buffers
+// in LDS: while the waves multiply one, the next is on its way from memory straight into the other.
+//   - A side whose contraction is contiguous in memory (ALONG) lies in LDS as [row][8 pieces of 16 bytes], piece p of row i at p ^ (i & 7), and is read 16
+//     bytes a lane: eight rows' equal pieces are in eight different places of 128 bytes.
+//   - A side whose rows are contiguous (ACROSS) lies as [contraction][T / 8 pieces], piece p of line c at p ^ 2 (c & 3), and is read by the transposing
+//     read: 16 lanes take 4 lines of 16 columns, and a lane gets one column of them.
+// What is outside is asked for beyond the end of a buffer resource, which gives zeros.
+constexpr uint32_t kStep = 64;
+
+// A tile's place and how far what may be read reaches from there: T lines along, or kStep lines across.
+struct Side {
+    const char *p;               // of the tile's first element
+    int64_t bytes;               // from there to the end of what is there
+    int64_t stride;              // bytes from one line to the next
+};
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ uint32_t records(int64_t bytes) { return bytes <= 0 ? 0u : bytes > 0xfffffff0ll ? 0xfffffff0u : (uint32_t)bytes; }
+
+// The next kStep of the contraction into LDS.  left: how much of it is still there (ALONG: beyond it the line goes on with something else).
+template <bool ALONG, uint32_t T, uint32_t THREADS>
+__device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left)
+{
+    constexpr uint32_t PIECES = T * kStep / 8u, LINE = ALONG ? kStep / 8u : T / 8u;
+    static_assert(PIECES % THREADS == 0, "whole rounds");
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)s.p, 0, records(s.bytes), 0x00020000);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (uint32_t i = 0; i < PIECES / THREADS; ++i) {
+        const uint32_t at = i * THREADS + threadIdx.x, line = at / LINE;
+        const uint32_t piece = at % LINE ^ (ALONG ? line & 7u : (line & 3u) * 2u);
+        uint32_t off = line * (uint32_t)s.stride + piece * 16u;
+        if (ALONG && (int64_t)(piece * 8u) >= left) off = 0xfffffff0u;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64u) * 16u), 16, off, 0, 0, 0);
+    }
+}
+
+// The 16 rows from row0 on, 32 of the contraction from c0 on: a lane has row lane % 16 and eight of the contraction, 8 (lane / 16) on.
+template <bool ALONG, uint32_t T>
+__device__ __forceinline__ bf16x8 fragment(const lds_char *lds, uint32_t row0, uint32_t c0)
+{
+    const uint32_t lane = threadIdx.x & 63u, quad = lane >> 4, i = lane & 15u;
+    if constexpr (ALONG) {
+        const uint32_t row = row0 + i, piece = (c0 / 8u + quad) ^ (row & 7u);
+        return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds + row * (kStep * 2u) + piece * 16u);
+    } else {
+        const uint32_t line = c0 + quad * 8u + (i >> 2), piece = (row0 / 8u + ((i & 3u) >> 1)) ^ ((line & 3u) * 2u);
+        const lds_char *at = lds + line * (T * 2u) + piece * 16u + (i & 1u) * 8u;            // four lines on: the same place in its line
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4u * T * 2u));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+}
+
+template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN> struct Big {
+    static constexpr uint32_t threads = 64u * WM * WN;
+    static constexpr bool along_m = FORM != DW, along_n = FORM == FWD;
+    static constexpr uint32_t FM = TM / WM / 16u, FN = TN / WN / 16u;           // fragments of a wave
+    static constexpr uint32_t bytes = (TM + TN) * kStep * 2u;                  // of a buffer
+    static constexpr uint32_t cols_out = TN / WN / (FORM == FWD ? 2u : 1u);    // columns of C that a wave has
+    static constexpr uint32_t part_rows = FM > 4u ? 64u : FM * 16u, part_pitch = TN / WN + 4u;     // of it, on its way out, in fp32
+    static constexpr uint32_t out_bytes = WM * WN * part_rows * part_pitch * 4u;
+    static constexpr uint32_t lds = 2u * bytes > out_bytes ? 2u * bytes : out_bytes;
+
+    static __device__ __forceinline__ void fetch_both(lds_char *lds, const Side &m, const Side &n, const Side &n2, int64_t left)
+    {
+        fetch<along_m, TM, threads>(lds, m, left);
+        if constexpr (FORM == FWD) {
+            fetch<true, TN / 2u, threads>(lds + TM * kStep * 2u, n, left);
+            fetch<true, TN / 2u, threads>(lds + (TM + TN / 2u) * kStep * 2u, n2, left);
+        } else fetch<along_n, TN, threads>(lds + TM * kStep * 2u, n, left);
+    }
+    // row of the n side's fragment j: a wave of FWD has the same columns of gate and up
+    static __device__ __forceinline__ uint32_t n_row(uint32_t wn, uint32_t j)
+    {
+        if constexpr (FORM == FWD) return (j >= FN / 2u ? TN / 2u + (j - FN / 2u) * 16u : j * 16u) + wn * (TN / WN / 2u);
+        else return wn * (TN / WN) + j * 16u;
+    }
+    static __device__ __forceinline__ void multiply(f32x4 (&acc)[FM][FN], const lds_char *lds, uint32_t wm, uint32_t wn)
+    {
+#pragma unroll
+        for (uint32_t c = 0; c < kStep; c += 32u) {
+            bf16x8 m[FM], n[FN];
+#pragma unroll
+            for (uint32_t j = 0; j < FN; ++j) n[j] = fragment<along_n, TN>(lds + TM * kStep * 2u, n_row(wn, j), c);
+#pragma unroll
+            for (uint32_t i = 0; i < FM; ++i) m[i] = fragment<along_m, TM>(lds, wm * (TM / WM) + i * 16u, c);
+#pragma unroll
+            for (uint32_t i = 0; i < FM; ++i) {
+#pragma unroll
+                for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m[i], acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+    // cur is read while next is written: told apart by restrict, or every read would wait for the loads into next.
+    static __device__ __forceinline__ void step(f32x4 (&acc)[FM][FN], const lds_char *__restrict__ cur, lds_char *__restrict__ next, const Side &m,
+                                                const Side &n, const Side &n2, int64_t left, bool more, uint32_t wm, uint32_t wn)
+    {
+        if (more) fetch_both(next, m, n, n2, left);
+        multiply(acc, cur, wm, wn);
+    }
+};
+
+// Eight elements of bf16 or, where they may not be stored at once, as many as there are.
+__device__ __forceinline__ void store_some(char *p, int64_t at, bool at_once, uint32_t there, const float (&v)[8])
+{
+    if (at_once) store8<true, true>(p, at, 8u, v);
+    else store8<true, false>(p, at, there, v);
+}
+
+struct TileMap {
+    uint32_t first[65];          // tiles of the replicas before, and of all
+    uint32_t replicas;
+};
+
+// Workgroups are dealt out to the eight XCDs in turn; each XCD gets tiles that follow each other, which share their sides in its L2.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total)
+{
+    const uint32_t x = id & 7u, per = total >> 3, more = total & 7u;
+    return x * per + (x < more ? x : more) + (id >> 3);
+}
+
+template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN>
+__global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)
+{
+    using S = Big<FORM, TM, TN, WM, WN>;
+    __shared__ __attribute__((aligned(1024))) char lds_mem[S::lds];
+    lds_char *lds = (lds_char *)lds_mem;
+    const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
+    uint32_t k = 0;
+    for (uint32_t half = 32u; half; half >>= 1)
+        if (k + half < map.replicas && map.first[k + half] <= id) k += half;
+    uint32_t tile = id - map.first[k];
+    const uint32_t rows = a.rows[k], cols = a.cols, wide = a.wide;
+    const uint32_t M = FORM == DW ? wide : rows, N = FORM == FWD ? wide : cols;
+    const uint32_t tm = (M + TM - 1u) / TM;
+    const bool second = FORM == DW && tile >= tm * ((N + TN - 1u) / TN);         // DW: first all of the gate's gradient, then up's
+    if (second) tile -= tm * ((N + TN - 1u) / TN);
+    constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;                          // columns of C
+    const int64_t m0 = (int64_t)(tile % tm) * TM, n0 = (int64_t)(tile / tm) * NT;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WN, wn = w % WN;
+    const int64_t pitch = (int64_t)a.pitch * 2, width = (int64_t)cols * 2, xs = a.x.ss * 2;
+    const uint64_t first = (uint64_t)a.first[k] * pitch;
+    const char *x = a.x.p + k * a.x.rs * 2;
+    Side m, n, n2;
+    int64_t deep;
+    if constexpr (FORM == FWD) {
+        deep = cols;
+        m = Side{x + m0 * xs, (rows - 1 - m0) * xs + width, xs};
+        n = Side{a.gate[k] + n0 * width, (wide - n0) * width, width};
+        n2 = Side{a.up[k] + n0 * width, (wide - n0) * width, width};
+    } else if constexpr (FORM == DX) {
+        deep = a.pitch;
+        m = Side{a.dg + first + m0 * pitch, (rows - m0) * pitch, pitch};
+        n = Side{a.gate[k] + n0 * 2, wide * width - n0 * 2, width};
+        n2 = n;
+    } else {
+        deep = rows;
+        m = Side{(second ? a.du : a.dg) + first + m0 * 2, rows * pitch - m0 * 2, pitch};
+        n = Side{x + n0 * 2, (rows - 1) * xs + width - n0 * 2, xs};
+        n2 = n;
+    }
+    const uint32_t steps1 = (uint32_t)((deep + kStep - 1) / kStep), steps = FORM == DX ? 2u * steps1 : steps1;
+    const Side m_again = m, n_again = n;
+    f32x4 acc[S::FM][S::FN] = {};
+    int64_t left = deep;
+    auto advance = [&](uint32_t next) {
+        const int64_t am = S::along_m ? kStep * 2 : kStep * m.stride, an = S::along_n ? kStep * 2 : kStep * n.stride;
+        m.p += am, m.bytes -= am;
+        n.p += an, n.bytes -= an;
+        n2.p += an, n2.bytes -= an;
+        left -= kStep;
+        if (FORM == DX && next == steps1) {          // the second pair
+            m = m_again, n = n_again;
+            m.p += a.du - a.dg;
+            n.p += a.up[k] - a.gate[k];
+            left = deep;
+        }
+    };
+    if (steps) S::fetch_both(lds, m, n, n2, left);
+    for (uint32_t s = 0; s < steps; ++s) {
+        advance(s + 1u);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        lds_char *cur = lds + (s & 1u) * S::bytes, *next = lds + (~s & 1u) * S::bytes;
+        S::step(acc, cur, next, m, n, n2, left, s + 1u < steps, wm, wn);
+    }
+    // C through LDS, each wave in a part of its own, so that a lane has eight columns next to each other and the activation's code is there once.
+    __syncthreads();
+    float *mine = reinterpret_cast<float *>(lds_mem) + w * (S::part_rows * S::part_pitch);
+    const uint32_t lane = threadIdx.x & 63u;
+    constexpr uint32_t LANES = S::cols_out / 8u, ROWS = 64u / LANES;              // lanes a row, rows at a time
+#pragma unroll
+    for (uint32_t i0 = 0; i0 < S::FM; i0 += S::part_rows / 16u) {
+#pragma unroll
+        for (uint32_t i = 0; i < S::part_rows / 16u; ++i) {
+#pragma unroll
+            for (uint32_t j = 0; j < S::FN; ++j)
+                *reinterpret_cast<f32x4 *>(mine + (i * 16u + (lane & 15u)) * S::part_pitch + j * 16u + (lane >> 4) * 4u) = acc[i0 + i][j];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int64_t row0 = m0 + wm * (TM / WM) + i0 * 16u, col = n0 + wn * S::cols_out + lane % LANES * 8u;
+#pragma unroll 1
+        for (uint32_t r = lane / LANES; r < S::part_rows; r += ROWS) {
+            const int64_t row = row0 + r;
+            if (row >= M || col >= N) break;
+            const float *from = mine + r * S::part_pitch + lane % LANES * 8u;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = from[e];
+            const uint32_t there = (uint32_t)(N - col < 8 ? N - col : 8);
+            const bool at_once = a.wide_out && there == 8u;
+            if constexpr (FORM == FWD) {
+                float u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = from[S::cols_out + e];
+                if (a.g.p) {
+                    store_some(a.g.p, k * a.g.rs + row * a.g.ss + col, at_once, there, v);
+                    store_some(a.u.p, k * a.u.rs + row * a.u.ss + col, at_once, there, u);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = activation(a.act, v[e]).f * u[e];
+                store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
+            } else if constexpr (FORM == DX) {
+                store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
+            } else {                                  // cols counts whole eights
+                char *grad = second ? a.up[k] : a.gate[k];
+                if (a.accumulate) {
+                    float old[8];
+                    load8<true, true>(old, grad, row * cols + col, 8u);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += old[e];
+                }
+                store8<true, true>(grad, row * cols + col, 8u, v);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 

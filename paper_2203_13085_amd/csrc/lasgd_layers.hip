@@ -380,6 +380,35 @@ template <int FORM> void launch_product(const Gated &d, const ProductArgs &a, bo
     });
 }
 
+// Whether a product's sides can go straight from memory into LDS: bf16, 16-byte pieces, a tile's lines within 32 bits of bytes.
+bool streams(const Gated &d, int64_t cols, const RowsAt &x, bool vx)
+{
+    constexpr int64_t most = (1ll << 31) / 256 / 2;          // elements from one line to the next
+    return d.v.bf16 && vx && cols <= most && d.pitch <= most && x.ss <= most && d.r.most >= 32u;
+}
+
+template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN>
+void launch_big(const Gated &d, const ProductArgs &a, hipStream_t st)
+{
+    constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;
+    TileMap map{};
+    map.replicas = (uint32_t)d.v.K;
+    uint32_t total = 0;
+    for (int32_t k = 0; k < d.v.K; ++k) {
+        map.first[k] = total;
+        const uint32_t tm = ceil_div(FORM == DW ? a.wide : d.r.n[k], TM);
+        total += tm * ceil_div(FORM == FWD ? a.wide : a.cols, NT) * (FORM == DW ? 2u : 1u);
+    }
+    map.first[d.v.K] = total;
+    hipLaunchKernelGGL((big_product_kernel<FORM, TM, TN, WM, WN>), dim3(total), dim3(Big<FORM, TM, TN, WM, WN>::threads), 0, st, a, map);
+}
+
+template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, hipStream_t st)
+{
+    if (big) launch_big<FORM, 256, 256, 2, 4>(d, a, st);
+    else launch_product<FORM>(d, a, vm, vn, st);
+}
+
 int64_t gated_bytes(const Gated &d) { return 2 * (int64_t)d.r.total * d.pitch * d.es; }
 
 } // namespace
@@ -404,7 +433,8 @@ extern "C" lasgd_status lasgd_gated(lasgd_ctx *c, int32_t gate, int32_t up, cons
     TRY(check_device(c, d.v));
     if (!d.r.most) return LASGD_OK;
     weights(p, d, d.v.params, gate, up, cols);
-    launch_product<FWD>(d, p, vx, cols % 8 == 0, (hipStream_t)stream);
+    p.wide_out = vo;
+    launch_form<FWD>(d, p, streams(d, cols, p.x, vx), vx, cols % 8 == 0, (hipStream_t)stream);
     return launched(c);
 }
 
@@ -458,15 +488,17 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
         });
         TRY(launched(c));
     }
+    const bool big = streams(d, cols, p.x, vx);
     if (dx && d.r.most) {
         ProductArgs q = p;
         q.a = out;
         weights(q, d, d.v.params, gate, up, cols);
-        launch_product<DX>(d, q, true, cols % 8 == 0, st);
+        q.wide_out = vo;
+        launch_form<DX>(d, q, big, true, cols % 8 == 0, st);
         TRY(launched(c));
     }
     p.accumulate = accumulate;
     weights(p, d, d.v.grads, gate, up, cols);
-    launch_product<DW>(d, p, true, vx, st);
+    launch_form<DW>(d, p, big, true, vx, st);
     return launched(c);
 }
