@@ -249,11 +249,12 @@ template <bool ALONG, uint32_t T, uint32_t THREADS>
 __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left)
 {
     constexpr uint32_t PIECES = T * kStep / 8u, LINE = ALONG ? kStep / 8u : T / 8u;
-    static_assert(PIECES % THREADS == 0, "whole rounds");
+    static_assert(PIECES % 64u == 0, "whole waves");
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)s.p, 0, records(s.bytes), 0x00020000);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (uint32_t i = 0; i < PIECES / THREADS; ++i) {
+    for (uint32_t i = 0; i < (PIECES + THREADS - 1u) / THREADS; ++i) {
+        if ((i + 1u) * THREADS > PIECES && i * THREADS + wave * 64u >= PIECES) break;
         const uint32_t at = i * THREADS + threadIdx.x, line = at / LINE;
         const uint32_t piece = at % LINE ^ (ALONG ? line & 7u : (line & 3u) * 2u);
         uint32_t off = line * (uint32_t)s.stride + piece * 16u;
@@ -338,6 +339,9 @@ __device__ __forceinline__ void store_some(char *p, int64_t at, bool at_once, ui
 struct TileMap {
     uint32_t first[65];          // tiles of the replicas before, and of all
     uint32_t replicas;
+    uint32_t splits;             // workgroups that share a tile's contraction (DX)
+    float *part;                 // more than one: what each of them has, [splits][rows of all replicas][cols]
+    uint64_t part_stride;        // elements from one split to the next
 };
 
 // Workgroups are dealt out to the eight XCDs in turn; each XCD gets tiles that follow each other, which share their sides in its L2.
@@ -353,7 +357,8 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN>::threads)) void big_prod
     using S = Big<FORM, TM, TN, WM, WN>;
     __shared__ __attribute__((aligned(1024))) char lds_mem[S::lds];
     lds_char *lds = (lds_char *)lds_mem;
-    const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
+    const uint32_t order = xcd_order(blockIdx.x, gridDim.x);
+    const uint32_t id = FORM == DX ? order / map.splits : order, split = FORM == DX ? order % map.splits : 0u;
     uint32_t k = 0;
     for (uint32_t half = 32u; half; half >>= 1)
         if (k + half < map.replicas && map.first[k + half] <= id) k += half;
@@ -387,30 +392,27 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN>::threads)) void big_prod
         n = Side{x + n0 * 2, (rows - 1) * xs + width - n0 * 2, xs};
         n2 = n;
     }
-    const uint32_t steps1 = (uint32_t)((deep + kStep - 1) / kStep), steps = FORM == DX ? 2u * steps1 : steps1;
-    const Side m_again = m, n_again = n;
+    const uint32_t steps1 = (uint32_t)((deep + kStep - 1) / kStep), all = FORM == DX ? 2u * steps1 : steps1;
+    const uint32_t begin = FORM == DX ? (uint32_t)((uint64_t)all * split / map.splits) : 0u;
+    const uint32_t end = FORM == DX ? (uint32_t)((uint64_t)all * (split + 1u) / map.splits) : all;
+    const int64_t to_du = FORM == DX ? a.du - a.dg : 0, to_up = FORM == DX ? a.up[k] - a.gate[k] : 0;
     f32x4 acc[S::FM][S::FN] = {};
-    int64_t left = deep;
-    auto advance = [&](uint32_t next) {
-        const int64_t am = S::along_m ? kStep * 2 : kStep * m.stride, an = S::along_n ? kStep * 2 : kStep * n.stride;
-        m.p += am, m.bytes -= am;
-        n.p += an, n.bytes -= an;
-        n2.p += an, n2.bytes -= an;
-        left -= kStep;
-        if (FORM == DX && next == steps1) {          // the second pair
-            m = m_again, n = n_again;
-            m.p += a.du - a.dg;
-            n.p += a.up[k] - a.gate[k];
-            left = deep;
-        }
+    // step s's sides: DX goes through the first pair and then through the second
+    auto side = [&](const Side &from, bool along, uint32_t s, int64_t to_second) {
+        Side at = from;
+        const int64_t on = (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * (along ? kStep * 2 : kStep * from.stride);
+        at.p += on + (FORM == DX && s >= steps1 ? to_second : 0);
+        at.bytes -= on;
+        return at;
     };
-    if (steps) S::fetch_both(lds, m, n, n2, left);
-    for (uint32_t s = 0; s < steps; ++s) {
-        advance(s + 1u);
+    auto left = [&](uint32_t s) { return deep - (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * kStep; };
+    if (begin < end) S::fetch_both(lds, side(m, S::along_m, begin, to_du), side(n, S::along_n, begin, to_up), side(n2, S::along_n, begin, 0), left(begin));
+    for (uint32_t s = begin; s < end; ++s) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        lds_char *cur = lds + (s & 1u) * S::bytes, *next = lds + (~s & 1u) * S::bytes;
-        S::step(acc, cur, next, m, n, n2, left, s + 1u < steps, wm, wn);
+        lds_char *cur = lds + ((s - begin) & 1u) * S::bytes, *next = lds + (~(s - begin) & 1u) * S::bytes;
+        S::step(acc, cur, next, side(m, S::along_m, s + 1u, to_du), side(n, S::along_n, s + 1u, to_up), side(n2, S::along_n, s + 1u, 0), left(s + 1u),
+                s + 1u < end, wm, wn);
     }
     // C through LDS, each wave in a part of its own, so that a lane has eight columns next to each other and the activation's code is there once.
     __syncthreads();
@@ -449,7 +451,8 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN>::threads)) void big_prod
                 for (int e = 0; e < 8; ++e) v[e] = activation(a.act, v[e]).f * u[e];
                 store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
             } else if constexpr (FORM == DX) {
-                store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
+                if (map.splits > 1u) store8<false, true>((char *)(map.part + split * map.part_stride), (int64_t)(a.first[k] + row) * cols + col, 8u, v);
+                else store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
             } else {                                  // cols counts whole eights
                 char *grad = second ? a.up[k] : a.gate[k];
                 if (a.accumulate) {
@@ -462,6 +465,101 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN>::threads)) void big_prod
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// dx from the parts of a contraction that several workgroups shared, added in their order.
+struct JoinRowsArgs {
+    RowsAt a;
+    const float *part;
+    uint64_t part_stride;
+    uint32_t splits, cols;       // cols counts whole eights
+    int32_t wide_out;
+    uint32_t rows[64];
+    uint32_t first[64];
+};
+template <int = 0>
+__global__ __launch_bounds__(256) void join_rows_kernel(const JoinRowsArgs a)
+{
+    const uint32_t k = blockIdx.y, rows = a.rows[k], groups = a.cols / 8u;
+    for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (uint32_t g = threadIdx.x; g < groups; g += 256u) {
+            float sum[8], v[8];
+            const char *from = (const char *)a.part;
+            const int64_t at = (int64_t)(a.first[k] + r) * a.cols + g * 8u;
+            load8<false, true>(sum, from, at, 8u);
+#pragma unroll 4
+            for (uint32_t s = 1; s < a.splits; ++s) {
+                load8<false, true>(v, from, at + (int64_t)(s * a.part_stride), 8u);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += v[e];
+            }
+            store_some(a.a.p, k * a.a.rs + (int64_t)r * a.a.ss + g * 8u, a.wide_out, 8u, sum);
+        }
+}
+
+// ---- bf16, aligned, a few rows ------------------------------------------------------------------------------------------------------
+// FWD, bound by the weights' bytes.  A workgroup has 16 columns of gate and of up and all of a replica's rows, up to 16 FM; its four waves share
+// the contraction, take the weights straight from memory into registers, and are added up in LDS.
+template <uint32_t FM>
+__global__ __launch_bounds__(256) void few_rows_kernel(const ProductArgs a)
+{
+    constexpr uint32_t U = FM == 1u ? 4u : 2u;                  // of 32 of the contraction, asked for together
+    __shared__ float part[4][2][FM * 16u][17];
+    const uint32_t k = blockIdx.y, rows = a.rows[k], cols = a.cols, wide = a.wide;
+    if (!rows) return;
+    const uint32_t n0 = blockIdx.x * 16u, w = threadIdx.x >> 6, lane = threadIdx.x & 63u, i = lane & 15u, quad = lane >> 4;
+    const bool there = n0 + i < wide;
+    const char *gate = a.gate[k] + ((uint64_t)(there ? n0 + i : 0u) * cols + quad * 8u) * 2u, *up = a.up[k] + ((uint64_t)(there ? n0 + i : 0u) * cols + quad * 8u) * 2u;
+    const char *x[FM];
+#pragma unroll
+    for (uint32_t f = 0; f < FM; ++f) x[f] = a.x.p + (k * a.x.rs + (int64_t)(f * 16u + i < rows ? f * 16u + i : 0u) * a.x.ss + quad * 8u) * 2;
+    f32x4 g[FM] = {}, u[FM] = {};
+    for (uint32_t c0 = w * 32u; c0 < cols; c0 += U * 128u) {
+        u32x4 wg[U], wu[U], m[U][FM];
+#pragma unroll
+        for (uint32_t t = 0; t < U; ++t) {
+            const uint32_t c = c0 + t * 128u;
+            wg[t] = wu[t] = u32x4{};
+#pragma unroll
+            for (uint32_t f = 0; f < FM; ++f) m[t][f] = u32x4{};
+            if (c + quad * 8u < cols) {
+                wg[t] = __builtin_nontemporal_load(as_global<u32x4>(gate + c * 2u));
+                wu[t] = __builtin_nontemporal_load(as_global<u32x4>(up + c * 2u));
+#pragma unroll
+                for (uint32_t f = 0; f < FM; ++f) m[t][f] = *as_global<u32x4>(x[f] + c * 2u);
+            }
+        }
+#pragma unroll
+        for (uint32_t t = 0; t < U; ++t) {
+#pragma unroll
+            for (uint32_t f = 0; f < FM; ++f) {
+                const bf16x8 v = __builtin_bit_cast(bf16x8, m[t][f]);
+                g[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wg[t]), v, g[f], 0, 0, 0);
+                u[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wu[t]), v, u[f], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (uint32_t f = 0; f < FM; ++f) {
+#pragma unroll
+        for (uint32_t e = 0; e < 4u; ++e) {
+            part[w][0][f * 16u + i][quad * 4u + e] = g[f][e];
+            part[w][1][f * 16u + i][quad * 4u + e] = u[f][e];
+        }
+    }
+    __syncthreads();
+    const uint32_t n = threadIdx.x & 15u;
+    if (n0 + n >= wide) return;
+    for (uint32_t r = threadIdx.x >> 4; r < rows; r += 16u) {
+        float gv = 0.f, uv = 0.f;
+#pragma unroll
+        for (uint32_t v = 0; v < 4u; ++v) gv += part[v][0][r][n], uv += part[v][1][r][n];
+        store1<true>(a.a.p, k * a.a.rs + (int64_t)r * a.a.ss + n0 + n, activation(a.act, gv).f * uv);
+        if (a.g.p) {
+            store1<true>(a.g.p, k * a.g.rs + (int64_t)r * a.g.ss + n0 + n, gv);
+            store1<true>(a.u.p, k * a.u.rs + (int64_t)r * a.u.ss + n0 + n, uv);
+        }
     }
 }
 

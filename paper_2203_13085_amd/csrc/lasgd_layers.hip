@@ -120,6 +120,8 @@ lasgd_status launched(lasgd_ctx *c)
 
 template <class T> void copy_rows(T &a, const Rows &r, int32_t K) { memcpy(a.rows, r.n, K * sizeof(uint32_t)); }
 
+uint64_t round_up16(uint64_t n) { return (n + 15) / 16 * 16; }
+
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
 // f(std::integral_constant<bool, ...>...) for two flags.
@@ -384,15 +386,46 @@ template <int FORM> void launch_product(const Gated &d, const ProductArgs &a, bo
 bool streams(const Gated &d, int64_t cols, const RowsAt &x, bool vx)
 {
     constexpr int64_t most = (1ll << 31) / 256 / 2;          // elements from one line to the next
-    return d.v.bf16 && vx && cols <= most && d.pitch <= most && x.ss <= most && d.r.most >= 32u;
+    return d.v.bf16 && vx && cols <= most && d.pitch <= most && x.ss <= most;
+}
+
+// Tiles of all replicas.
+template <int FORM> uint64_t tiles_of(const Gated &d, int64_t cols, uint32_t tm, uint32_t tn)
+{
+    uint64_t rows = 0;
+    for (int32_t k = 0; k < d.v.K; ++k) rows += ceil_div(FORM == DW ? d.wide : d.r.n[k], tm);
+    return rows * ceil_div(FORM == FWD ? d.wide : cols, tn) * (FORM == DW ? 2 : 1);
+}
+
+// Rows of a tile of a gated block's products.
+constexpr uint32_t kCus = 256;
+template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
+{
+    if (FORM == DX && d.r.most <= 16u) return 16u;
+    if (FORM == DX && d.r.most <= 64u) return 64u;
+    return tiles_of<FORM>(d, cols, 256, FORM == FWD ? 128 : 256) >= 2 * kCus ? 256u : 128u;
+}
+
+// Workgroups that share a tile of dx: a contraction of 2 wide, and often few tiles.
+uint32_t dx_splits(const Gated &d, int64_t cols)
+{
+    if (!d.v.bf16 || !d.r.most) return 1;
+    const uint32_t tm = tile_rows<DX>(d, cols), tn = tm == 128u ? 128u : 256u;
+    const uint64_t tiles = tiles_of<DX>(d, cols, tm, tn), steps = 2 * (uint64_t)ceil_div(d.pitch, kStep);
+    const uint64_t want = (tm == 256u ? 2 * kCus : 4 * kCus) / tiles, most = steps / 4;
+    const uint64_t n = want < most ? want : most;
+    return n < 1 ? 1u : n > 64 ? 64u : (uint32_t)n;
 }
 
 template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN>
-void launch_big(const Gated &d, const ProductArgs &a, hipStream_t st)
+void launch_big(const Gated &d, const ProductArgs &a, uint32_t splits, float *part, hipStream_t st)
 {
     constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;
     TileMap map{};
     map.replicas = (uint32_t)d.v.K;
+    map.splits = splits;
+    map.part = part;
+    map.part_stride = (uint64_t)d.r.total * a.cols;
     uint32_t total = 0;
     for (int32_t k = 0; k < d.v.K; ++k) {
         map.first[k] = total;
@@ -400,16 +433,36 @@ void launch_big(const Gated &d, const ProductArgs &a, hipStream_t st)
         total += tm * ceil_div(FORM == FWD ? a.wide : a.cols, NT) * (FORM == DW ? 2u : 1u);
     }
     map.first[d.v.K] = total;
-    hipLaunchKernelGGL((big_product_kernel<FORM, TM, TN, WM, WN>), dim3(total), dim3(Big<FORM, TM, TN, WM, WN>::threads), 0, st, a, map);
+    hipLaunchKernelGGL((big_product_kernel<FORM, TM, TN, WM, WN>), dim3(total * splits), dim3(Big<FORM, TM, TN, WM, WN>::threads), 0, st, a, map);
 }
 
-template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, hipStream_t st)
+template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, uint32_t splits, float *part, hipStream_t st)
 {
-    if (big) launch_big<FORM, 256, 256, 2, 4>(d, a, st);
-    else launch_product<FORM>(d, a, vm, vn, st);
+    if (!big) return launch_product<FORM>(d, a, vm, vn, st);
+    if constexpr (FORM == FWD) {
+        const dim3 grid(ceil_div(a.wide, 16), d.v.K);
+        if (d.r.most <= 64u) {
+            if (d.r.most <= 16u) hipLaunchKernelGGL((few_rows_kernel<1>), grid, dim3(256), 0, st, a);
+            else if (d.r.most <= 32u) hipLaunchKernelGGL((few_rows_kernel<2>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((few_rows_kernel<4>), grid, dim3(256), 0, st, a);
+            return;
+        }
+    }
+    const uint32_t tm = tile_rows<FORM>(d, a.cols);
+    if constexpr (FORM == DX) {
+        if (tm == 16u) return launch_big<FORM, 16, 256, 1, 4>(d, a, splits, part, st);
+        if (tm == 64u) return launch_big<FORM, 64, 256, 1, 4>(d, a, splits, part, st);
+    }
+    if (tm == 128u) launch_big<FORM, 128, 128, 2, 2>(d, a, splits, part, st);
+    else launch_big<FORM, 256, 256, 2, 4>(d, a, splits, part, st);
 }
 
-int64_t gated_bytes(const Gated &d) { return 2 * (int64_t)d.r.total * d.pitch * d.es; }
+int64_t gates_bytes(const Gated &d) { return (int64_t)round_up16((uint64_t)d.r.total * d.pitch * d.es); }          // dg, and du again
+int64_t gated_bytes(const Gated &d, int64_t cols)
+{
+    const uint32_t splits = dx_splits(d, cols);
+    return 2 * gates_bytes(d) + (splits > 1 ? (int64_t)splits * d.r.total * cols * (int64_t)sizeof(float) : 0);
+}
 
 } // namespace
 
@@ -434,7 +487,7 @@ extern "C" lasgd_status lasgd_gated(lasgd_ctx *c, int32_t gate, int32_t up, cons
     if (!d.r.most) return LASGD_OK;
     weights(p, d, d.v.params, gate, up, cols);
     p.wide_out = vo;
-    launch_form<FWD>(d, p, streams(d, cols, p.x, vx), vx, cols % 8 == 0, (hipStream_t)stream);
+    launch_form<FWD>(d, p, streams(d, cols, p.x, vx), vx, cols % 8 == 0, 1, nullptr, (hipStream_t)stream);
     return launched(c);
 }
 
@@ -444,7 +497,7 @@ extern "C" lasgd_status lasgd_gated_backward_bytes(lasgd_ctx *c, int32_t gate, i
     Gated d;
     CHECK(bytes, LASGD_ERR_INVALID, "NULL bytes");
     TRY(check_gated(c, d, gate, up, rows, cols));
-    *bytes = gated_bytes(d);
+    *bytes = gated_bytes(d, cols);
     return LASGD_OK;
 }
 
@@ -465,14 +518,14 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
     TRY(check_rows(c, d.v, d.r, "u", u, d.wide, d.es, false, e.u, vg));
     TRY(check_rows(c, d.v, d.r, "da", da, d.wide, d.es, false, e.da, vg));
     if (dx) TRY(check_rows(c, d.v, d.r, "dx", dx, cols, d.es, true, out, vo));
-    const int64_t need = gated_bytes(d);
+    const int64_t need = gated_bytes(d, cols);
     TRY(check_workspace(c, workspace, workspace_bytes, need));
     CHECK(d.v.all_bound, LASGD_ERR_STATE, "not every replica is bound");
     TRY(check_device(c, d.v));
     if (!d.r.most && accumulate) return LASGD_OK;
     const hipStream_t st = (hipStream_t)stream;
     e.dg = (char *)workspace;
-    e.du = e.dg + need / 2;
+    e.du = e.dg + gates_bytes(d);
     p.dg = e.dg;
     p.du = e.du;
     if (d.r.most) {
@@ -494,11 +547,20 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
         q.a = out;
         weights(q, d, d.v.params, gate, up, cols);
         q.wide_out = vo;
-        launch_form<DX>(d, q, big, true, cols % 8 == 0, st);
+        const uint32_t splits = big ? dx_splits(d, cols) : 1;
+        float *part = (float *)(e.du + gates_bytes(d));
+        launch_form<DX>(d, q, big, true, cols % 8 == 0, splits, part, st);
         TRY(launched(c));
+        if (splits > 1) {
+            JoinRowsArgs j{out, part, (uint64_t)d.r.total * cols, splits, (uint32_t)cols, vo, {}, {}};
+            copy_rows(j, d.r, d.v.K);
+            memcpy(j.first, d.r.first, d.v.K * sizeof(uint32_t));
+            hipLaunchKernelGGL((join_rows_kernel<>), dim3(d.r.most < 4096u ? d.r.most : 4096u, d.v.K), dim3(256), 0, st, j);
+            TRY(launched(c));
+        }
     }
     p.accumulate = accumulate;
     weights(p, d, d.v.grads, gate, up, cols);
-    launch_form<DW>(d, p, big, true, vx, st);
+    launch_form<DW>(d, p, big, true, vx, 1, nullptr, st);
     return launched(c);
 }
