@@ -45,7 +45,7 @@ struct GatesArgs {
     uint32_t first[64];          // rows of the replicas before
 };
 
-template <bool BF16, bool VEC>
+template <bool BF16, int VEC>
 __global__ __launch_bounds__(256) void gates_backward_kernel(const GatesArgs a)
 {
     const uint32_t k = blockIdx.y, rows = a.rows[k];
@@ -63,8 +63,8 @@ __global__ __launch_bounds__(256) void gates_backward_kernel(const GatesArgs a)
                 uv[j] = dv[j] * f.f;
             }
             const int64_t at = (int64_t)(a.first[k] + r) * a.pitch + c;
-            store8<BF16, true>(a.dg, at, 8u, gv);            // whole groups: the columns behind the last are the workspace's own
-            store8<BF16, true>(a.du, at, 8u, uv);
+            store8<BF16, WIDE>(a.dg, at, 8u, gv);            // whole groups: the columns behind the last are the workspace's own
+            store8<BF16, WIDE>(a.du, at, 8u, uv);
         }
 }
 
@@ -110,8 +110,8 @@ __device__ __forceinline__ void stage(typename Elem<BF16>::type *lds, const char
     const uint32_t n = left >= 8 ? 8u : left > 0 ? (uint32_t)left : 0u;
     const int64_t at = ALONG ? i * stride + c : c * stride + i;
     float v[8];
-    if (VEC && n) load8<BF16, VEC>(v, p, at, 8u);
-    else load8<BF16, false>(v, p, at, VEC ? 0u : n);
+    if (VEC && n) load8<BF16, WIDE>(v, p, at, 8u);
+    else load8<BF16, LOOSE>(v, p, at, VEC ? 0u : n);
 #pragma unroll
     for (uint32_t j = 0; j < 8u; ++j) {
         const uint32_t w = ALONG ? il * P + cl + j : (il + j) * P + cl;
@@ -332,8 +332,8 @@ template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN> struct B
 // Eight elements of bf16 or, where they may not be stored at once, as many as there are.
 __device__ __forceinline__ void store_some(char *p, int64_t at, bool at_once, uint32_t there, const float (&v)[8])
 {
-    if (at_once) store8<true, true>(p, at, 8u, v);
-    else store8<true, false>(p, at, there, v);
+    if (at_once) store8<true, WIDE>(p, at, 8u, v);
+    else store8<true, LOOSE>(p, at, there, v);
 }
 
 struct TileMap {
@@ -451,17 +451,17 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN>::threads)) void big_prod
                 for (int e = 0; e < 8; ++e) v[e] = activation(a.act, v[e]).f * u[e];
                 store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
             } else if constexpr (FORM == DX) {
-                if (map.splits > 1u) store8<false, true>((char *)(map.part + split * map.part_stride), (int64_t)(a.first[k] + row) * cols + col, 8u, v);
+                if (map.splits > 1u) store8<false, WIDE>((char *)(map.part + split * map.part_stride), (int64_t)(a.first[k] + row) * cols + col, 8u, v);
                 else store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
             } else {                                  // cols counts whole eights
                 char *grad = second ? a.up[k] : a.gate[k];
                 if (a.accumulate) {
                     float old[8];
-                    load8<true, true>(old, grad, row * cols + col, 8u);
+                    load8<true, WIDE>(old, grad, row * cols + col, 8u);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] += old[e];
                 }
-                store8<true, true>(grad, row * cols + col, 8u, v);
+                store8<true, WIDE>(grad, row * cols + col, 8u, v);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -487,10 +487,10 @@ __global__ __launch_bounds__(256) void join_rows_kernel(const JoinRowsArgs a)
             float sum[8], v[8];
             const char *from = (const char *)a.part;
             const int64_t at = (int64_t)(a.first[k] + r) * a.cols + g * 8u;
-            load8<false, true>(sum, from, at, 8u);
+            load8<false, WIDE>(sum, from, at, 8u);
 #pragma unroll 4
             for (uint32_t s = 1; s < a.splits; ++s) {
-                load8<false, true>(v, from, at + (int64_t)(s * a.part_stride), 8u);
+                load8<false, WIDE>(v, from, at + (int64_t)(s * a.part_stride), 8u);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += v[e];
             }

@@ -7,6 +7,7 @@
 
 namespace lasgd {
 
+
 struct RowsAt {             // element (k, r, c) is at p + (k * rs + r * ss + c) elements
     char *p;
     int64_t rs, ss;
@@ -81,38 +82,78 @@ template <bool BF16> __device__ __forceinline__ void store1(char *p, int64_t i, 
     else as_global<float>(p)[i] = v;
 }
 
-// VEC: 16-byte accesses, and all eight are there; otherwise n of them are.
-template <bool BF16, bool VEC> __device__ __forceinline__ void load8(float (&v)[8], const char *p, int64_t at, uint32_t n)
+// The type of a 16-byte access to elements of ES bytes that are aligned to themselves only.
+template <int ES> struct Loose;
+template <> struct Loose<2> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct Loose<4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
+
+// Eight elements as they are in memory.
+template <bool BF16> struct Raw8 { u32x4 w[BF16 ? 1 : 2]; };
+
+// How a call's rows are accessed.  LOOSE: n elements are there, eight or more at once, fewer one by one.  (Rows that do not start on 16 bytes: a norm of 1023
+// fp32 columns took 53 us with single accesses throughout, 18 so.)  WIDE: aligned, and all eight are there.  STREAM: the same with the streaming hint, for calls
+// that move more than the memory-side cache holds.
+enum Access : int { LOOSE = 0, WIDE = 1, STREAM = 2 };
+template <bool BF16, int VEC> __device__ __forceinline__ Raw8<BF16> load_raw(const char *p, int64_t at, uint32_t n)
 {
-    if constexpr (VEC && BF16) {
-        const u32x4 w = *as_global<u32x4>(p + at * 2);
+    constexpr int ES = BF16 ? 2 : 4;
+    Raw8<BF16> r;
+    if constexpr (VEC) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[2 * j] = widen_lo(w[j]), v[2 * j + 1] = widen_hi(w[j]);
-    } else if constexpr (VEC) {
-        const u32x4 a = *as_global<u32x4>(p + at * 4), b = *as_global<u32x4>(p + at * 4 + 16);
+        for (int i = 0; i < 8 * ES / 16; ++i) {
+            if constexpr (VEC == STREAM) r.w[i] = __builtin_nontemporal_load(as_global<u32x4>(p + at * ES + i * 16));
+            else r.w[i] = *as_global<u32x4>(p + at * ES + i * 16);
+        }
+    } else if (n >= 8u) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(a[j]), v[4 + j] = __uint_as_float(b[j]);
+        for (int i = 0; i < 8 * ES / 16; ++i) r.w[i] = *as_global<typename Loose<ES>::type>(p + at * ES + i * 16);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (uint32_t)j < n ? load1<BF16>(p, at + j) : 0.f;
+        for (int i = 0; i < 8 * ES / 16; ++i) r.w[i] = u32x4{};
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if ((uint32_t)j < n) {
+                if constexpr (BF16) r.w[0][j >> 1] |= (uint32_t)as_global<uint16_t>(p)[at + j] << (16 * (j & 1));
+                else r.w[j >> 2][j & 3] = as_global<uint32_t>(p)[at + j];
+            }
+    }
+    return r;
+}
+template <bool BF16> __device__ __forceinline__ void widen8(float (&v)[8], const Raw8<BF16> &r)
+{
+    if constexpr (BF16) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[2 * j] = widen_lo(r.w[0][j]), v[2 * j + 1] = widen_hi(r.w[0][j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r.w[j >> 2][j & 3]);
     }
 }
-template <bool BF16, bool VEC> __device__ __forceinline__ void store8(char *p, int64_t at, uint32_t n, const float (&v)[8])
+template <bool BF16, int VEC> __device__ __forceinline__ void load8(float (&v)[8], const char *p, int64_t at, uint32_t n)
 {
-    if constexpr (VEC && BF16) {
-        u32x4 w;
+    widen8<BF16>(v, load_raw<BF16, VEC>(p, at, n));
+}
+template <bool BF16, int VEC> __device__ __forceinline__ void store8(char *p, int64_t at, uint32_t n, const float (&v)[8])
+{
+    constexpr int ES = BF16 ? 2 : 4;
+    if (VEC || n >= 8u) {
+        Raw8<BF16> r;
+        if constexpr (BF16) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = narrow2(v[2 * j], v[2 * j + 1]);
-        *as_global<u32x4>(p + at * 2) = w;
-    } else if constexpr (VEC) {
-        u32x4 a, b;
+            for (int j = 0; j < 4; ++j) r.w[0][j] = narrow2(v[2 * j], v[2 * j + 1]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(v[j]), b[j] = __float_as_uint(v[4 + j]);
-        *as_global<u32x4>(p + at * 4) = a;
-        *as_global<u32x4>(p + at * 4 + 16) = b;
+            for (int j = 0; j < 8; ++j) r.w[j >> 2][j & 3] = __float_as_uint(v[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8 * ES / 16; ++i) {
+            if constexpr (VEC == STREAM) __builtin_nontemporal_store(r.w[i], as_global<u32x4>(p + at * ES + i * 16));
+            else if constexpr (VEC) *as_global<u32x4>(p + at * ES + i * 16) = r.w[i];
+            else *as_global<typename Loose<ES>::type>(p + at * ES + i * 16) = r.w[i];
+        }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 7; ++j)
             if ((uint32_t)j < n) store1<BF16>(p, at + j, v[j]);
     }
 }
@@ -130,7 +171,7 @@ struct DropoutArgs {
     uint32_t rows[64];
 };
 
-template <bool BF16, bool VEC>
+template <bool BF16, int VEC>
 __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a)
 {
     const uint32_t k = blockIdx.y, rows = a.rows[k];
@@ -142,13 +183,13 @@ __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a)
     const uint64_t call = call_number(a.drop);
     for (uint32_t g = tx; g < a.groups; g += 1u << a.tx_shift) {
         const uint32_t c = g * 8u, n = a.cols - c;
-        float x[kDropRows][8], res[kDropRows][8];
+        Raw8<BF16> x[kDropRows], res[kDropRows];
 #pragma unroll
         for (uint32_t u = 0; u < kDropRows; ++u) {
             const uint64_t r = r1 + u * ty;
             if (r < rows) {
-                load8<BF16, VEC>(x[u], a.x.p, k * a.x.rs + (int64_t)r * a.x.ss + c, n);
-                if (a.residual.p) load8<BF16, VEC>(res[u], a.residual.p, k * a.residual.rs + (int64_t)r * a.residual.ss + c, n);
+                x[u] = load_raw<BF16, VEC>(a.x.p, k * a.x.rs + (int64_t)r * a.x.ss + c, n);
+                if (a.residual.p) res[u] = load_raw<BF16, VEC>(a.residual.p, k * a.residual.rs + (int64_t)r * a.residual.ss + c, n);
             }
         }
 #pragma unroll
@@ -156,11 +197,13 @@ __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a)
             const uint64_t r = r1 + u * ty;
             if (r >= rows) break;
             const Lots lots = draw_lots(a.drop, call, k, r * a.groups + g);
-            float y[8];
+            float y[8], z[8];
+            widen8<BF16>(y, x[u]);
+            if (a.residual.p) widen8<BF16>(z, res[u]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                y[j] = stays(lots, j, a.drop.below) ? x[u][j] * a.drop.scale : 0.f;
-                if (a.residual.p) y[j] = res[u][j] + y[j];
+                y[j] = stays(lots, j, a.drop.below) ? y[j] * a.drop.scale : 0.f;
+                if (a.residual.p) y[j] = z[j] + y[j];
             }
             store8<BF16, VEC>(a.y.p, k * a.y.rs + (int64_t)r * a.y.ss + c, n, y);
         }
@@ -198,6 +241,21 @@ template <int G> __device__ __forceinline__ float row_sum(float v, float *lds)
     }
     return v;
 }
+// Two at once.
+template <int G> __device__ __forceinline__ float2 row_sums(float2 v, float2 *lds)
+{
+#pragma unroll
+    for (int d = (G < 64 ? G : 64) / 2; d; d >>= 1) v.x += __shfl_xor(v.x, d, 64), v.y += __shfl_xor(v.y, d, 64);
+    if constexpr (G > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63u) == 0u) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < G / 64; ++w) v.x += lds[w].x, v.y += lds[w].y;
+    }
+    return v;
+}
 __device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }      // a NaN stays
 template <int G> __device__ __forceinline__ float row_max(float v, float *lds)
 {
@@ -216,7 +274,7 @@ template <int G> __device__ __forceinline__ float row_max(float v, float *lds)
 
 constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
 
-template <bool BF16, bool VEC, int G, int NV>
+template <bool BF16, int VEC, int G, int NV>
 __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRowsArgs a)
 {
     __shared__ float lds[G > 64 ? G / 64 : 1];
@@ -230,35 +288,35 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRow
     const char *gain = a.gain[k];
     float h[NV][8];
     float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const uint32_t g = t + i * G, c = g * 8u;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[i][j] = 0.f;
-        if (g < a.groups) {
-            load8<BF16, VEC>(h[i], a.x.p, k * a.x.rs + (int64_t)r * a.x.ss + c, a.cols - c);
-        }
-    }
-    if (a.drop.below) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t g = t + i * G;
-            if (g < a.groups) {
-                const Lots lots = draw_lots(a.drop, call, k, r * a.groups + g);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[i][j] = stays(lots, j, a.drop.below) ? h[i][j] * a.drop.scale : 0.f;
-            }
-        }
-    }
-    if (a.residual.p) {
+    {
+        Raw8<BF16> x[NV], res[NV];               // all asked for before the first is looked at
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t g = t + i * G, c = g * 8u;
-            if (g < a.groups) {
-                float res[8];
-                load8<BF16, VEC>(res, a.residual.p, k * a.residual.rs + (int64_t)r * a.residual.ss + c, a.cols - c);
+            x[i] = Raw8<BF16>{};
+            if (g < a.groups) x[i] = load_raw<BF16, VEC>(a.x.p, k * a.x.rs + (int64_t)r * a.x.ss + c, a.cols - c);
+        }
+        if (a.residual.p) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[i][j] = res[j] + h[i][j];
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t g = t + i * G, c = g * 8u;
+                res[i] = Raw8<BF16>{};
+                if (g < a.groups) res[i] = load_raw<BF16, VEC>(a.residual.p, k * a.residual.rs + (int64_t)r * a.residual.ss + c, a.cols - c);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            widen8<BF16>(h[i], x[i]);
+            if (a.drop.below) {
+                const Lots lots = draw_lots(a.drop, call, k, r * a.groups + t + i * G);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] = stays(lots, j, a.drop.below) ? h[i][j] * a.drop.scale : 0.f;
+            }
+            if (a.residual.p) {
+                float z[8];
+                widen8<BF16>(z, res[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] = z[j] + h[i][j];
             }
         }
     }
@@ -282,7 +340,7 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRow
         const uint32_t g = t + i * G, c = g * 8u;
         if (g < a.groups) {
             float w[8];
-            load8<BF16, VEC>(w, gain, c, a.cols - c);
+            load8<BF16, VEC ? WIDE : LOOSE>(w, gain, c, a.cols - c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 h[i][j] = w[j] * (h[i][j] * rho);
@@ -310,7 +368,9 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRow
                 q[j] = (uint32_t)w;
             }
             char *y = a.y.p + (k * a.y.rs + (int64_t)r * a.y.ss + c);
+            typedef uint32_t loose2 __attribute__((ext_vector_type(2), aligned(1)));
             if constexpr (VEC) *as_global<u32x2>(y) = u32x2{q[0], q[1]};
+            else if (a.cols - c >= 8u) *as_global<loose2>(y) = u32x2{q[0], q[1]};
             else {
 #pragma unroll
                 for (uint32_t j = 0; j < 8u; ++j)
@@ -330,15 +390,16 @@ struct NormBackArgs {
     uint32_t cols, groups;
     float eps, inv_cols;
     uint32_t parts;              // workgroups a replica
-    float *part;                 // [K][parts * rows a workgroup][groups * 8]
+    float *part;                 // [K][parts][groups * 8]
     uint32_t rows[64];
     const char *gain[64];
 };
 
-template <bool BF16, bool VEC, int G, int NV>
+template <bool BF16, int VEC, int G, int NV>
 __global__ __launch_bounds__(norm_threads(G)) void rms_norm_backward_kernel(const NormBackArgs a)
 {
-    __shared__ float lds[G > 64 ? G / 64 : 1];
+    __shared__ float2 lds[G > 64 ? G / 64 : 1];
+    constexpr bool AHEAD = G < 1024;             // the next row is on its way while this one is worked on; 1024 threads have no registers for it
     constexpr uint32_t R = norm_threads(G) / G;
     const uint32_t k = blockIdx.y, rows = a.rows[k];
     const uint32_t t = threadIdx.x % G, lane_row = threadIdx.x / G;
@@ -350,67 +411,102 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_backward_kernel(cons
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
     }
-    for (uint64_t r = (uint64_t)blockIdx.x * R + lane_row; r < rows; r += (uint64_t)a.parts * R) {
-        float h[NV][8], d[NV][8];
+    struct Row {
+        Raw8<BF16> h[NV], dy[NV], dsum[NV];
+    };
+    auto ask = [&](Row &row, uint64_t r) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G, c = g * 8u;
+            row.h[i] = row.dy[i] = row.dsum[i] = Raw8<BF16>{};
+            if (g < a.groups && r < rows) {
+                row.h[i] = load_raw<BF16, VEC>(a.h.p, k * a.h.rs + (int64_t)r * a.h.ss + c, a.cols - c);
+                row.dy[i] = load_raw<BF16, VEC>(a.dy.p, k * a.dy.rs + (int64_t)r * a.dy.ss + c, a.cols - c);
+                if (a.dsum.p) row.dsum[i] = load_raw<BF16, VEC>(a.dsum.p, k * a.dsum.rs + (int64_t)r * a.dsum.ss + c, a.cols - c);
+            }
+        }
+    };
+    const uint64_t on = (uint64_t)a.parts * R;
+    Row row;
+    ask(row, (uint64_t)blockIdx.x * R + lane_row);
+    for (uint64_t r = (uint64_t)blockIdx.x * R + lane_row; r < rows; r += on) {
+        Row next;
+        if constexpr (AHEAD) ask(next, r + on);
         float sum = 0.f, dot = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t g = t + i * G, c = g * 8u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[i][j] = d[i][j] = 0.f;
             if (g < a.groups) {
-                load8<BF16, VEC>(h[i], a.h.p, k * a.h.rs + (int64_t)r * a.h.ss + c, a.cols - c);
-                load8<BF16, VEC>(d[i], a.dy.p, k * a.dy.rs + (int64_t)r * a.dy.ss + c, a.cols - c);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t g = t + i * G, c = g * 8u;
-            if (g < a.groups) {
-                float w[8];
-                load8<BF16, VEC>(w, gain, c, a.cols - c);
+                float w[8], h[8], d[8];
+                load8<BF16, VEC ? WIDE : LOOSE>(w, gain, c, a.cols - c);
+                widen8<BF16>(h, row.h[i]);
+                widen8<BF16>(d, row.dy[i]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    sum = __builtin_fmaf(h[i][j], h[i][j], sum);
-                    dot = __builtin_fmaf(h[i][j], w[j] * d[i][j], dot);
+                    sum = __builtin_fmaf(h[j], h[j], sum);
+                    dot = __builtin_fmaf(h[j], w[j] * d[j], dot);
                 }
             }
         }
-        sum = row_sum<G>(sum, lds);
-        dot = row_sum<G>(dot, lds);
+        const float2 both = row_sums<G>(make_float2(sum, dot), lds);
+        sum = both.x, dot = both.y;
         const float rho = 1.f / __builtin_sqrtf(__builtin_fmaf(sum, a.inv_cols, a.eps));
         const float mean = dot * rho * a.inv_cols;           // of hhat gain dy
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t g = t + i * G, c = g * 8u;
             if (g < a.groups) {
-                float w[8], more[8];
-                load8<BF16, VEC>(w, gain, c, a.cols - c);
-                if (a.dsum.p) load8<BF16, VEC>(more, a.dsum.p, k * a.dsum.rs + (int64_t)r * a.dsum.ss + c, a.cols - c);
+                float w[8], h[8], d[8], more[8];
+                load8<BF16, VEC ? WIDE : LOOSE>(w, gain, c, a.cols - c);
+                widen8<BF16>(h, row.h[i]);
+                widen8<BF16>(d, row.dy[i]);
+                if (a.dsum.p) widen8<BF16>(more, row.dsum[i]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float hat = h[i][j] * rho;
-                    acc[i][j] = __builtin_fmaf(d[i][j], hat, acc[i][j]);
-                    d[i][j] = rho * __builtin_fmaf(-hat, mean, w[j] * d[i][j]);
-                    if (a.dsum.p) d[i][j] += more[j];
+                    const float hat = h[j] * rho;
+                    acc[i][j] = __builtin_fmaf(d[j], hat, acc[i][j]);
+                    d[j] = rho * __builtin_fmaf(-hat, mean, w[j] * d[j]);
+                    if (a.dsum.p) d[j] += more[j];
                 }
-                if (a.dresidual.p) store8<BF16, VEC>(a.dresidual.p, k * a.dresidual.rs + (int64_t)r * a.dresidual.ss + c, a.cols - c, d[i]);
+                if (a.dresidual.p) store8<BF16, VEC>(a.dresidual.p, k * a.dresidual.rs + (int64_t)r * a.dresidual.ss + c, a.cols - c, d);
                 if (a.dx.p) {
                     if (a.drop.below) {
                         const Lots lots = draw_lots(a.drop, call, k, r * a.groups + g);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) d[i][j] = stays(lots, j, a.drop.below) ? d[i][j] * a.drop.scale : 0.f;
+                        for (int j = 0; j < 8; ++j) d[j] = stays(lots, j, a.drop.below) ? d[j] * a.drop.scale : 0.f;
                     }
-                    store8<BF16, VEC>(a.dx.p, k * a.dx.rs + (int64_t)r * a.dx.ss + c, a.cols - c, d[i]);
+                    store8<BF16, VEC>(a.dx.p, k * a.dx.rs + (int64_t)r * a.dx.ss + c, a.cols - c, d);
                 }
             }
         }
+        if constexpr (AHEAD) row = next;
+        else ask(row, r + on);
     }
-    const uint64_t part = ((uint64_t)k * a.parts + blockIdx.x) * R + lane_row;
+    // the workgroup's rows, added in their order
+    if constexpr (R > 1) {
+        __shared__ float sums[R - 1][G * NV][9];
+        if (lane_row) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sums[lane_row - 1][i * G + t][j] = acc[i][j];
+            }
+        }
+        __syncthreads();
+        if (lane_row) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                for (uint32_t o = 0; o < R - 1u; ++o) acc[i][j] += sums[o][i * G + t][j];
+            }
+        }
+    }
+    const uint64_t part = (uint64_t)k * a.parts + blockIdx.x;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t g = t + i * G;
-        if (g < a.groups) store8<false, true>(reinterpret_cast<char *>(a.part), (int64_t)(part * a.groups + g) * 8, 8u, acc[i]);
+        if (g < a.groups) store8<false, WIDE>(reinterpret_cast<char *>(a.part), (int64_t)(part * a.groups + g) * 8, 8u, acc[i]);
     }
 }
 
