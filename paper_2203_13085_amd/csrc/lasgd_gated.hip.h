@@ -245,7 +245,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ uint32_t records(int64_t bytes) { return bytes <= 0 ? 0u : bytes > 0xfffffff0ll ? 0xfffffff0u : (uint32_t)bytes; }
 
 // The next kStep of the contraction into LDS.  left: how much of it is still there (ALONG: beyond it the line goes on with something else).
-template <bool ALONG, uint32_t T, uint32_t THREADS>
+template <bool ALONG, uint32_t T, uint32_t THREADS, bool HINT = false>
 __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left)
 {
     constexpr uint32_t PIECES = T * kStep / 8u, LINE = ALONG ? kStep / 8u : T / 8u;
@@ -259,7 +259,7 @@ __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left
         const uint32_t piece = at % LINE ^ (ALONG ? line & 7u : (line & 3u) * 2u);
         uint32_t off = line * (uint32_t)s.stride + piece * 16u;
         if (ALONG && (int64_t)(piece * 8u) >= left) off = 0xfffffff0u;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64u) * 16u), 16, off, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64u) * 16u), 16, off, 0, 0, HINT ? 2 : 0);
     }
 }
 
@@ -280,7 +280,8 @@ __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, uint32_t row0, u
     }
 }
 
-template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN> struct Big {
+// HINT: the weights are read with the streaming hint.
+template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT> struct Big {
     static constexpr uint32_t threads = 64u * WM * WN;
     static constexpr bool along_m = FORM != DW, along_n = FORM == FWD;
     static constexpr uint32_t FM = TM / WM / 16u, FN = TN / WN / 16u;           // fragments of a wave
@@ -294,9 +295,9 @@ template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN> struct B
     {
         fetch<along_m, TM, threads>(lds, m, left);
         if constexpr (FORM == FWD) {
-            fetch<true, TN / 2u, threads>(lds + TM * kStep * 2u, n, left);
-            fetch<true, TN / 2u, threads>(lds + (TM + TN / 2u) * kStep * 2u, n2, left);
-        } else fetch<along_n, TN, threads>(lds + TM * kStep * 2u, n, left);
+            fetch<true, TN / 2u, threads, HINT>(lds + TM * kStep * 2u, n, left);
+            fetch<true, TN / 2u, threads, HINT>(lds + (TM + TN / 2u) * kStep * 2u, n2, left);
+        } else fetch<along_n, TN, threads, HINT>(lds + TM * kStep * 2u, n, left);
     }
     // row of the n side's fragment j: a wave of FWD has the same columns of gate and up
     static __device__ __forceinline__ uint32_t n_row(uint32_t wn, uint32_t j)
@@ -351,14 +352,15 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total)
     return x * per + (x < more ? x : more) + (id >> 3);
 }
 
-template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN>
-__global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)
+template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT>
+__global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN, HINT>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)
 {
-    using S = Big<FORM, TM, TN, WM, WN>;
+    using S = Big<FORM, TM, TN, WM, WN, HINT>;
     __shared__ __attribute__((aligned(1024))) char lds_mem[S::lds];
     lds_char *lds = (lds_char *)lds_mem;
     const uint32_t order = xcd_order(blockIdx.x, gridDim.x);
-    const uint32_t id = FORM == DX ? order / map.splits : order, split = FORM == DX ? order % map.splits : 0u;
+    const uint32_t tiles = map.first[map.replicas];
+    const uint32_t id = FORM == DX ? order % tiles : order, split = FORM == DX ? order / tiles : 0u;
     uint32_t k = 0;
     for (uint32_t half = 32u; half; half >>= 1)
         if (k + half < map.replicas && map.first[k + half] <= id) k += half;
@@ -499,67 +501,59 @@ __global__ __launch_bounds__(256) void join_rows_kernel(const JoinRowsArgs a)
 }
 
 // ---- bf16, aligned, a few rows ------------------------------------------------------------------------------------------------------
-// FWD, bound by the weights' bytes.  A workgroup has 16 columns of gate and of up and all of a replica's rows, up to 16 FM; its four waves share
-// the contraction, take the weights straight from memory into registers, and are added up in LDS.
-template <uint32_t FM>
-__global__ __launch_bounds__(256) void few_rows_kernel(const ProductArgs a)
+// DW, bound by the gradients' bytes: up to 32 rows are one step of the contraction.  A workgroup has 256 columns of the hidden side, 16 at a time, and 256 of
+// the model's, 64 a wave, and both sides' rows in LDS as they are in memory.  C goes through LDS once more, so that a store writes whole lines of 128 bytes:
+// with the streaming hint on halves of lines, 180 MB of gradients a weight (K = 8, 2048 x 5504) took 105 us in place of 68, on quarters 225.
+constexpr uint32_t kFewRows = 32;
+template <bool ACCUMULATE, int ACCESS>
+__global__ __launch_bounds__(256) void few_rows_weights_kernel(const ProductArgs a)
 {
-    constexpr uint32_t U = FM == 1u ? 4u : 2u;                  // of 32 of the contraction, asked for together
-    __shared__ float part[4][2][FM * 16u][17];
+    constexpr uint32_t T = 256;
+    __shared__ __attribute__((aligned(1024))) char mem[2][kFewRows * T * 2u];
+    __shared__ float out[4][16][68];
+    lds_char *hidden = (lds_char *)mem[0], *model = (lds_char *)mem[1];
     const uint32_t k = blockIdx.y, rows = a.rows[k], cols = a.cols, wide = a.wide;
-    if (!rows) return;
-    const uint32_t n0 = blockIdx.x * 16u, w = threadIdx.x >> 6, lane = threadIdx.x & 63u, i = lane & 15u, quad = lane >> 4;
-    const bool there = n0 + i < wide;
-    const char *gate = a.gate[k] + ((uint64_t)(there ? n0 + i : 0u) * cols + quad * 8u) * 2u, *up = a.up[k] + ((uint64_t)(there ? n0 + i : 0u) * cols + quad * 8u) * 2u;
-    const char *x[FM];
+    const uint32_t tn = (cols + T - 1u) / T, d0 = blockIdx.x % tn * T, f0 = blockIdx.x / tn * T;
+    const char *from = (blockIdx.z ? a.du : a.dg) + (uint64_t)a.first[k] * a.pitch * 2u, *x = a.x.p + k * a.x.rs * 2;
+    char *grad = blockIdx.z ? a.up[k] : a.gate[k];
 #pragma unroll
-    for (uint32_t f = 0; f < FM; ++f) x[f] = a.x.p + (k * a.x.rs + (int64_t)(f * 16u + i < rows ? f * 16u + i : 0u) * a.x.ss + quad * 8u) * 2;
-    f32x4 g[FM] = {}, u[FM] = {};
-    for (uint32_t c0 = w * 32u; c0 < cols; c0 += U * 128u) {
-        u32x4 wg[U], wu[U], m[U][FM];
-#pragma unroll
-        for (uint32_t t = 0; t < U; ++t) {
-            const uint32_t c = c0 + t * 128u;
-            wg[t] = wu[t] = u32x4{};
-#pragma unroll
-            for (uint32_t f = 0; f < FM; ++f) m[t][f] = u32x4{};
-            if (c + quad * 8u < cols) {
-                wg[t] = __builtin_nontemporal_load(as_global<u32x4>(gate + c * 2u));
-                wu[t] = __builtin_nontemporal_load(as_global<u32x4>(up + c * 2u));
-#pragma unroll
-                for (uint32_t f = 0; f < FM; ++f) m[t][f] = *as_global<u32x4>(x[f] + c * 2u);
-            }
-        }
-#pragma unroll
-        for (uint32_t t = 0; t < U; ++t) {
-#pragma unroll
-            for (uint32_t f = 0; f < FM; ++f) {
-                const bf16x8 v = __builtin_bit_cast(bf16x8, m[t][f]);
-                g[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wg[t]), v, g[f], 0, 0, 0);
-                u[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wu[t]), v, u[f], 0, 0, 0);
-            }
-        }
-    }
-#pragma unroll
-    for (uint32_t f = 0; f < FM; ++f) {
-#pragma unroll
-        for (uint32_t e = 0; e < 4u; ++e) {
-            part[w][0][f * 16u + i][quad * 4u + e] = g[f][e];
-            part[w][1][f * 16u + i][quad * 4u + e] = u[f][e];
-        }
+    for (uint32_t t = threadIdx.x; t < kFewRows * T / 8u; t += 256u) {
+        const uint32_t line = t / (T / 8u), c = t % (T / 8u) * 8u, at = line * (T * 2u) + ((c * 2u) ^ (line & 3u) * 32u);          // as fragment expects it
+        u32x4 h{}, m{};
+        if (line < rows && f0 + c < a.pitch) h = *as_global<u32x4>(from + ((uint64_t)line * a.pitch + f0 + c) * 2u);
+        if (line < rows && d0 + c < cols) m = *as_global<u32x4>(x + ((int64_t)line * a.x.ss + d0 + c) * 2);
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(hidden + at) = h;
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(model + at) = m;
     }
     __syncthreads();
-    const uint32_t n = threadIdx.x & 15u;
-    if (n0 + n >= wide) return;
-    for (uint32_t r = threadIdx.x >> 4; r < rows; r += 16u) {
-        float gv = 0.f, uv = 0.f;
+    const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6, col = d0 + w * 64u + (lane & 7u) * 8u;
+    bf16x8 n[4];
 #pragma unroll
-        for (uint32_t v = 0; v < 4u; ++v) gv += part[v][0][r][n], uv += part[v][1][r][n];
-        store1<true>(a.a.p, k * a.a.rs + (int64_t)r * a.a.ss + n0 + n, activation(a.act, gv).f * uv);
-        if (a.g.p) {
-            store1<true>(a.g.p, k * a.g.rs + (int64_t)r * a.g.ss + n0 + n, gv);
-            store1<true>(a.u.p, k * a.u.rs + (int64_t)r * a.u.ss + n0 + n, uv);
+    for (uint32_t j = 0; j < 4u; ++j) n[j] = fragment<false, T>(model, w * 64u + j * 16u, 0);
+#pragma unroll 2
+    for (uint32_t i = 0; i < T; i += 16u) {
+        if (f0 + i >= wide) break;
+        const bf16x8 m = fragment<false, T>(hidden, i, 0);
+#pragma unroll
+        for (uint32_t j = 0; j < 4u; ++j)
+            *reinterpret_cast<f32x4 *>(&out[w][lane & 15u][j * 16u + (lane >> 4) * 4u]) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m, f32x4{}, 0, 0, 0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (uint32_t r = lane >> 3; r < 16u; r += 8u) {
+            if (f0 + i + r >= wide || col >= cols) continue;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = out[w][r][(lane & 7u) * 8u + e];
+            const int64_t at = (int64_t)(f0 + i + r) * cols + col;
+            if constexpr (ACCUMULATE) {
+                float old[8];
+                load8<true, ACCESS>(old, grad, at, 8u);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += old[e];
+            }
+            store8<true, ACCESS>(grad, at, 8u, v);
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 

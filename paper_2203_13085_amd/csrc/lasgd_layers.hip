@@ -136,7 +136,9 @@ template <class F> void two_flags(bool a, bool b, F f)
     }
 }
 
-// f(storage is bf16, Access) for a call whose accesses are aligned or not, and that moves so many bytes.  The hint from 256 MiB on, the size of the memory-side
+constexpr int64_t kBeyondCache = 256ll << 20;        // the memory-side cache
+
+// f(storage is bf16, Access) for a call whose accesses are aligned or not, and that moves so many bytes.  The hint beyond the memory-side
 // cache: dropout of 8 x 4096 x 2048 bf16, forward and backward, 79 us without and 67 with it (the median of the two); a norm with an
 // 8-bit output of 8 x 2048 x 4096 86 and 79; a norm's backward pass 139 and 137.  Below, what is written is still there for the next call.
 template <class F> void row_access(bool bf16, bool vec, int64_t bytes, F f)
@@ -146,7 +148,7 @@ template <class F> void row_access(bool bf16, bool vec, int64_t bytes, F f)
         else f(std::false_type{}, v);
     };
     if (!vec) storage(std::integral_constant<int, LOOSE>{});
-    else if (bytes < (256ll << 20)) storage(std::integral_constant<int, WIDE>{});
+    else if (bytes < kBeyondCache) storage(std::integral_constant<int, WIDE>{});
     else storage(std::integral_constant<int, STREAM>{});
 }
 
@@ -428,8 +430,8 @@ template <int FORM> uint64_t tiles_of(const Gated &d, int64_t cols, uint32_t tm,
 constexpr uint32_t kCus = 256;
 template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
 {
-    if (FORM == DX && d.r.most <= 16u) return 16u;
-    if (FORM == DX && d.r.most <= 64u) return 64u;
+    if (FORM != DW && d.r.most <= 16u) return 16u;
+    if (FORM != DW && d.r.most <= 64u) return 64u;
     return tiles_of<FORM>(d, cols, 256, FORM == FWD ? 128 : 256) >= 2 * kCus ? 256u : 128u;
 }
 
@@ -444,7 +446,7 @@ uint32_t dx_splits(const Gated &d, int64_t cols)
     return n < 1 ? 1u : n > 64 ? 64u : (uint32_t)n;
 }
 
-template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN>
+template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT = false>
 void launch_big(const Gated &d, const ProductArgs &a, uint32_t splits, float *part, hipStream_t st)
 {
     constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;
@@ -460,24 +462,30 @@ void launch_big(const Gated &d, const ProductArgs &a, uint32_t splits, float *pa
         total += tm * ceil_div(FORM == FWD ? a.wide : a.cols, NT) * (FORM == DW ? 2u : 1u);
     }
     map.first[d.v.K] = total;
-    hipLaunchKernelGGL((big_product_kernel<FORM, TM, TN, WM, WN>), dim3(total * splits), dim3(Big<FORM, TM, TN, WM, WN>::threads), 0, st, a, map);
+    hipLaunchKernelGGL((big_product_kernel<FORM, TM, TN, WM, WN, HINT>), dim3(total * splits), dim3(Big<FORM, TM, TN, WM, WN, HINT>::threads), 0, st, a, map);
 }
 
 template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, uint32_t splits, float *part, hipStream_t st)
 {
     if (!big) return launch_product<FORM>(d, a, vm, vn, st);
-    if constexpr (FORM == FWD) {
-        const dim3 grid(ceil_div(a.wide, 16), d.v.K);
-        if (d.r.most <= 64u) {
-            if (d.r.most <= 16u) hipLaunchKernelGGL((few_rows_kernel<1>), grid, dim3(256), 0, st, a);
-            else if (d.r.most <= 32u) hipLaunchKernelGGL((few_rows_kernel<2>), grid, dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((few_rows_kernel<4>), grid, dim3(256), 0, st, a);
+    if constexpr (FORM == DW) {
+        if (d.r.most <= kFewRows) {
+            const dim3 grid(ceil_div(a.wide, 256) * ceil_div(a.cols, 256), d.v.K, 2);
+            two_flags(a.accumulate, 4 * (uint64_t)d.v.K * a.wide * a.cols >= kBeyondCache, [&](auto add, auto stream) {
+                hipLaunchKernelGGL((few_rows_weights_kernel<add, stream ? STREAM : WIDE>), grid, dim3(256), 0, st, a);
+            });
             return;
         }
     }
     const uint32_t tm = tile_rows<FORM>(d, a.cols);
+    if constexpr (FORM == FWD) {
+        // Weights in the cache (K = 4, 1 row, 2048 x 5504, 180 MB): 28 us without the hint, 34 with it; beyond it (K = 8, 4 rows) 75 and 70.
+        const bool hint = 4 * (uint64_t)d.v.K * a.wide * a.cols >= kBeyondCache;
+        if (tm == 16u) return hint ? launch_big<FORM, 16, 128, 1, 4, true>(d, a, 1, nullptr, st) : launch_big<FORM, 16, 128, 1, 4>(d, a, 1, nullptr, st);
+        if (tm == 64u) return launch_big<FORM, 64, 128, 1, 4>(d, a, 1, nullptr, st);
+    }
     if constexpr (FORM == DX) {
-        if (tm == 16u) return launch_big<FORM, 16, 256, 1, 4>(d, a, splits, part, st);
+        if (tm == 16u) return launch_big<FORM, 16, 256, 1, 4, true>(d, a, splits, part, st);
         if (tm == 64u) return launch_big<FORM, 64, 256, 1, 4>(d, a, splits, part, st);
     }
     if (tm == 128u) launch_big<FORM, 128, 128, 2, 2>(d, a, splits, part, st);
