@@ -221,17 +221,20 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
     }
 }
 
-// ---- bf16, aligned, more rows than a few ------------------------------------------------------------------------------------------
-// Bound by the matrix cores.  A workgroup makes TM x TN of C, wave by wave, and takes the contraction kStep at a time through two buffers
-// in LDS: while the waves multiply one, the next is on its way from memory straight into the other.
+// ---- aligned ------------------------------------------------------------------------------------------------------------------------
+// Bound by the matrix cores.  A workgroup makes TM x TN of C, wave by wave, and takes the contraction a step (128 bytes: 64 elements of bf16, 32 of fp32)
+// at a time through two buffers in LDS: while the waves multiply one, the next is on its way from memory straight into the other.
 //   - A side whose contraction is contiguous in memory (ALONG) lies in LDS as [row][8 pieces of 16 bytes], piece p of row i at p ^ (i & 7), and is read 16
 //     bytes a lane: eight rows' equal pieces are in eight different places of 128 bytes.
-//   - A side whose rows are contiguous (ACROSS) lies as [contraction][T / 8 pieces], piece p of line c at p ^ 2 (c & 3), and is read by the transposing
-//     read: 16 lanes take 4 lines of 16 columns, and a lane gets one column of them.
+//   - A side whose rows are contiguous (ACROSS) lies as [contraction][T elements].  bf16: piece p of line c at p ^ 2 (c & 3), read by the transposing read: 16 lanes
+//     take 4 lines of 16 columns, and a lane gets one column of them.  fp32: piece p at p ^ 4 (c / 4 & 3), read an element a lane: the lines of
+//     the four quarters of a wave are in four different places.
 // What is outside is asked for beyond the end of a buffer resource, which gives zeros.
-constexpr uint32_t kStep = 64;
+template <bool BF16> struct Width {
+    static constexpr uint32_t bytes = BF16 ? 2 : 4, piece = 16u / bytes, step = 128u / bytes;        // of an element; elements
+};
 
-// A tile's place and how far what may be read reaches from there: T lines along, or kStep lines across.
+// A tile's place and how far what may be read reaches from there: T lines along, or a step's lines across.
 struct Side {
     const char *p;               // of the tile's first element
     int64_t bytes;               // from there to the end of what is there
@@ -244,11 +247,11 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ uint32_t records(int64_t bytes) { return bytes <= 0 ? 0u : bytes > 0xfffffff0ll ? 0xfffffff0u : (uint32_t)bytes; }
 
-// The next kStep of the contraction into LDS.  left: how much of it is still there (ALONG: beyond it the line goes on with something else).
-template <bool ALONG, uint32_t T, uint32_t THREADS, bool HINT = false>
+// The next step of the contraction into LDS.  left: how much of it is still there (ALONG: beyond it the line goes on with something else).
+template <bool BF16, bool ALONG, uint32_t T, uint32_t THREADS, bool HINT = false>
 __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left)
 {
-    constexpr uint32_t PIECES = T * kStep / 8u, LINE = ALONG ? kStep / 8u : T / 8u;
+    constexpr uint32_t PIECES = T * 8u, LINE = ALONG ? 8u : T / Width<BF16>::piece;
     static_assert(PIECES % 64u == 0, "whole waves");
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)s.p, 0, records(s.bytes), 0x00020000);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -256,36 +259,46 @@ __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left
     for (uint32_t i = 0; i < (PIECES + THREADS - 1u) / THREADS; ++i) {
         if ((i + 1u) * THREADS > PIECES && i * THREADS + wave * 64u >= PIECES) break;
         const uint32_t at = i * THREADS + threadIdx.x, line = at / LINE;
-        const uint32_t piece = at % LINE ^ (ALONG ? line & 7u : (line & 3u) * 2u);
+        const uint32_t piece = at % LINE ^ (ALONG ? line & 7u : BF16 ? (line & 3u) * 2u : (line & 12u));
         uint32_t off = line * (uint32_t)s.stride + piece * 16u;
-        if (ALONG && (int64_t)(piece * 8u) >= left) off = 0xfffffff0u;
+        if (ALONG && (int64_t)(piece * Width<BF16>::piece) >= left) off = 0xfffffff0u;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64u) * 16u), 16, off, 0, 0, HINT ? 2 : 0);
     }
 }
 
-// The 16 rows from row0 on, 32 of the contraction from c0 on: a lane has row lane % 16 and eight of the contraction, 8 (lane / 16) on.
-template <bool ALONG, uint32_t T>
-__device__ __forceinline__ bf16x8 fragment(const lds_char *lds, uint32_t row0, uint32_t c0)
+// What a lane has of 16 rows from row0 on and of the contraction from c0 on: row lane % 16, and of 32 (bf16: 16 bytes) or 16 (fp32) of the contraction
+// the share of its quarter of the wave.  Both sides take it in the same order, which is all that counts.
+template <bool BF16> struct Frag { typedef f32x4 type; };
+template <> struct Frag<true> { typedef bf16x8 type; };
+template <bool BF16, bool ALONG, uint32_t T>
+__device__ __forceinline__ typename Frag<BF16>::type fragment(const lds_char *lds, uint32_t row0, uint32_t c0)
 {
     const uint32_t lane = threadIdx.x & 63u, quad = lane >> 4, i = lane & 15u;
     if constexpr (ALONG) {
-        const uint32_t row = row0 + i, piece = (c0 / 8u + quad) ^ (row & 7u);
-        return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds + row * (kStep * 2u) + piece * 16u);
-    } else {
+        const uint32_t row = row0 + i, piece = (c0 / Width<BF16>::piece + quad) ^ (row & 7u);
+        return *reinterpret_cast<const __attribute__((address_space(3))) typename Frag<BF16>::type *>(lds + row * 128u + piece * 16u);
+    } else if constexpr (BF16) {
         const uint32_t line = c0 + quad * 8u + (i >> 2), piece = (row0 / 8u + ((i & 3u) >> 1)) ^ ((line & 3u) * 2u);
         const lds_char *at = lds + line * (T * 2u) + piece * 16u + (i & 1u) * 8u;            // four lines on: the same place in its line
         const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
         const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4u * T * 2u));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        const uint32_t line = c0 + quad * 4u, piece = ((row0 + i) / 4u) ^ (line & 12u);
+        const lds_char *at = lds + line * (T * 4u) + piece * 16u + (i & 3u) * 4u;
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const __attribute__((address_space(3))) float *>(at + e * T * 4u);
+        return v;
     }
 }
 
 // HINT: the weights are read with the streaming hint.
-template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT> struct Big {
+template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT> struct Big {
     static constexpr uint32_t threads = 64u * WM * WN;
     static constexpr bool along_m = FORM != DW, along_n = FORM == FWD;
     static constexpr uint32_t FM = TM / WM / 16u, FN = TN / WN / 16u;           // fragments of a wave
-    static constexpr uint32_t bytes = (TM + TN) * kStep * 2u;                  // of a buffer
+    static constexpr uint32_t bytes = (TM + TN) * 128u;                        // of a buffer
     static constexpr uint32_t cols_out = TN / WN / (FORM == FWD ? 2u : 1u);    // columns of C that a wave has
     static constexpr uint32_t part_rows = FM > 4u ? 64u : FM * 16u, part_pitch = TN / WN + 4u;     // of it, on its way out, in fp32
     static constexpr uint32_t out_bytes = WM * WN * part_rows * part_pitch * 4u;
@@ -293,11 +306,11 @@ template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HIN
 
     static __device__ __forceinline__ void fetch_both(lds_char *lds, const Side &m, const Side &n, const Side &n2, int64_t left)
     {
-        fetch<along_m, TM, threads>(lds, m, left);
+        fetch<BF16, along_m, TM, threads>(lds, m, left);
         if constexpr (FORM == FWD) {
-            fetch<true, TN / 2u, threads, HINT>(lds + TM * kStep * 2u, n, left);
-            fetch<true, TN / 2u, threads, HINT>(lds + (TM + TN / 2u) * kStep * 2u, n2, left);
-        } else fetch<along_n, TN, threads, HINT>(lds + TM * kStep * 2u, n, left);
+            fetch<BF16, true, TN / 2u, threads, HINT>(lds + TM * 128u, n, left);
+            fetch<BF16, true, TN / 2u, threads, HINT>(lds + (TM + TN / 2u) * 128u, n2, left);
+        } else fetch<BF16, along_n, TN, threads, HINT>(lds + TM * 128u, n, left);
     }
     // row of the n side's fragment j: a wave of FWD has the same columns of gate and up
     static __device__ __forceinline__ uint32_t n_row(uint32_t wn, uint32_t j)
@@ -308,16 +321,27 @@ template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HIN
     static __device__ __forceinline__ void multiply(f32x4 (&acc)[FM][FN], const lds_char *lds, uint32_t wm, uint32_t wn)
     {
 #pragma unroll
-        for (uint32_t c = 0; c < kStep; c += 32u) {
-            bf16x8 m[FM], n[FN];
+        for (uint32_t c = 0; c < Width<BF16>::step; c += Width<BF16>::step / 2u) {
+            typename Frag<BF16>::type m[FM], n[FN];
 #pragma unroll
-            for (uint32_t j = 0; j < FN; ++j) n[j] = fragment<along_n, TN>(lds + TM * kStep * 2u, n_row(wn, j), c);
+            for (uint32_t j = 0; j < FN; ++j) n[j] = fragment<BF16, along_n, TN>(lds + TM * 128u, n_row(wn, j), c);
 #pragma unroll
-            for (uint32_t i = 0; i < FM; ++i) m[i] = fragment<along_m, TM>(lds, wm * (TM / WM) + i * 16u, c);
+            for (uint32_t i = 0; i < FM; ++i) m[i] = fragment<BF16, along_m, TM>(lds, wm * (TM / WM) + i * 16u, c);
+            if constexpr (BF16) {
 #pragma unroll
-            for (uint32_t i = 0; i < FM; ++i) {
+                for (uint32_t i = 0; i < FM; ++i) {
 #pragma unroll
-                for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m[i], acc[i][j], 0, 0, 0);
+                    for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m[i], acc[i][j], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                    for (uint32_t i = 0; i < FM; ++i) {
+#pragma unroll
+                        for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(n[j][e], m[i][e], acc[i][j], 0, 0, 0);
+                    }
+                }
             }
         }
     }
@@ -330,11 +354,11 @@ template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HIN
     }
 };
 
-// Eight elements of bf16 or, where they may not be stored at once, as many as there are.
-__device__ __forceinline__ void store_some(char *p, int64_t at, bool at_once, uint32_t there, const float (&v)[8])
+// Eight elements or, where they may not be stored at once, as many as there are.
+template <bool BF16> __device__ __forceinline__ void store_some(char *p, int64_t at, bool at_once, uint32_t there, const float (&v)[8])
 {
-    if (at_once) store8<true, WIDE>(p, at, 8u, v);
-    else store8<true, LOOSE>(p, at, there, v);
+    if (at_once) store8<BF16, WIDE>(p, at, 8u, v);
+    else store8<BF16, LOOSE>(p, at, there, v);
 }
 
 struct TileMap {
@@ -352,10 +376,12 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total)
     return x * per + (x < more ? x : more) + (id >> 3);
 }
 
-template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT>
-__global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN, HINT>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)
+template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT>
+__global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, HINT>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)
 {
-    using S = Big<FORM, TM, TN, WM, WN, HINT>;
+    using S = Big<BF16, FORM, TM, TN, WM, WN, HINT>;
+    constexpr int ES = Width<BF16>::bytes;
+    constexpr uint32_t STEP = Width<BF16>::step;
     __shared__ __attribute__((aligned(1024))) char lds_mem[S::lds];
     lds_char *lds = (lds_char *)lds_mem;
     const uint32_t order = xcd_order(blockIdx.x, gridDim.x);
@@ -373,9 +399,9 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN, HINT>::threads)) void bi
     constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;                          // columns of C
     const int64_t m0 = (int64_t)(tile % tm) * TM, n0 = (int64_t)(tile / tm) * NT;
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WN, wn = w % WN;
-    const int64_t pitch = (int64_t)a.pitch * 2, width = (int64_t)cols * 2, xs = a.x.ss * 2;
+    const int64_t pitch = (int64_t)a.pitch * ES, width = (int64_t)cols * ES, xs = a.x.ss * ES;
     const uint64_t first = (uint64_t)a.first[k] * pitch;
-    const char *x = a.x.p + k * a.x.rs * 2;
+    const char *x = a.x.p + k * a.x.rs * ES;
     Side m, n, n2;
     int64_t deep;
     if constexpr (FORM == FWD) {
@@ -386,15 +412,15 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN, HINT>::threads)) void bi
     } else if constexpr (FORM == DX) {
         deep = a.pitch;
         m = Side{a.dg + first + m0 * pitch, (rows - m0) * pitch, pitch};
-        n = Side{a.gate[k] + n0 * 2, wide * width - n0 * 2, width};
+        n = Side{a.gate[k] + n0 * ES, wide * width - n0 * ES, width};
         n2 = n;
     } else {
         deep = rows;
-        m = Side{(second ? a.du : a.dg) + first + m0 * 2, rows * pitch - m0 * 2, pitch};
-        n = Side{x + n0 * 2, (rows - 1) * xs + width - n0 * 2, xs};
+        m = Side{(second ? a.du : a.dg) + first + m0 * ES, rows * pitch - m0 * ES, pitch};
+        n = Side{x + n0 * ES, (int64_t)(rows - 1) * xs + width - n0 * ES, xs};
         n2 = n;
     }
-    const uint32_t steps1 = (uint32_t)((deep + kStep - 1) / kStep), all = FORM == DX ? 2u * steps1 : steps1;
+    const uint32_t steps1 = (uint32_t)((deep + STEP - 1) / STEP), all = FORM == DX ? 2u * steps1 : steps1;
     const uint32_t begin = FORM == DX ? (uint32_t)((uint64_t)all * split / map.splits) : 0u;
     const uint32_t end = FORM == DX ? (uint32_t)((uint64_t)all * (split + 1u) / map.splits) : all;
     const int64_t to_du = FORM == DX ? a.du - a.dg : 0, to_up = FORM == DX ? a.up[k] - a.gate[k] : 0;
@@ -402,12 +428,12 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN, HINT>::threads)) void bi
     // step s's sides: DX goes through the first pair and then through the second
     auto side = [&](const Side &from, bool along, uint32_t s, int64_t to_second) {
         Side at = from;
-        const int64_t on = (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * (along ? kStep * 2 : kStep * from.stride);
+        const int64_t on = (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * (along ? 128 : STEP * from.stride);
         at.p += on + (FORM == DX && s >= steps1 ? to_second : 0);
         at.bytes -= on;
         return at;
     };
-    auto left = [&](uint32_t s) { return deep - (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * kStep; };
+    auto left = [&](uint32_t s) { return deep - (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * STEP; };
     if (begin < end) S::fetch_both(lds, side(m, S::along_m, begin, to_du), side(n, S::along_n, begin, to_up), side(n2, S::along_n, begin, 0), left(begin));
     for (uint32_t s = begin; s < end; ++s) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -446,24 +472,24 @@ __global__ __launch_bounds__((Big<FORM, TM, TN, WM, WN, HINT>::threads)) void bi
 #pragma unroll
                 for (int e = 0; e < 8; ++e) u[e] = from[S::cols_out + e];
                 if (a.g.p) {
-                    store_some(a.g.p, k * a.g.rs + row * a.g.ss + col, at_once, there, v);
-                    store_some(a.u.p, k * a.u.rs + row * a.u.ss + col, at_once, there, u);
+                    store_some<BF16>(a.g.p, k * a.g.rs + row * a.g.ss + col, at_once, there, v);
+                    store_some<BF16>(a.u.p, k * a.u.rs + row * a.u.ss + col, at_once, there, u);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = activation(a.act, v[e]).f * u[e];
-                store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
+                store_some<BF16>(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
             } else if constexpr (FORM == DX) {
                 if (map.splits > 1u) store8<false, WIDE>((char *)(map.part + split * map.part_stride), (int64_t)(a.first[k] + row) * cols + col, 8u, v);
-                else store_some(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
+                else store_some<BF16>(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
             } else {                                  // cols counts whole eights
                 char *grad = second ? a.up[k] : a.gate[k];
                 if (a.accumulate) {
                     float old[8];
-                    load8<true, WIDE>(old, grad, row * cols + col, 8u);
+                    load8<BF16, WIDE>(old, grad, row * cols + col, 8u);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] += old[e];
                 }
-                store8<true, WIDE>(grad, row * cols + col, 8u, v);
+                store8<BF16, WIDE>(grad, row * cols + col, 8u, v);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -480,7 +506,7 @@ struct JoinRowsArgs {
     uint32_t rows[64];
     uint32_t first[64];
 };
-template <int = 0>
+template <bool BF16>
 __global__ __launch_bounds__(256) void join_rows_kernel(const JoinRowsArgs a)
 {
     const uint32_t k = blockIdx.y, rows = a.rows[k], groups = a.cols / 8u;
@@ -496,7 +522,7 @@ __global__ __launch_bounds__(256) void join_rows_kernel(const JoinRowsArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += v[e];
             }
-            store_some(a.a.p, k * a.a.rs + (int64_t)r * a.a.ss + g * 8u, a.wide_out, 8u, sum);
+            store_some<BF16>(a.a.p, k * a.a.rs + (int64_t)r * a.a.ss + g * 8u, a.wide_out, 8u, sum);
         }
 }
 
@@ -529,11 +555,11 @@ __global__ __launch_bounds__(256) void few_rows_weights_kernel(const ProductArgs
     const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6, col = d0 + w * 64u + (lane & 7u) * 8u;
     bf16x8 n[4];
 #pragma unroll
-    for (uint32_t j = 0; j < 4u; ++j) n[j] = fragment<false, T>(model, w * 64u + j * 16u, 0);
+    for (uint32_t j = 0; j < 4u; ++j) n[j] = fragment<true, false, T>(model, w * 64u + j * 16u, 0);
 #pragma unroll 2
     for (uint32_t i = 0; i < T; i += 16u) {
         if (f0 + i >= wide) break;
-        const bf16x8 m = fragment<false, T>(hidden, i, 0);
+        const bf16x8 m = fragment<true, false, T>(hidden, i, 0);
 #pragma unroll
         for (uint32_t j = 0; j < 4u; ++j)
             *reinterpret_cast<f32x4 *>(&out[w][lane & 15u][j * 16u + (lane >> 4) * 4u]) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m, f32x4{}, 0, 0, 0);

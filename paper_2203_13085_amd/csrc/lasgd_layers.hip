@@ -411,11 +411,11 @@ template <int FORM> void launch_product(const Gated &d, const ProductArgs &a, bo
     });
 }
 
-// Whether a product's sides can go straight from memory into LDS: bf16, 16-byte pieces, a tile's lines within 32 bits of bytes.
+// Whether a product's sides can go straight from memory into LDS: 16-byte pieces, a tile's lines within 32 bits of bytes.
 bool streams(const Gated &d, int64_t cols, const RowsAt &x, bool vx)
 {
-    constexpr int64_t most = (1ll << 31) / 256 / 2;          // elements from one line to the next
-    return d.v.bf16 && vx && cols <= most && d.pitch <= most && x.ss <= most;
+    constexpr int64_t most = (1ll << 31) / 256 / 4;          // elements from one line to the next
+    return vx && cols <= most && d.pitch <= most && x.ss <= most;
 }
 
 // Tiles of all replicas.
@@ -438,9 +438,9 @@ template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
 // Workgroups that share a tile of dx: a contraction of 2 wide, and often few tiles.
 uint32_t dx_splits(const Gated &d, int64_t cols)
 {
-    if (!d.v.bf16 || !d.r.most) return 1;
+    if (!d.r.most) return 1;
     const uint32_t tm = tile_rows<DX>(d, cols), tn = tm == 128u ? 128u : 256u;
-    const uint64_t tiles = tiles_of<DX>(d, cols, tm, tn), steps = 2 * (uint64_t)ceil_div(d.pitch, kStep);
+    const uint64_t tiles = tiles_of<DX>(d, cols, tm, tn), steps = 2 * (uint64_t)ceil_div(d.pitch, 128 / d.es);
     const uint64_t want = (tm == 256u ? 2 * kCus : 4 * kCus) / tiles, most = steps / 4;
     const uint64_t n = want < most ? want : most;
     return n < 1 ? 1u : n > 64 ? 64u : (uint32_t)n;
@@ -462,14 +462,16 @@ void launch_big(const Gated &d, const ProductArgs &a, uint32_t splits, float *pa
         total += tm * ceil_div(FORM == FWD ? a.wide : a.cols, NT) * (FORM == DW ? 2u : 1u);
     }
     map.first[d.v.K] = total;
-    hipLaunchKernelGGL((big_product_kernel<FORM, TM, TN, WM, WN, HINT>), dim3(total * splits), dim3(Big<FORM, TM, TN, WM, WN, HINT>::threads), 0, st, a, map);
+    const dim3 grid(total * splits), threads(64u * WM * WN);
+    if (d.v.bf16) hipLaunchKernelGGL((big_product_kernel<true, FORM, TM, TN, WM, WN, HINT>), grid, threads, 0, st, a, map);
+    else hipLaunchKernelGGL((big_product_kernel<false, FORM, TM, TN, WM, WN, HINT>), grid, threads, 0, st, a, map);
 }
 
 template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, uint32_t splits, float *part, hipStream_t st)
 {
     if (!big) return launch_product<FORM>(d, a, vm, vn, st);
     if constexpr (FORM == DW) {
-        if (d.r.most <= kFewRows) {
+        if (d.v.bf16 && d.r.most <= kFewRows) {
             const dim3 grid(ceil_div(a.wide, 256) * ceil_div(a.cols, 256), d.v.K, 2);
             two_flags(a.accumulate, 4 * (uint64_t)d.v.K * a.wide * a.cols >= kBeyondCache, [&](auto add, auto stream) {
                 hipLaunchKernelGGL((few_rows_weights_kernel<add, stream ? STREAM : WIDE>), grid, dim3(256), 0, st, a);
@@ -480,7 +482,7 @@ template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool 
     const uint32_t tm = tile_rows<FORM>(d, a.cols);
     if constexpr (FORM == FWD) {
         // Weights in the cache (K = 4, 1 row, 2048 x 5504, 180 MB): 28 us without the hint, 34 with it; beyond it (K = 8, 4 rows) 75 and 70.
-        const bool hint = 4 * (uint64_t)d.v.K * a.wide * a.cols >= kBeyondCache;
+        const bool hint = 2 * (uint64_t)d.es * d.v.K * a.wide * a.cols >= kBeyondCache;
         if (tm == 16u) return hint ? launch_big<FORM, 16, 128, 1, 4, true>(d, a, 1, nullptr, st) : launch_big<FORM, 16, 128, 1, 4>(d, a, 1, nullptr, st);
         if (tm == 64u) return launch_big<FORM, 64, 128, 1, 4>(d, a, 1, nullptr, st);
     }
@@ -590,7 +592,9 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
             JoinRowsArgs j{out, part, (uint64_t)d.r.total * cols, splits, (uint32_t)cols, vo, {}, {}};
             copy_rows(j, d.r, d.v.K);
             memcpy(j.first, d.r.first, d.v.K * sizeof(uint32_t));
-            hipLaunchKernelGGL((join_rows_kernel<>), dim3(d.r.most < 4096u ? d.r.most : 4096u, d.v.K), dim3(256), 0, st, j);
+            const dim3 grid(d.r.most < 4096u ? d.r.most : 4096u, d.v.K);
+            if (d.v.bf16) hipLaunchKernelGGL((join_rows_kernel<true>), grid, dim3(256), 0, st, j);
+            else hipLaunchKernelGGL((join_rows_kernel<false>), grid, dim3(256), 0, st, j);
             TRY(launched(c));
         }
     }
