@@ -181,6 +181,11 @@ class Context:
         self._clip_arg = Clip()
         self._clip_ref = ctypes.byref(self._clip_arg)
         self._step_size = self._step_sizes = None
+        self._rows_seen = self._rows_arg = None
+        self._acts = [Rows() for _ in range(5)]
+        self._act_refs = [ctypes.byref(r) for r in self._acts]
+        self._drop_arg = Drop()
+        self._drop_ref = ctypes.byref(self._drop_arg)
         self.bound_grads = [None] * self.K        # per replica: the gradient addresses in effect (a ctypes array)
 
     # -- plumbing ---------------------------------------------------------
@@ -309,25 +314,36 @@ class Context:
     # -- layers: dropout, root-mean-square norms and gated blocks of all replicas -----------
     # rows: K counts.  An activation is (address, replica stride, row stride), strides in elements, or None where it may be absent.
     # The passes run on `stream` (a raw handle; None = the default stream).
+    # Short calls are bound by the host: counts are converted when they change, and the structures are made once and filled in.
     def _counts(self, rows):
-        assert len(rows) == self.K
-        return (ctypes.c_int64 * self.K)(*rows)
+        if rows != self._rows_seen:
+            assert len(rows) == self.K
+            self._rows_arg, self._rows_seen = (ctypes.c_int64 * self.K)(*rows), list(rows)
+        return self._rows_arg
 
-    @staticmethod
-    def _at(a):
-        return None if a is None else ctypes.byref(Rows(a[0], a[1], a[2]))
+    def _at(self, a, i: int):
+        if a is None:
+            return None
+        r = self._acts[i]
+        r.data, r.replica_stride, r.row_stride = a
+        return self._act_refs[i]
+
+    def _drop(self, p: float, seed: int, call: int, counter: Optional[int]):
+        d = self._drop_arg
+        d.p, d.seed, d.call, d.counter = p, seed, call, counter
+        return self._drop_ref
 
     def dropout(self, rows, cols: int, x, y, p: float, *, residual=None, seed: int = 0, call: int = 0,
                 counter: Optional[int] = None, stream: Optional[int] = None) -> None:
         """y = residual + drop(x).  counter: device address of 64 bits that are added to `call`."""
-        self._check(self._L.lasgd_dropout(self._h, self._counts(rows), cols, self._at(x), self._at(residual), self._at(y),
-                                          ctypes.byref(Drop(p, seed, call, counter)), stream or None))
+        self._check(self._L.lasgd_dropout(self._h, self._counts(rows), cols, self._at(x, 0), self._at(residual, 1), self._at(y, 2),
+                                          self._drop(p, seed, call, counter), stream or None))
 
     def rms_norm(self, gain: int, rows, x, y, *, residual=None, sum=None, scales=None, eps: float = 1e-6, p: float = 0.0,
                  seed: int = 0, call: int = 0, counter: Optional[int] = None, stream: Optional[int] = None) -> None:
         """sum = residual + drop(x), y = gain * sum / rms(sum); with scales (address, replica stride, row stride) y is e4m3."""
-        self._check(self._L.lasgd_rms_norm(self._h, gain, self._counts(rows), self._at(x), self._at(residual), self._at(sum),
-                                           self._at(y), self._at(scales), eps, ctypes.byref(Drop(p, seed, call, counter)), stream or None))
+        self._check(self._L.lasgd_rms_norm(self._h, gain, self._counts(rows), self._at(x, 0), self._at(residual, 1), self._at(sum, 2),
+                                           self._at(y, 3), self._at(scales, 4), eps, self._drop(p, seed, call, counter), stream or None))
 
     def rms_norm_backward_bytes(self, gain: int, rows) -> int:
         n = ctypes.c_int64(0)
@@ -337,15 +353,15 @@ class Context:
     def rms_norm_backward(self, gain: int, rows, h, dy, dx=None, *, dsum=None, dresidual=None, eps: float = 1e-6, p: float = 0.0,
                           seed: int = 0, call: int = 0, counter: Optional[int] = None, accumulate: bool = True,
                           workspace: Optional[int] = None, workspace_bytes: int = 0, stream: Optional[int] = None) -> None:
-        self._check(self._L.lasgd_rms_norm_backward(self._h, gain, self._counts(rows), self._at(h), self._at(dy), self._at(dsum),
-                                                    self._at(dresidual), self._at(dx), eps, ctypes.byref(Drop(p, seed, call, counter)),
+        self._check(self._L.lasgd_rms_norm_backward(self._h, gain, self._counts(rows), self._at(h, 0), self._at(dy, 1), self._at(dsum, 2),
+                                                    self._at(dresidual, 3), self._at(dx, 4), eps, self._drop(p, seed, call, counter),
                                                     int(bool(accumulate)), workspace or None, workspace_bytes, stream or None))
 
     def gated(self, gate: int, up: int, rows, cols: int, x, a, *, g=None, u=None, activation: int = SILU,
               stream: Optional[int] = None) -> None:
         """a = f(x Wg^T) * (x Wu^T); g and u are the two products, for the backward pass."""
-        self._check(self._L.lasgd_gated(self._h, gate, up, self._counts(rows), cols, self._at(x), self._at(g), self._at(u),
-                                        self._at(a), activation, stream or None))
+        self._check(self._L.lasgd_gated(self._h, gate, up, self._counts(rows), cols, self._at(x, 0), self._at(g, 1), self._at(u, 2),
+                                        self._at(a, 3), activation, stream or None))
 
     def gated_backward_bytes(self, gate: int, up: int, rows, cols: int) -> int:
         n = ctypes.c_int64(0)
@@ -355,8 +371,8 @@ class Context:
     def gated_backward(self, gate: int, up: int, rows, cols: int, x, g, u, da, dx=None, *, activation: int = SILU,
                        accumulate: bool = True, workspace: Optional[int] = None, workspace_bytes: int = 0,
                        stream: Optional[int] = None) -> None:
-        self._check(self._L.lasgd_gated_backward(self._h, gate, up, self._counts(rows), cols, self._at(x), self._at(g), self._at(u),
-                                                 self._at(da), self._at(dx), activation, int(bool(accumulate)), workspace or None,
+        self._check(self._L.lasgd_gated_backward(self._h, gate, up, self._counts(rows), cols, self._at(x, 0), self._at(g, 1), self._at(u, 2),
+                                                 self._at(da, 3), self._at(dx, 4), activation, int(bool(accumulate)), workspace or None,
                                                  workspace_bytes, stream or None))
 
     def read_state(self, which: int, k: int = 0, tensor: int = -1) -> np.ndarray:

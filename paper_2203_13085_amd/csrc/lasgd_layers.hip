@@ -56,7 +56,7 @@ lasgd_status check_device(lasgd_ctx *c, const ContextView &v)
 lasgd_status check_rows(lasgd_ctx *c, const ContextView &v, const Rows &r, const char *name, const lasgd_rows *a, int64_t cols, int es, bool output,
                         RowsAt &at, bool &vec)
 {
-    CHECK(a && a->data, LASGD_ERR_INVALID, "NULL %s", name);
+    CHECK(a && (a->data || !r.most), LASGD_ERR_INVALID, "NULL %s", name);
     at = RowsAt{(char *)a->data, v.K > 1 ? a->replica_stride : 0, r.most > 1 ? a->row_stride : 0};
     CHECK((uintptr_t)a->data % es == 0, LASGD_ERR_INVALID, "%s is not aligned to its elements", name);
     CHECK(at.rs >= 0 && at.ss >= 0, LASGD_ERR_INVALID, "%s has a negative stride", name);

@@ -16,6 +16,9 @@ change; clear them with `zero_grad()` of this class (or
 With `max_grad_norm` every local update clips: each replica's gradients count times min(1, max_grad_norm / (norm + 1e-6)), the
 norm taken over all its parameters, inside the update and without writing the gradients.  `clip_grad_norm_()` scales them
 in place, for a program that updates by itself.
+
+For replicas that run in step, activations [K, ..., columns], `dropout()`, `rms_norm()`, `rms_norm_8bit()` and `gated()` compute a layer of all of them
+in one call, forward and backward, with each replica's own bound weights; the weights' gradients are added to the attached buffers.
 """
 from __future__ import annotations
 
@@ -26,6 +29,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from . import torch_layers as L
 
 
 def _load_walk():
@@ -50,7 +54,7 @@ class LASGD:
     def __init__(self, replicas: Sequence[torch.nn.Module], lr: float, momentum: float = 0.9,
                  nesterov: bool = True, weight_decay: float = 0.0, m: int = 1,
                  no_decay_1d: bool = False, side_stream: bool = True, max_grad_norm: Optional[float] = None,
-                 skip_nonfinite: bool = False):
+                 skip_nonfinite: bool = False, seed: int = 0):
         """replicas: K modules with identical parameter lists on the same GPU, already
         holding the same initial weights (every node starts from the same model).
         m: local steps per global update (tau_max with the early exit disabled).
@@ -58,7 +62,8 @@ class LASGD:
         max_grad_norm: clip every replica's gradients to this norm in step() (None: no clipping; infinity: take the norms only);
         step() then leaves the norms before clipping in `grad_norms`, a tensor of K floats on the GPU.
         skip_nonfinite (with max_grad_norm): a replica whose gradients hold an infinity or a NaN takes no local update in
-        that step, and keeps its momentum; it still takes part in a global update."""
+        that step, and keeps its momentum; it still takes part in a global update.
+        seed: key of the dropout masks, 64 bits."""
         assert len(replicas) >= 1 and m >= 1
         assert max_grad_norm is None or max_grad_norm >= 0.0
         assert max_grad_norm is not None or not skip_nonfinite, "skip_nonfinite needs a max_grad_norm (infinity: no limit)"
@@ -80,7 +85,10 @@ class LASGD:
         self.max_grad_norm = None if max_grad_norm is None else float(max_grad_norm)
         self.skip_nonfinite = bool(skip_nonfinite)
         self.grad_norms = torch.zeros(len(self.replicas), device=dev)
-        self.device = dev
+        self.device, self.dtype = dev, dtype
+        self._names = [n for n, p in self.replicas[0].named_parameters() if p.requires_grad]
+        self.seed, self._masks = int(seed), 0
+        self.mask_counter = torch.zeros(1, dtype=torch.int64, device=dev)        # added to the call numbers of recorded masks
         self.main = torch.cuda.Stream(device=dev)
         self.side = torch.cuda.Stream(device=dev) if side_stream else self.main
         wd = [0.0 if (no_decay_1d and p.dim() <= 1) else float(weight_decay) for p in first]
@@ -174,6 +182,97 @@ class LASGD:
             return
         for p in self._flat:
             assert p.grad is not None, "a gradient buffer was dropped (use zero_grad(set_to_none=False))"
+
+    # ---- layers of all replicas ------------------------------------------------------------------------------------------
+    # x: [K, ..., columns] of the replicas' type, row by row; a weight: its name in named_parameters(), or its index among the trainable
+    # parameters.  rows: how many of each replica's rows (of [K, rows, columns]) there are, None: all; the outputs' others are zeros, and
+    # nothing flows back through them.  They run on the current stream.  A backward pass takes the weights as they are when it runs, so
+    # step() comes after it, and adds their gradients to the buffers that __init__ attached, past autograd.
+    #
+    # Masks: every dropout takes the next call number (`call`: another one, as for a forward pass that is run again).  A recorded call's number is fixed,
+    # and `mask_counter` is added to it, forward and backward: move it on by the number of dropouts before each replay.
+    def _tensor(self, name) -> int:
+        if isinstance(name, str):
+            if name not in self._names:
+                raise KeyError(f"no trainable parameter {name!r}")
+            return self._names.index(name)
+        if not 0 <= int(name) < len(self._names):
+            raise KeyError(f"no parameter {name}")
+        return int(name)
+
+    def _grads_to_add_to(self, t: int) -> List[torch.Tensor]:
+        grads = [ps[t].grad for ps in self.params]
+        for k, g in enumerate(grads):
+            if g is None or g.data_ptr() != self.ctx.bound_grads[k][t] or g.dtype != self.dtype or not g.is_contiguous():
+                raise RuntimeError("a gradient is not the buffer that was bound (use zero_grad(set_to_none=False))")
+        return grads
+
+    def _trainable(self, *tensors: int) -> None:
+        if torch.is_grad_enabled() and not all(ps[t].requires_grad for ps in self.params for t in tensors):
+            raise RuntimeError("a parameter was frozen after it was bound: its gradient would be added all the same (use no_grad)")
+
+    def _drop(self, p: float, call: Optional[int]) -> dict:
+        if not p:
+            return dict(p=0.0)
+        if call is None:
+            call, self._masks = self._masks, self._masks + 1
+        recorded = torch.cuda.is_current_stream_capturing()
+        return dict(p=float(p), seed=self.seed, call=call, counter=self.mask_counter.data_ptr() if recorded else None)
+
+    def dropout(self, x: torch.Tensor, p: float, residual: Optional[torch.Tensor] = None, *, rows: Optional[Sequence[int]] = None,
+                call: Optional[int] = None) -> torch.Tensor:
+        """residual + drop(x); a mask of its own for each replica, which is made again in the backward pass."""
+        r = L.Rows(self, x.shape, rows)
+        self._same_shape(x, residual)
+        return L.Dropout.apply(self, r, x, residual, self._drop(p, call))
+
+    def rms_norm(self, gain, x: torch.Tensor, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-6, p: float = 0.0,
+                 rows: Optional[Sequence[int]] = None, call: Optional[int] = None):
+        """gain * h / rms(h) with h = residual + drop(x).  With a residual: (that, h), h being the next residual."""
+        t = self._tensor(gain)
+        r = L.Rows(self, x.shape, rows)
+        self._same_shape(x, residual)
+        self._same_columns(x, t, 1)
+        self._trainable(t)
+        return L.RmsNorm.apply(self, r, t, x, residual, L._anchor(self), float(eps), self._drop(p, call), residual is not None)
+
+    @torch.no_grad()
+    def rms_norm_8bit(self, gain, x: torch.Tensor, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
+                      rows: Optional[Sequence[int]] = None):
+        """The norm in e4m3 with a scale for each row, y = q * scale: (q, scales), and h with a residual.  Without a backward pass."""
+        t = self._tensor(gain)
+        r = L.Rows(self, x.shape, rows)
+        self._same_shape(x, residual)
+        self._same_columns(x, t, 1)
+        v = r.view(self, x, "x")
+        res = None if residual is None else r.view(self, residual, "residual")
+        q, scales = r.new(v, x.shape[-1], torch.uint8), r.new(v, 1, torch.float32)
+        h = None if res is None else r.new(v, x.shape[-1])
+        with torch.cuda.device(self.device):
+            self.ctx.rms_norm(t, r.counts, L._at(v), L._at(q), residual=L._at(res), sum=L._at(h), scales=L._at(scales), eps=float(eps),
+                              stream=L._stream(self))
+        out = q.view(torch.float8_e4m3fn).view(x.shape), scales.view(*x.shape[:-1], 1)
+        return out if h is None else (*out, h.view(x.shape))
+
+    def gated(self, gate, up, x: torch.Tensor, activation: str = "silu", *, rows: Optional[Sequence[int]] = None) -> torch.Tensor:
+        """f(x Wg^T) * (x Wu^T); weights [wide, columns].  One name for both: a weight [2 wide, columns], the gate's rows first."""
+        g, u = self._tensor(gate), self._tensor(up)
+        r = L.Rows(self, x.shape, rows)
+        self._same_columns(x, g, 2)
+        self._same_columns(x, u, 2)
+        self._trainable(g, u)
+        if activation not in L.ACTIVATIONS:
+            raise ValueError(f"activation {activation!r} is none of {sorted(L.ACTIVATIONS)}")
+        return L.Gated.apply(self, r, g, u, x, L._anchor(self), L.ACTIVATIONS[activation])
+
+    def _same_shape(self, x: torch.Tensor, residual: Optional[torch.Tensor]) -> None:
+        if residual is not None and residual.shape != x.shape:
+            raise ValueError(f"x is {tuple(x.shape)}, the residual {tuple(residual.shape)}")
+
+    def _same_columns(self, x: torch.Tensor, t: int, dims: int) -> None:
+        w = self.params[0][t]
+        if w.dim() != dims or w.shape[-1] != x.shape[-1]:
+            raise ValueError(f"{self._names[t]} is {tuple(w.shape)}, x has {x.shape[-1]} columns")
 
     @torch.no_grad()
     def step(self, lr: Optional[float] = None) -> bool:
