@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "lasgd.hip")
@@ -21,11 +22,19 @@ FLAGS = [
 
 
 def build_hip(verbose: bool = False) -> str:
+    """Both translation units at the same time, then the library."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + ["-parallel-jobs=2", "-o", LIB, SRC, LAYERS_SRC]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    with tempfile.TemporaryDirectory() as d:
+        objs = [os.path.join(d, f"{i}.o") for i in range(2)]
+        cmds = [[hipcc] + [f for f in FLAGS if f != "-shared"] + ["-c", "-o", o, src] for o, src in zip(objs, (SRC, LAYERS_SRC))]
+        link = [hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB, *objs]
+        if verbose:
+            print("\n".join(" ".join(c) for c in (*cmds, link)), flush=True)
+        running = [subprocess.Popen(c) for c in cmds]
+        for code, c in zip([r.wait() for r in running], cmds):
+            if code:
+                raise subprocess.CalledProcessError(code, c)
+        subprocess.check_call(link)
     return LIB
 
 

@@ -13,12 +13,20 @@ struct ActPair {
     float f, slope;
 };
 
+// 1 / (1 + exp(-v)).  BF16: by the two instructions for it, some roundings of 2^-24 (and of v's size, where the result is small) off, which the rounding to 8
+// bits that follows hides; exact division and exponential took a product's epilogue TIME_E.
+template <bool BF16> __device__ __forceinline__ float sigmoid(float v)
+{
+    if constexpr (BF16) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * v));
+    else return 1.f / (1.f + expf(-v));
+}
+
 // The activation and its slope, in 32 bits.
-__device__ __forceinline__ ActPair activation(int act, float v)
+template <bool BF16> __device__ __forceinline__ ActPair activation(int act, float v)
 {
     switch (act) {
     case ACT_SILU: {
-        const float s = 1.f / (1.f + expf(-v));
+        const float s = sigmoid<BF16>(v);
         return {v * s, s * __builtin_fmaf(v, 1.f - s, 1.f)};
     }
     case ACT_GELU: {
@@ -58,7 +66,7 @@ __global__ __launch_bounds__(256) void gates_backward_kernel(const GatesArgs a)
             load8<BF16, VEC>(dv, a.da.p, k * a.da.rs + (int64_t)r * a.da.ss + c, n);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const ActPair f = activation(a.act, gv[j]);
+                const ActPair f = activation<BF16>(a.act, gv[j]);
                 gv[j] = dv[j] * uv[j] * f.slope;
                 uv[j] = dv[j] * f.f;
             }
@@ -203,7 +211,7 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
                 if (n >= N) continue;
                 if constexpr (FORM == FWD) {
                     const float g = acc[0][i][j][e], u = acc[1][i][j][e];
-                    store1<BF16>(a.a.p, k * a.a.rs + m * a.a.ss + n, activation(a.act, g).f * u);
+                    store1<BF16>(a.a.p, k * a.a.rs + m * a.a.ss + n, activation<BF16>(a.act, g).f * u);
                     if (a.g.p) {
                         store1<BF16>(a.g.p, k * a.g.rs + m * a.g.ss + n, g);
                         store1<BF16>(a.u.p, k * a.u.rs + m * a.u.ss + n, u);
@@ -222,17 +230,20 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
 }
 
 // ---- aligned ------------------------------------------------------------------------------------------------------------------------
-// Bound by the matrix cores.  A workgroup makes TM x TN of C, wave by wave, and takes the contraction a step (128 bytes: 64 elements of bf16, 32 of fp32)
-// at a time through two buffers in LDS: while the waves multiply one, the next is on its way from memory straight into the other.
-//   - A side whose contraction is contiguous in memory (ALONG) lies in LDS as [row][8 pieces of 16 bytes], piece p of row i at p ^ (i & 7), and is read 16
-//     bytes a lane: eight rows' equal pieces are in eight different places of 128 bytes.
-//   - A side whose rows are contiguous (ACROSS) lies as [contraction][T elements].  bf16: piece p of line c at p ^ 2 (c & 3), read by the transposing read: 16 lanes
-//     take 4 lines of 16 columns, and a lane gets one column of them.  fp32: piece p at p ^ 4 (c / 4 & 3), read an element a lane: the lines of
-//     the four quarters of a wave are in four different places.
+// Bound by the matrix cores.  A workgroup makes TM x TN of C, wave by wave, and takes the contraction a step (LP pieces of 16 bytes) at a time through NS
+// buffers in LDS: while the waves multiply one, the next ones are on their way from memory straight into the others.
+//   - A side whose contraction is contiguous in memory (ALONG) lies in LDS as [row][LP pieces], and is read 16 bytes a lane.  Piece p of row i is
+//     at p ^ (i & 7), or p ^ (i / 2 & 3) where a step has four: eight rows' equal pieces are in eight different places of 128 bytes.
+//   - A side whose rows are contiguous (ACROSS) lies as [contraction][T elements].  bf16: read by the transposing read, 16 lanes of which take 4 lines of 16
+//     columns, and a lane gets one column of them; piece p of line c is at p ^ 2 (c & 3) ^ (c & 8), so that the 8 lines that half a wave reads
+//     are in eight different places of 256 bytes.  fp32: read an element a lane; p ^ (c & 12): the four lines of a wave are in four different places.
 // What is outside is asked for beyond the end of a buffer resource, which gives zeros.
 template <bool BF16> struct Width {
-    static constexpr uint32_t bytes = BF16 ? 2 : 4, piece = 16u / bytes, step = 128u / bytes;        // of an element; elements
+    static constexpr uint32_t bytes = BF16 ? 2 : 4, piece = 16u / bytes, deep = 4u * piece;        // of an element; elements; a fragment's contraction
 };
+// Where piece p of a line is.
+template <uint32_t LP> __device__ __forceinline__ uint32_t along_place(uint32_t row, uint32_t p) { return p ^ (LP == 8u ? row & 7u : row >> 1 & 3u); }
+template <bool BF16> __device__ __forceinline__ uint32_t across_place(uint32_t line, uint32_t p) { return p ^ (BF16 ? (line & 3u) * 2u ^ (line & 8u) : line & 12u); }
 
 // A tile's place and how far what may be read reaches from there: T lines along, or a step's lines across.
 struct Side {
@@ -248,10 +259,10 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ uint32_t records(int64_t bytes) { return bytes <= 0 ? 0u : bytes > 0xfffffff0ll ? 0xfffffff0u : (uint32_t)bytes; }
 
 // The next step of the contraction into LDS.  left: how much of it is still there (ALONG: beyond it the line goes on with something else).
-template <bool BF16, bool ALONG, uint32_t T, uint32_t THREADS, bool HINT = false>
+template <bool BF16, uint32_t LP, bool ALONG, uint32_t T, uint32_t THREADS, bool HINT = false>
 __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left)
 {
-    constexpr uint32_t PIECES = T * 8u, LINE = ALONG ? 8u : T / Width<BF16>::piece;
+    constexpr uint32_t PIECES = T * LP, LINE = ALONG ? LP : T / Width<BF16>::piece;
     static_assert(PIECES % 64u == 0, "whole waves");
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)s.p, 0, records(s.bytes), 0x00020000);
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -259,7 +270,7 @@ __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left
     for (uint32_t i = 0; i < (PIECES + THREADS - 1u) / THREADS; ++i) {
         if ((i + 1u) * THREADS > PIECES && i * THREADS + wave * 64u >= PIECES) break;
         const uint32_t at = i * THREADS + threadIdx.x, line = at / LINE;
-        const uint32_t piece = at % LINE ^ (ALONG ? line & 7u : BF16 ? (line & 3u) * 2u : (line & 12u));
+        const uint32_t piece = ALONG ? along_place<LP>(line, at % LINE) : across_place<BF16>(line, at % LINE);
         uint32_t off = line * (uint32_t)s.stride + piece * 16u;
         if (ALONG && (int64_t)(piece * Width<BF16>::piece) >= left) off = 0xfffffff0u;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64u) * 16u), 16, off, 0, 0, HINT ? 2 : 0);
@@ -270,21 +281,21 @@ __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left
 // the share of its quarter of the wave.  Both sides take it in the same order, which is all that counts.
 template <bool BF16> struct Frag { typedef f32x4 type; };
 template <> struct Frag<true> { typedef bf16x8 type; };
-template <bool BF16, bool ALONG, uint32_t T>
+template <bool BF16, uint32_t LP, bool ALONG, uint32_t T>
 __device__ __forceinline__ typename Frag<BF16>::type fragment(const lds_char *lds, uint32_t row0, uint32_t c0)
 {
     const uint32_t lane = threadIdx.x & 63u, quad = lane >> 4, i = lane & 15u;
     if constexpr (ALONG) {
-        const uint32_t row = row0 + i, piece = (c0 / Width<BF16>::piece + quad) ^ (row & 7u);
-        return *reinterpret_cast<const __attribute__((address_space(3))) typename Frag<BF16>::type *>(lds + row * 128u + piece * 16u);
+        const uint32_t row = row0 + i, piece = along_place<LP>(row, c0 / Width<BF16>::piece + quad);
+        return *reinterpret_cast<const __attribute__((address_space(3))) typename Frag<BF16>::type *>(lds + row * (LP * 16u) + piece * 16u);
     } else if constexpr (BF16) {
-        const uint32_t line = c0 + quad * 8u + (i >> 2), piece = (row0 / 8u + ((i & 3u) >> 1)) ^ ((line & 3u) * 2u);
+        const uint32_t line = c0 + quad * 8u + (i >> 2), piece = across_place<true>(line, row0 / 8u + ((i & 3u) >> 1));
         const lds_char *at = lds + line * (T * 2u) + piece * 16u + (i & 1u) * 8u;            // four lines on: the same place in its line
         const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
         const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4u * T * 2u));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-        const uint32_t line = c0 + quad * 4u, piece = ((row0 + i) / 4u) ^ (line & 12u);
+        const uint32_t line = c0 + quad * 4u, piece = across_place<false>(line, (row0 + i) / 4u);
         const lds_char *at = lds + line * (T * 4u) + piece * 16u + (i & 3u) * 4u;
         f32x4 v;
 #pragma unroll
@@ -294,23 +305,30 @@ __device__ __forceinline__ typename Frag<BF16>::type fragment(const lds_char *ld
 }
 
 // HINT: the weights are read with the streaming hint.
-template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT> struct Big {
+template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, uint32_t LP, uint32_t NS, bool HINT> struct Big {
     static constexpr uint32_t threads = 64u * WM * WN;
     static constexpr bool along_m = FORM != DW, along_n = FORM == FWD;
     static constexpr uint32_t FM = TM / WM / 16u, FN = TN / WN / 16u;           // fragments of a wave
-    static constexpr uint32_t bytes = (TM + TN) * 128u;                        // of a buffer
+    static constexpr uint32_t bytes = (TM + TN) * LP * 16u, n_at = TM * LP * 16u;            // of a buffer, and where the n side is in it
+    static constexpr uint32_t step = LP * Width<BF16>::piece;                  // elements of the contraction
     static constexpr uint32_t cols_out = TN / WN / (FORM == FWD ? 2u : 1u);    // columns of C that a wave has
     static constexpr uint32_t part_rows = FM > 4u ? 64u : FM * 16u, part_pitch = TN / WN + 4u;     // of it, on its way out, in fp32
     static constexpr uint32_t out_bytes = WM * WN * part_rows * part_pitch * 4u;
-    static constexpr uint32_t lds = 2u * bytes > out_bytes ? 2u * bytes : out_bytes;
+    static constexpr uint32_t lds = NS * bytes > out_bytes ? NS * bytes : out_bytes;
+    // loads a step of a wave: whole rounds, and one more of the first `more` waves where a side has less than a round
+    static constexpr uint32_t sides[3] = {TM * LP, FORM == FWD ? TN / 2u * LP : TN * LP, FORM == FWD ? TN / 2u * LP : 0u};
+    static constexpr uint32_t rounds = sides[0] / threads + sides[1] / threads + sides[2] / threads;
+    static constexpr uint32_t more = sides[0] % threads / 64u;
+    static_assert(sides[1] % threads == 0 && sides[2] % threads == 0 && sides[0] % 64u == 0, "whole waves");
+    static_assert(lds <= 163840u && (NS - 2u) * (rounds + 1u) < 64u, "LDS; what the counter of loads holds");
 
     static __device__ __forceinline__ void fetch_both(lds_char *lds, const Side &m, const Side &n, const Side &n2, int64_t left)
     {
-        fetch<BF16, along_m, TM, threads>(lds, m, left);
+        fetch<BF16, LP, along_m, TM, threads>(lds, m, left);
         if constexpr (FORM == FWD) {
-            fetch<BF16, true, TN / 2u, threads, HINT>(lds + TM * 128u, n, left);
-            fetch<BF16, true, TN / 2u, threads, HINT>(lds + (TM + TN / 2u) * 128u, n2, left);
-        } else fetch<BF16, along_n, TN, threads, HINT>(lds + TM * 128u, n, left);
+            fetch<BF16, LP, true, TN / 2u, threads, HINT>(lds + n_at, n, left);
+            fetch<BF16, LP, true, TN / 2u, threads, HINT>(lds + n_at + TN / 2u * LP * 16u, n2, left);
+        } else fetch<BF16, LP, along_n, TN, threads, HINT>(lds + n_at, n, left);
     }
     // row of the n side's fragment j: a wave of FWD has the same columns of gate and up
     static __device__ __forceinline__ uint32_t n_row(uint32_t wn, uint32_t j)
@@ -321,12 +339,12 @@ template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t W
     static __device__ __forceinline__ void multiply(f32x4 (&acc)[FM][FN], const lds_char *lds, uint32_t wm, uint32_t wn)
     {
 #pragma unroll
-        for (uint32_t c = 0; c < Width<BF16>::step; c += Width<BF16>::step / 2u) {
+        for (uint32_t c = 0; c < step; c += Width<BF16>::deep) {
             typename Frag<BF16>::type m[FM], n[FN];
 #pragma unroll
-            for (uint32_t j = 0; j < FN; ++j) n[j] = fragment<BF16, along_n, TN>(lds + TM * 128u, n_row(wn, j), c);
+            for (uint32_t j = 0; j < FN; ++j) n[j] = fragment<BF16, LP, along_n, TN>(lds + n_at, n_row(wn, j), c);
 #pragma unroll
-            for (uint32_t i = 0; i < FM; ++i) m[i] = fragment<BF16, along_m, TM>(lds, wm * (TM / WM) + i * 16u, c);
+            for (uint32_t i = 0; i < FM; ++i) m[i] = fragment<BF16, LP, along_m, TM>(lds, wm * (TM / WM) + i * 16u, c);
             if constexpr (BF16) {
 #pragma unroll
                 for (uint32_t i = 0; i < FM; ++i) {
@@ -343,14 +361,35 @@ template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t W
                     }
                 }
             }
+            // The order of a fragment's worth: enough reads to begin with, then one after every FN products, four rows of fragments ahead.
+            if constexpr (BF16 && FM > 4u) {
+                constexpr int NB = along_n ? 1 : 2, MB = along_m ? 1 : 2;
+                __builtin_amdgcn_sched_group_barrier(0x100, FN * NB + 4 * MB, 0);
+#pragma unroll
+                for (uint32_t i = 4; i < FM; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, FN, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, MB, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, 4 * FN, 0);
+            }
         }
     }
-    // cur is read while next is written: told apart by restrict, or every read would wait for the loads into next.
-    static __device__ __forceinline__ void step(f32x4 (&acc)[FM][FN], const lds_char *__restrict__ cur, lds_char *__restrict__ next, const Side &m,
-                                                const Side &n, const Side &n2, int64_t left, bool more, uint32_t wm, uint32_t wn)
+    // The step in cur is there once no more than the loads of the NS - 2 steps behind it are on their way; and every wave is done with the step before.
+    static __device__ __forceinline__ void arrive(uint32_t wave)
     {
-        if (more) fetch_both(next, m, n, n2, left);
-        multiply(acc, cur, wm, wn);
+        if (more && wave < more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2u) * (rounds + 1u)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2u) * rounds) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+    // cur is read while far is written: told apart by restrict, or every read would wait for all loads into LDS.  One place in the code for both, also for
+    // the first loads, which nothing is multiplied beside, or they would not be told apart.
+    static __device__ __forceinline__ void turn(f32x4 (&acc)[FM][FN], const lds_char *__restrict__ cur, lds_char *__restrict__ far, const Side &m,
+                                                const Side &n, const Side &n2, int64_t left, bool ready, uint32_t wm, uint32_t wn)
+    {
+        fetch_both(far, m, n, n2, left);
+        __builtin_amdgcn_sched_barrier(0);
+        if (ready) multiply(acc, cur, wm, wn);
     }
 };
 
@@ -364,10 +403,13 @@ template <bool BF16> __device__ __forceinline__ void store_some(char *p, int64_t
 struct TileMap {
     uint32_t first[65];          // tiles of the replicas before, and of all
     uint32_t replicas;
-    uint32_t splits;             // workgroups that share a tile's contraction (DX)
+    uint32_t splits, per_split;  // workgroups that share a tile's contraction (DX), and the steps of each
     float *part;                 // more than one: what each of them has, [splits][rows of all replicas][cols]
     uint64_t part_stride;        // elements from one split to the next
 };
+
+// A quotient: divisions are made by the vector unit, and what comes of one stays in vector registers, with all that is computed from it.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // Workgroups are dealt out to the eight XCDs in turn; each XCD gets tiles that follow each other, which share their sides in its L2.
 __device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total)
@@ -376,17 +418,17 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total)
     return x * per + (x < more ? x : more) + (id >> 3);
 }
 
-template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT>
-__global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, HINT>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)
+template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, uint32_t LP, uint32_t NS, bool HINT>
+__global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, LP, NS, HINT>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)
 {
-    using S = Big<BF16, FORM, TM, TN, WM, WN, HINT>;
+    using S = Big<BF16, FORM, TM, TN, WM, WN, LP, NS, HINT>;
     constexpr int ES = Width<BF16>::bytes;
-    constexpr uint32_t STEP = Width<BF16>::step;
+    constexpr uint32_t STEP = S::step;
     __shared__ __attribute__((aligned(1024))) char lds_mem[S::lds];
     lds_char *lds = (lds_char *)lds_mem;
     const uint32_t order = xcd_order(blockIdx.x, gridDim.x);
     const uint32_t tiles = map.first[map.replicas];
-    const uint32_t id = FORM == DX ? order % tiles : order, split = FORM == DX ? order / tiles : 0u;
+    const uint32_t split = FORM == DX ? uniform(order / tiles) : 0u, id = FORM == DX ? order - split * tiles : order;
     uint32_t k = 0;
     for (uint32_t half = 32u; half; half >>= 1)
         if (k + half < map.replicas && map.first[k + half] <= id) k += half;
@@ -397,7 +439,8 @@ __global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, HINT>::threads)) v
     const bool second = FORM == DW && tile >= tm * ((N + TN - 1u) / TN);         // DW: first all of the gate's gradient, then up's
     if (second) tile -= tm * ((N + TN - 1u) / TN);
     constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;                          // columns of C
-    const int64_t m0 = (int64_t)(tile % tm) * TM, n0 = (int64_t)(tile / tm) * NT;
+    const uint32_t tile_n = uniform(tile / tm), tile_m = tile - tile_n * tm;
+    const int64_t m0 = (int64_t)tile_m * TM, n0 = (int64_t)tile_n * NT;
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WN, wn = w % WN;
     const int64_t pitch = (int64_t)a.pitch * ES, width = (int64_t)cols * ES, xs = a.x.ss * ES;
     const uint64_t first = (uint64_t)a.first[k] * pitch;
@@ -406,7 +449,7 @@ __global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, HINT>::threads)) v
     int64_t deep;
     if constexpr (FORM == FWD) {
         deep = cols;
-        m = Side{x + m0 * xs, (rows - 1 - m0) * xs + width, xs};
+        m = Side{x + m0 * xs, ((int64_t)rows - 1 - m0) * xs + width, xs};
         n = Side{a.gate[k] + n0 * width, (wide - n0) * width, width};
         n2 = Side{a.up[k] + n0 * width, (wide - n0) * width, width};
     } else if constexpr (FORM == DX) {
@@ -417,31 +460,45 @@ __global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, HINT>::threads)) v
     } else {
         deep = rows;
         m = Side{(second ? a.du : a.dg) + first + m0 * ES, rows * pitch - m0 * ES, pitch};
-        n = Side{x + n0 * ES, (int64_t)(rows - 1) * xs + width - n0 * ES, xs};
+        n = Side{x + n0 * ES, ((int64_t)rows - 1) * xs + width - n0 * ES, xs};
         n2 = n;
     }
     const uint32_t steps1 = (uint32_t)((deep + STEP - 1) / STEP), all = FORM == DX ? 2u * steps1 : steps1;
-    const uint32_t begin = FORM == DX ? (uint32_t)((uint64_t)all * split / map.splits) : 0u;
-    const uint32_t end = FORM == DX ? (uint32_t)((uint64_t)all * (split + 1u) / map.splits) : all;
+    const uint32_t begin = FORM == DX ? split * map.per_split : 0u, end = FORM == DX && begin + map.per_split < all ? begin + map.per_split : all;
     const int64_t to_du = FORM == DX ? a.du - a.dg : 0, to_up = FORM == DX ? a.up[k] - a.gate[k] : 0;
     f32x4 acc[S::FM][S::FN] = {};
-    // step s's sides: DX goes through the first pair and then through the second
-    auto side = [&](const Side &from, bool along, uint32_t s, int64_t to_second) {
-        Side at = from;
-        const int64_t on = (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * (along ? 128 : STEP * from.stride);
-        at.p += on + (FORM == DX && s >= steps1 ? to_second : 0);
-        at.bytes -= on;
-        return at;
+    // The sides of the step that is asked for next.  DX goes through the first pair and then through the second; beyond the last step there is nothing to read.
+    const int64_t on_m = S::along_m ? LP * 16 : STEP * m.stride, on_n = S::along_n ? LP * 16 : STEP * n.stride;
+    const Side m_first = m, n_first = n;
+    int64_t left = deep;
+    auto move = [&](int64_t steps) {
+        m.p += steps * on_m, m.bytes -= steps * on_m;
+        n.p += steps * on_n, n.bytes -= steps * on_n;
+        n2.p += steps * on_n, n2.bytes -= steps * on_n;
+        left -= steps * STEP;
     };
-    auto left = [&](uint32_t s) { return deep - (int64_t)(FORM == DX && s >= steps1 ? s - steps1 : s) * STEP; };
-    if (begin < end) S::fetch_both(lds, side(m, S::along_m, begin, to_du), side(n, S::along_n, begin, to_up), side(n2, S::along_n, begin, 0), left(begin));
-    for (uint32_t s = begin; s < end; ++s) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        lds_char *cur = lds + ((s - begin) & 1u) * S::bytes, *next = lds + (~(s - begin) & 1u) * S::bytes;
-        S::step(acc, cur, next, side(m, S::along_m, s + 1u, to_du), side(n, S::along_n, s + 1u, to_up), side(n2, S::along_n, s + 1u, 0), left(s + 1u),
-                s + 1u < end, wm, wn);
+    auto second_pair = [&] {
+        m = m_first, n = n_first, left = deep;
+        m.p += to_du, n.p += to_up;
+    };
+    if (FORM == DX && begin >= steps1) {
+        second_pair();
+        move(begin - steps1);
+    } else move(begin);
+    const uint32_t steps = end - begin;
+    if (!steps) m.bytes = n.bytes = n2.bytes = 0;     // no rows at all: what is asked for in any case is zeros
+    uint32_t into = 0u, cur = 0u;                     // buffers: of the step asked for next, and of the step that is multiplied next
+    for (uint32_t t = 0; t < steps + NS - 1u; ++t) {              // asks for the t-th step, and multiplies the one NS - 1 before
+        const bool ready = t >= NS - 1u;
+        if (ready) S::arrive(w);
+        S::turn(acc, lds + cur * S::bytes, lds + into * S::bytes, m, n, n2, left, ready, wm, wn);
+        move(1);
+        if (FORM == DX && begin + t + 1u == steps1) second_pair();
+        if (t + 1u >= steps) m.bytes = n.bytes = n2.bytes = 0;
+        into = into + 1u == NS ? 0u : into + 1u;
+        if (ready) cur = cur + 1u == NS ? 0u : cur + 1u;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // C through LDS, each wave in a part of its own, so that a lane has eight columns next to each other and the activation's code is there once.
     __syncthreads();
     float *mine = reinterpret_cast<float *>(lds_mem) + w * (S::part_rows * S::part_pitch);
@@ -476,7 +533,7 @@ __global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, HINT>::threads)) v
                     store_some<BF16>(a.u.p, k * a.u.rs + row * a.u.ss + col, at_once, there, u);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = activation(a.act, v[e]).f * u[e];
+                for (int e = 0; e < 8; ++e) v[e] = activation<BF16>(a.act, v[e]).f * u[e];
                 store_some<BF16>(a.a.p, k * a.a.rs + row * a.a.ss + col, at_once, there, v);
             } else if constexpr (FORM == DX) {
                 if (map.splits > 1u) store8<false, WIDE>((char *)(map.part + split * map.part_stride), (int64_t)(a.first[k] + row) * cols + col, 8u, v);
@@ -544,7 +601,7 @@ __global__ __launch_bounds__(256) void few_rows_weights_kernel(const ProductArgs
     char *grad = blockIdx.z ? a.up[k] : a.gate[k];
 #pragma unroll
     for (uint32_t t = threadIdx.x; t < kFewRows * T / 8u; t += 256u) {
-        const uint32_t line = t / (T / 8u), c = t % (T / 8u) * 8u, at = line * (T * 2u) + ((c * 2u) ^ (line & 3u) * 32u);          // as fragment expects it
+        const uint32_t line = t / (T / 8u), c = t % (T / 8u) * 8u, at = line * (T * 2u) + across_place<true>(line, c / 8u) * 16u;
         u32x4 h{}, m{};
         if (line < rows && f0 + c < a.pitch) h = *as_global<u32x4>(from + ((uint64_t)line * a.pitch + f0 + c) * 2u);
         if (line < rows && d0 + c < cols) m = *as_global<u32x4>(x + ((int64_t)line * a.x.ss + d0 + c) * 2);
@@ -555,11 +612,11 @@ __global__ __launch_bounds__(256) void few_rows_weights_kernel(const ProductArgs
     const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6, col = d0 + w * 64u + (lane & 7u) * 8u;
     bf16x8 n[4];
 #pragma unroll
-    for (uint32_t j = 0; j < 4u; ++j) n[j] = fragment<true, false, T>(model, w * 64u + j * 16u, 0);
+    for (uint32_t j = 0; j < 4u; ++j) n[j] = fragment<true, 8, false, T>(model, w * 64u + j * 16u, 0);
 #pragma unroll 2
     for (uint32_t i = 0; i < T; i += 16u) {
         if (f0 + i >= wide) break;
-        const bf16x8 m = fragment<true, false, T>(hidden, i, 0);
+        const bf16x8 m = fragment<true, 8, false, T>(hidden, i, 0);
 #pragma unroll
         for (uint32_t j = 0; j < 4u; ++j)
             *reinterpret_cast<f32x4 *>(&out[w][lane & 15u][j * 16u + (lane >> 4) * 4u]) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m, f32x4{}, 0, 0, 0);

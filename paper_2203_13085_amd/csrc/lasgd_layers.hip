@@ -435,24 +435,33 @@ template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
     return tiles_of<FORM>(d, cols, 256, FORM == FWD ? 128 : 256) >= 2 * kCus ? 256u : 128u;
 }
 
-// Workgroups that share a tile of dx: a contraction of 2 wide, and often few tiles.
-uint32_t dx_splits(const Gated &d, int64_t cols)
+// Workgroups that share a tile of dx, in units of the contraction that every step divides: a contraction of 2 wide, and often few tiles.
+constexpr uint32_t kUnit = 64;
+struct Split {
+    uint32_t count;
+    int64_t deep;                // of the contraction, each
+};
+Split dx_split(const Gated &d, int64_t cols)
 {
-    if (!d.r.most) return 1;
+    if (!d.r.most) return {1, 2 * d.pitch};
     const uint32_t tm = tile_rows<DX>(d, cols), tn = tm == 128u ? 128u : 256u;
-    const uint64_t tiles = tiles_of<DX>(d, cols, tm, tn), steps = 2 * (uint64_t)ceil_div(d.pitch, 128 / d.es);
-    const uint64_t want = (tm == 256u ? 2 * kCus : 4 * kCus) / tiles, most = steps / 4;
-    const uint64_t n = want < most ? want : most;
-    return n < 1 ? 1u : n > 64 ? 64u : (uint32_t)n;
+    const uint64_t tiles = tiles_of<DX>(d, cols, tm, tn), units = 2 * (uint64_t)ceil_div(d.pitch, kUnit);
+    const uint64_t want = (tm == 256u ? 2 * kCus : 4 * kCus) / tiles, most = units / 4;
+    uint64_t n = want < most ? want : most;
+    n = n < 1 ? 1 : n > 64 ? 64 : n;
+    const uint32_t per = ceil_div(units, n);
+    return {ceil_div(units, per), (int64_t)per * kUnit};
 }
 
-template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, bool HINT = false>
-void launch_big(const Gated &d, const ProductArgs &a, uint32_t splits, float *part, hipStream_t st)
+template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, uint32_t LP, uint32_t NS, bool HINT = false>
+void launch_big(const Gated &d, const ProductArgs &a, const Split &split, float *part, hipStream_t st)
 {
+    static_assert(kUnit % (LP * 8u) == 0, "whole steps");
     constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;
     TileMap map{};
     map.replicas = (uint32_t)d.v.K;
-    map.splits = splits;
+    map.splits = split.count;
+    map.per_split = (uint32_t)(split.deep / (LP * 16 / d.es));
     map.part = part;
     map.part_stride = (uint64_t)d.r.total * a.cols;
     uint32_t total = 0;
@@ -462,12 +471,12 @@ void launch_big(const Gated &d, const ProductArgs &a, uint32_t splits, float *pa
         total += tm * ceil_div(FORM == FWD ? a.wide : a.cols, NT) * (FORM == DW ? 2u : 1u);
     }
     map.first[d.v.K] = total;
-    const dim3 grid(total * splits), threads(64u * WM * WN);
-    if (d.v.bf16) hipLaunchKernelGGL((big_product_kernel<true, FORM, TM, TN, WM, WN, HINT>), grid, threads, 0, st, a, map);
-    else hipLaunchKernelGGL((big_product_kernel<false, FORM, TM, TN, WM, WN, HINT>), grid, threads, 0, st, a, map);
+    const dim3 grid(total * split.count), threads(64u * WM * WN);
+    if (d.v.bf16) hipLaunchKernelGGL((big_product_kernel<true, FORM, TM, TN, WM, WN, LP, NS, HINT>), grid, threads, 0, st, a, map);
+    else hipLaunchKernelGGL((big_product_kernel<false, FORM, TM, TN, WM, WN, LP, NS, HINT>), grid, threads, 0, st, a, map);
 }
 
-template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, uint32_t splits, float *part, hipStream_t st)
+template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, const Split &split, float *part, hipStream_t st)
 {
     if (!big) return launch_product<FORM>(d, a, vm, vn, st);
     if constexpr (FORM == DW) {
@@ -483,21 +492,21 @@ template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool 
     if constexpr (FORM == FWD) {
         // Weights in the cache (K = 4, 1 row, 2048 x 5504, 180 MB): 28 us without the hint, 34 with it; beyond it (K = 8, 4 rows) 75 and 70.
         const bool hint = 2 * (uint64_t)d.es * d.v.K * a.wide * a.cols >= kBeyondCache;
-        if (tm == 16u) return hint ? launch_big<FORM, 16, 128, 1, 4, true>(d, a, 1, nullptr, st) : launch_big<FORM, 16, 128, 1, 4>(d, a, 1, nullptr, st);
-        if (tm == 64u) return launch_big<FORM, 64, 128, 1, 4>(d, a, 1, nullptr, st);
+        if (tm == 16u) return hint ? launch_big<FORM, 16, 128, 1, 4, 8, 2, true>(d, a, split, nullptr, st) : launch_big<FORM, 16, 128, 1, 4, 8, 2>(d, a, split, nullptr, st);
+        if (tm == 64u) return launch_big<FORM, 64, 128, 1, 4, 8, 2>(d, a, split, nullptr, st);
     }
     if constexpr (FORM == DX) {
-        if (tm == 16u) return launch_big<FORM, 16, 256, 1, 4, true>(d, a, splits, part, st);
-        if (tm == 64u) return launch_big<FORM, 64, 256, 1, 4>(d, a, splits, part, st);
+        if (tm == 16u) return launch_big<FORM, 16, 256, 1, 4, 8, 2, true>(d, a, split, part, st);
+        if (tm == 64u) return launch_big<FORM, 64, 256, 1, 4, 8, 2>(d, a, split, part, st);
     }
-    if (tm == 128u) launch_big<FORM, 128, 128, 2, 2>(d, a, splits, part, st);
-    else launch_big<FORM, 256, 256, 2, 4>(d, a, splits, part, st);
+    if (tm == 128u) launch_big<FORM, 128, 128, 2, 2, 8, 2>(d, a, split, part, st);
+    else launch_big<FORM, 256, 256, 2, 4, 8, 2>(d, a, split, part, st);
 }
 
 int64_t gates_bytes(const Gated &d) { return (int64_t)round_up16((uint64_t)d.r.total * d.pitch * d.es); }          // dg, and du again
 int64_t gated_bytes(const Gated &d, int64_t cols)
 {
-    const uint32_t splits = dx_splits(d, cols);
+    const uint32_t splits = dx_split(d, cols).count;
     return 2 * gates_bytes(d) + (splits > 1 ? (int64_t)splits * d.r.total * cols * (int64_t)sizeof(float) : 0);
 }
 
@@ -524,7 +533,7 @@ extern "C" lasgd_status lasgd_gated(lasgd_ctx *c, int32_t gate, int32_t up, cons
     if (!d.r.most) return LASGD_OK;
     weights(p, d, d.v.params, gate, up, cols);
     p.wide_out = vo;
-    launch_form<FWD>(d, p, streams(d, cols, p.x, vx), vx, cols % 8 == 0, 1, nullptr, (hipStream_t)stream);
+    launch_form<FWD>(d, p, streams(d, cols, p.x, vx), vx, cols % 8 == 0, Split{1, 0}, nullptr, (hipStream_t)stream);
     return launched(c);
 }
 
@@ -584,9 +593,10 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
         q.a = out;
         weights(q, d, d.v.params, gate, up, cols);
         q.wide_out = vo;
-        const uint32_t splits = big ? dx_splits(d, cols) : 1;
+        const Split split = big ? dx_split(d, cols) : Split{1, 0};
+        const uint32_t splits = split.count;
         float *part = (float *)(e.du + gates_bytes(d));
-        launch_form<DX>(d, q, big, true, cols % 8 == 0, splits, part, st);
+        launch_form<DX>(d, q, big, true, cols % 8 == 0, split, part, st);
         TRY(launched(c));
         if (splits > 1) {
             JoinRowsArgs j{out, part, (uint64_t)d.r.total * cols, splits, (uint32_t)cols, vo, {}, {}};
@@ -600,6 +610,6 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
     }
     p.accumulate = accumulate;
     weights(p, d, d.v.grads, gate, up, cols);
-    launch_form<DW>(d, p, big, true, vx, 1, nullptr, st);
+    launch_form<DW>(d, p, big, true, vx, Split{1, 0}, nullptr, st);
     return launched(c);
 }
