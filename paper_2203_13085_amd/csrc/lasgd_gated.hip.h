@@ -98,129 +98,161 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ---- any size, stride and alignment ------------------------------------------------------------------------------------------
-// Tiles of 64 x 64, four waves of 32 x 32, 32 of the contraction at a time through LDS, where both sides lie [64][32] whatever they are in memory; what is
-// outside is zero there.
-constexpr uint32_t kTile = 64, kDeep = 32;
+// Tiles of T x T (FWD: half of the columns gate's, half up's), four waves, 32 of the contraction at a time through LDS, where both sides lie [T][32] whatever
+// they are in memory; what is outside is zero there.  The next 32 are asked for, in the widest accesses that the alignment allows, before these are multiplied.
+constexpr uint32_t kDeep = 32;
 
-template <bool BF16> struct Elem { typedef float type; static constexpr uint32_t pitch = kDeep + 1; };
+template <bool BF16> struct Elem { typedef float type; static constexpr uint32_t pitch = kDeep + 4; };
 template <> struct Elem<true> { typedef uint16_t type; static constexpr uint32_t pitch = kDeep + 8; };
 
-// One side's tile: element (i, c) of i < ni, c < nc is at p + i * stride + c (ALONG) or p + c * stride + i.
-// Eight at a time along what is contiguous; VEC: these are aligned, and ni or nc counts whole eights.
+// One side's tile: element (i, c) of i < ni, c < nc is at p + i * stride + c (ALONG) or p + c * stride + i.  A thread has eight next to each other in memory
+// of every 64 rows.  VEC: these are aligned, and ni or nc counts whole eights.
 template <bool BF16, bool ALONG, bool VEC>
-__device__ __forceinline__ void stage(typename Elem<BF16>::type *lds, const char *p, int64_t stride, int64_t i0, int64_t ni, int64_t c0, int64_t nc)
+__device__ __forceinline__ Raw8<BF16> ask(const char *p, int64_t stride, int64_t i, int64_t ni, int64_t c, int64_t nc)
 {
-    constexpr uint32_t P = Elem<BF16>::pitch;
-    const uint32_t t = threadIdx.x;
-    const uint32_t il = ALONG ? t >> 2 : (t & 7u) * 8u, cl = ALONG ? (t & 3u) * 8u : t >> 3;
-    const int64_t i = i0 + il, c = c0 + cl;
     const int64_t left = ALONG ? (i < ni ? nc - c : 0) : (c < nc ? ni - i : 0);
     const uint32_t n = left >= 8 ? 8u : left > 0 ? (uint32_t)left : 0u;
     const int64_t at = ALONG ? i * stride + c : c * stride + i;
-    float v[8];
-    if (VEC && n) load8<BF16, WIDE>(v, p, at, 8u);
-    else load8<BF16, LOOSE>(v, p, at, VEC ? 0u : n);
+    if (VEC && n) return load_raw<BF16, WIDE>(p, at, 8u);
+    return load_raw<BF16, LOOSE>(p, at, VEC ? 0u : n);
+}
+template <bool ALONG> __device__ __forceinline__ uint32_t own_row() { return ALONG ? threadIdx.x >> 2 : (threadIdx.x & 7u) * 8u; }
+template <bool ALONG> __device__ __forceinline__ uint32_t own_deep() { return ALONG ? (threadIdx.x & 3u) * 8u : threadIdx.x >> 3; }
+template <bool BF16, bool ALONG>
+__device__ __forceinline__ void put(typename Elem<BF16>::type *lds, const Raw8<BF16> &r)
+{
+    constexpr uint32_t P = Elem<BF16>::pitch;
+    typename Elem<BF16>::type *at = lds + own_row<ALONG>() * P + own_deep<ALONG>();
+    if constexpr (ALONG) {
 #pragma unroll
-    for (uint32_t j = 0; j < 8u; ++j) {
-        const uint32_t w = ALONG ? il * P + cl + j : (il + j) * P + cl;
-        if constexpr (BF16) lds[w] = (uint16_t)(__float_as_uint(v[j]) >> 16);          // exact: it was bf16
-        else lds[w] = v[j];
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) *reinterpret_cast<u32x4 *>(at + i * 4) = r.w[i];
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 8u; ++j) {
+            if constexpr (BF16) at[j * P] = (uint16_t)(r.w[0][j >> 1] >> (16u * (j & 1u)));
+            else at[j * P] = __uint_as_float(r.w[j >> 2][j & 3u]);
+        }
     }
+}
+
+// Column of C that a wave's fragment j of the n side starts with, in its half of the tile's lines in LDS (FWD: first gate's, then up's).
+template <int FORM, uint32_t T> __device__ __forceinline__ uint32_t loose_n_row(uint32_t wn, uint32_t j)
+{
+    if constexpr (FORM == FWD) return (j >= T / 64u ? T / 2u + (j - T / 64u) * 16u : j * 16u) + wn * (T / 4u);
+    else return wn * (T / 2u) + j * 16u;
 }
 
 // acc += the tile's part of C: element (n = 4 * (lane / 16) + reg, m = lane % 16) of each 16 x 16.
-template <bool BF16>
-__device__ __forceinline__ void multiply(f32x4 (&acc)[2][2], const typename Elem<BF16>::type *m, const typename Elem<BF16>::type *n, uint32_t wm, uint32_t wn)
+template <bool BF16, int FORM, uint32_t T>
+__device__ __forceinline__ void multiply(f32x4 (&acc)[T / 32u][T / 32u], const typename Elem<BF16>::type *m, const typename Elem<BF16>::type *n, uint32_t wm, uint32_t wn)
 {
-    constexpr uint32_t P = Elem<BF16>::pitch;
+    constexpr uint32_t P = Elem<BF16>::pitch, F = T / 32u;
     const uint32_t lane = threadIdx.x & 63u, row = lane & 15u, quad = lane >> 4;
     if constexpr (BF16) {
-        bf16x8 fm[2], fn[2];
+        bf16x8 fm[F], fn[F];
 #pragma unroll
-        for (uint32_t i = 0; i < 2u; ++i) {
-            fm[i] = *reinterpret_cast<const bf16x8 *>(m + (wm * 32u + i * 16u + row) * P + quad * 8u);
-            fn[i] = *reinterpret_cast<const bf16x8 *>(n + (wn * 32u + i * 16u + row) * P + quad * 8u);
+        for (uint32_t i = 0; i < F; ++i) {
+            fm[i] = *reinterpret_cast<const bf16x8 *>(m + (wm * (T / 2u) + i * 16u + row) * P + quad * 8u);
+            fn[i] = *reinterpret_cast<const bf16x8 *>(n + (loose_n_row<FORM, T>(wn, i) + row) * P + quad * 8u);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (uint32_t i = 0; i < F; ++i) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fn[j], fm[i], acc[i][j], 0, 0, 0);
+            for (uint32_t j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fn[j], fm[i], acc[i][j], 0, 0, 0);
         }
     } else {
 #pragma unroll
-        for (uint32_t c = 0; c < kDeep; c += 4u) {
-            float fm[2], fn[2];
+        for (uint32_t c = 0; c < kDeep; c += 16u) {               // a lane's four of the contraction next to each other, on both sides
+            f32x4 fm[F], fn[F];
 #pragma unroll
-            for (uint32_t i = 0; i < 2u; ++i) {
-                fm[i] = m[(wm * 32u + i * 16u + row) * P + c + quad];
-                fn[i] = n[(wn * 32u + i * 16u + row) * P + c + quad];
+            for (uint32_t i = 0; i < F; ++i) {
+                fm[i] = *reinterpret_cast<const f32x4 *>(m + (wm * (T / 2u) + i * 16u + row) * P + c + quad * 4u);
+                fn[i] = *reinterpret_cast<const f32x4 *>(n + (loose_n_row<FORM, T>(wn, i) + row) * P + c + quad * 4u);
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int e = 0; e < 4; ++e) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fn[j], fm[i], acc[i][j], 0, 0, 0);
+                for (uint32_t i = 0; i < F; ++i) {
+#pragma unroll
+                    for (uint32_t j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fn[j][e], fm[i][e], acc[i][j], 0, 0, 0);
+                }
             }
         }
     }
 }
 
-template <bool BF16, int FORM, bool VM, bool VN>
+template <bool BF16, int FORM, bool VM, bool VN, uint32_t T>
 __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
 {
-    typedef typename Elem<BF16>::type T;
-    constexpr uint32_t ES = BF16 ? 2u : 4u;
-    __shared__ __attribute__((aligned(16))) T ldsm[kTile * Elem<BF16>::pitch], ldsn[(FORM == FWD ? 2 : 1) * kTile * Elem<BF16>::pitch];
+    typedef typename Elem<BF16>::type E;
+    constexpr uint32_t ES = BF16 ? 2u : 4u, P = Elem<BF16>::pitch, R = T / 64u, F = T / 32u, NT = FORM == FWD ? T / 2u : T;
+    constexpr bool ALONG_M = FORM != DW, ALONG_N = FORM == FWD;
+    __shared__ __attribute__((aligned(16))) E ldsm[T * P], ldsn[T * P];
     const uint32_t k = blockIdx.y;
     const int64_t rows = a.rows[k], cols = a.cols, wide = a.wide;
     const int64_t M = FORM == DW ? wide : rows, N = FORM == FWD ? wide : cols;
-    const uint32_t tn = (uint32_t)((N + kTile - 1) / kTile);
-    const int64_t m0 = (int64_t)(blockIdx.x / tn) * kTile, n0 = (int64_t)(blockIdx.x % tn) * kTile;
+    const uint32_t tn = (uint32_t)((N + NT - 1) / NT);
+    const int64_t m0 = (int64_t)(blockIdx.x / tn) * T, n0 = (int64_t)(blockIdx.x % tn) * NT;
     if (m0 >= M) return;
     const uint32_t w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1u;
-    f32x4 acc[FORM == FWD ? 2 : 1][2][2] = {};
+    f32x4 acc[F][F] = {};
     const char *dg = a.dg + (uint64_t)a.first[k] * a.pitch * ES, *du = a.du + (uint64_t)a.first[k] * a.pitch * ES;
+    const char *x = a.x.p + k * a.x.rs * (int64_t)ES;
     const int64_t deep = FORM == FWD ? cols : FORM == DX ? wide : rows;
-    for (int half = 0; half < (FORM == DX ? 2 : 1); ++half)
-        for (int64_t c = 0; c < deep; c += kDeep) {
+    Raw8<BF16> rm[R], rn[R];
+    auto ask_both = [&](int half, int64_t c0) {
+        const int64_t cm = c0 + own_deep<ALONG_M>(), cn = c0 + own_deep<ALONG_N>();
+#pragma unroll
+        for (uint32_t q = 0; q < R; ++q) {
+            const uint32_t im = q * 64u + own_row<ALONG_M>(), in = q * 64u + own_row<ALONG_N>();
             if constexpr (FORM == FWD) {
-                stage<BF16, true, VM>(ldsm, a.x.p + k * a.x.rs * ES, a.x.ss, m0, M, c, deep);
-                stage<BF16, true, VN>(ldsn, a.gate[k], cols, n0, N, c, deep);
-                stage<BF16, true, VN>(ldsn + kTile * Elem<BF16>::pitch, a.up[k], cols, n0, N, c, deep);
+                rm[q] = ask<BF16, true, VM>(x, a.x.ss, m0 + im, M, cm, deep);
+                rn[q] = ask<BF16, true, VN>(in < T / 2u ? a.gate[k] : a.up[k], cols, n0 + in % (T / 2u), N, cn, deep);
             } else if constexpr (FORM == DX) {
-                stage<BF16, true, VM>(ldsm, half ? du : dg, a.pitch, m0, M, c, deep);
-                stage<BF16, false, VN>(ldsn, half ? a.up[k] : a.gate[k], cols, n0, N, c, deep);
+                rm[q] = ask<BF16, true, VM>(half ? du : dg, a.pitch, m0 + im, M, cm, deep);
+                rn[q] = ask<BF16, false, VN>(half ? a.up[k] : a.gate[k], cols, n0 + in, N, cn, deep);
             } else {
-                stage<BF16, false, VM>(ldsm, blockIdx.z ? du : dg, a.pitch, m0, M, c, deep);
-                stage<BF16, false, VN>(ldsn, a.x.p + k * a.x.rs * ES, a.x.ss, n0, N, c, deep);
+                rm[q] = ask<BF16, false, VM>(blockIdx.z ? du : dg, a.pitch, m0 + im, M, cm, deep);
+                rn[q] = ask<BF16, false, VN>(x, a.x.ss, n0 + in, N, cn, deep);
             }
-            __syncthreads();
-            multiply<BF16>(acc[0], ldsm, ldsn, wm, wn);
-            if constexpr (FORM == FWD) multiply<BF16>(acc[1], ldsm, ldsn + kTile * Elem<BF16>::pitch, wm, wn);
-            __syncthreads();
         }
+    };
+    const int64_t steps1 = (deep + kDeep - 1) / kDeep, steps = FORM == DX ? 2 * steps1 : steps1;
+    if (steps) ask_both(0, 0);
+    for (int64_t s = 0; s < steps; ++s) {
+#pragma unroll
+        for (uint32_t q = 0; q < R; ++q) {
+            put<BF16, ALONG_M>(ldsm + q * 64u * P, rm[q]);
+            put<BF16, ALONG_N>(ldsn + q * 64u * P, rn[q]);
+        }
+        __syncthreads();
+        if (s + 1 < steps) ask_both(FORM == DX && s + 1 >= steps1, (FORM == DX && s + 1 >= steps1 ? s + 1 - steps1 : s + 1) * kDeep);
+        multiply<BF16, FORM, T>(acc, ldsm, ldsn, wm, wn);
+        __syncthreads();
+    }
     const uint32_t lane = threadIdx.x & 63u;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < F; ++i) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t m = m0 + wm * 32u + i * 16 + (lane & 15u), n1 = n0 + wn * 32u + j * 16 + (lane >> 4) * 4u;
+        for (uint32_t j = 0; j < (FORM == FWD ? F / 2u : F); ++j) {
+            const int64_t m = m0 + wm * (T / 2u) + i * 16 + (lane & 15u), n1 = n0 + loose_n_row<FORM, T>(wn, j) + (lane >> 4) * 4u;
             if (m >= M) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int64_t n = n1 + e;
                 if (n >= N) continue;
                 if constexpr (FORM == FWD) {
-                    const float g = acc[0][i][j][e], u = acc[1][i][j][e];
+                    const float g = acc[i][j][e], u = acc[i][j + F / 2u][e];
                     store1<BF16>(a.a.p, k * a.a.rs + m * a.a.ss + n, activation<BF16>(a.act, g).f * u);
                     if (a.g.p) {
                         store1<BF16>(a.g.p, k * a.g.rs + m * a.g.ss + n, g);
                         store1<BF16>(a.u.p, k * a.u.rs + m * a.u.ss + n, u);
                     }
                 } else if constexpr (FORM == DX) {
-                    store1<BF16>(a.a.p, k * a.a.rs + m * a.a.ss + n, acc[0][i][j][e]);
+                    store1<BF16>(a.a.p, k * a.a.rs + m * a.a.ss + n, acc[i][j][e]);
                 } else {
                     char *grad = blockIdx.z ? a.up[k] : a.gate[k];
-                    float v = acc[0][i][j][e];
+                    float v = acc[i][j][e];
                     if (a.accumulate) v += load1<BF16>(grad, m * cols + n);
                     store1<BF16>(grad, m * cols + n, v);
                 }

@@ -370,8 +370,10 @@ lasgd_status check_gated(lasgd_ctx *c, Gated &d, int32_t gate, int32_t up, const
     CHECK(gate == up || d.v.numel[up] == n, LASGD_ERR_INVALID, "gate has %lld elements, up %lld", (long long)n, (long long)d.v.numel[up]);
     d.wide = n / per;
     d.pitch = (d.wide + 7) / 8 * 8;
-    const __int128 tiles_w = (d.wide + kTile - 1) / kTile, tiles_c = (cols + kTile - 1) / kTile, tiles_r = (d.r.most + kTile - 1) / kTile;
-    CHECK(tiles_r * tiles_w <= kMaxBlocks && tiles_r * tiles_c <= kMaxBlocks && tiles_w * tiles_c <= kMaxBlocks, LASGD_ERR_UNSUPPORTED, "too many tiles");
+    // workgroups of a launch, at the smallest tiles there are (16 x 64, 32 splits and more only of few tiles)
+    const __int128 wide64 = (d.wide + 31) / 32, cols64 = (cols + 31) / 32, rows16 = (int64_t)d.r.total / 16 + d.v.K;
+    CHECK(rows16 * wide64 <= kMaxBlocks / 4 && rows16 * cols64 <= kMaxBlocks / 4 && wide64 * cols64 * d.v.K <= kMaxBlocks, LASGD_ERR_UNSUPPORTED,
+          "more workgroups than a launch has");
     return LASGD_OK;
 }
 
@@ -401,16 +403,6 @@ void weights(ProductArgs &a, const Gated &d, void *const *of, int32_t gate, int3
     }
 }
 
-template <int FORM> void launch_product(const Gated &d, const ProductArgs &a, bool vm, bool vn, hipStream_t st)
-{
-    const uint64_t M = FORM == DW ? d.wide : d.r.most, N = FORM == FWD ? a.wide : a.cols;
-    const dim3 grid(ceil_div(M, kTile) * ceil_div(N, kTile), d.v.K, FORM == DW ? 2 : 1);
-    two_flags(vm, vn, [&](auto m, auto n) {
-        if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((product_kernel<false, FORM, m, n>), grid, dim3(256), 0, st, a);
-    });
-}
-
 // Whether a product's sides can go straight from memory into LDS: 16-byte pieces, a tile's lines within 32 bits of bytes.
 bool streams(const Gated &d, int64_t cols, const RowsAt &x, bool vx)
 {
@@ -426,8 +418,24 @@ template <int FORM> uint64_t tiles_of(const Gated &d, int64_t cols, uint32_t tm,
     return rows * ceil_div(FORM == FWD ? d.wide : cols, tn) * (FORM == DW ? 2 : 1);
 }
 
-// Rows of a tile of a gated block's products.
 constexpr uint32_t kCus = 256;
+
+template <int FORM> void launch_loose(const Gated &d, const ProductArgs &a, bool vm, bool vn, hipStream_t st)
+{
+    auto launch = [&](auto tile) {
+        constexpr uint32_t T = decltype(tile)::value;
+        const uint64_t M = FORM == DW ? d.wide : d.r.most, N = FORM == FWD ? a.wide : a.cols;
+        const dim3 grid(ceil_div(M, T) * ceil_div(N, FORM == FWD ? T / 2 : T), d.v.K, FORM == DW ? 2 : 1);
+        two_flags(vm, vn, [&](auto m, auto n) {
+            if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n, T>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((product_kernel<false, FORM, m, n, T>), grid, dim3(256), 0, st, a);
+        });
+    };
+    if (tiles_of<FORM>(d, a.cols, 128, FORM == FWD ? 64 : 128) >= 2 * kCus) launch(std::integral_constant<uint32_t, 128>{});
+    else launch(std::integral_constant<uint32_t, 64>{});
+}
+
+// Rows of a tile of a gated block's products.
 template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
 {
     if (FORM != DW && d.r.most <= 16u) return 16u;
@@ -478,7 +486,7 @@ void launch_big(const Gated &d, const ProductArgs &a, const Split &split, float 
 
 template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, const Split &split, float *part, hipStream_t st)
 {
-    if (!big) return launch_product<FORM>(d, a, vm, vn, st);
+    if (!big) return launch_loose<FORM>(d, a, vm, vn, st);
     if constexpr (FORM == DW) {
         if (d.v.bf16 && d.r.most <= kFewRows) {
             const dim3 grid(ceil_div(a.wide, 256) * ceil_div(a.cols, 256), d.v.K, 2);
