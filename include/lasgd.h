@@ -370,8 +370,8 @@ lasgd_status lasgd_sgd_ar_step_clip(lasgd_ctx *ctx, float lr, const lasgd_clip *
  * write the same gradient may not.  workspace: device memory of the caller's, 16-byte aligned, as many bytes as the call's _bytes function
  * says, in use until the call has run: two calls that may run at the same time, and two graphs that may be replayed at the same time, need one each.
  *
- * Sums, norms and products are in fp32, results are rounded to the storage type once.  The same call on the same data gives the
- * same bits.  accumulate: the weights' gradients are added to what their buffers hold (0: they replace it, also
+ * Sums, norms and products are in fp32 (of a norm with an 8-bit output in fp64), results are rounded to the storage type once.  The same call on the same
+ * data gives the same bits.  accumulate: the weights' gradients are added to what their buffers hold (0: they replace it, also
  * of a replica with 0 rows, which are then 0).
  * Errors of all: INVALID (NULL, a stride, size or tensor index out of range, misaligned, a workspace that is too small, the context's device not current),
  * STATE (a replica is unbound), UNSUPPORTED (2^31 rows of all replicas together, or beyond a limit below), HIP.
@@ -406,7 +406,7 @@ lasgd_status lasgd_dropout(lasgd_ctx *ctx, const int64_t *rows, int64_t cols, co
  * h = residual + drop(x),  y = gain * h / sqrt(mean(h^2) + eps) over a row.  gain: index of a bound tensor, whose length is the number of columns.
  * residual may be NULL (none), sum too (h is not written; h enters the norm before it is rounded), and drop (no dropout).  scales NULL: y of the
  * storage type.  Otherwise y is e4m3 (OCP, one byte an element) and scales, fp32, gets scale = max |y| / 448 of each row (at least 2^-126) at
- * data[k * replica_stride + r * row_stride]; y / scale is rounded to nearest even.  sum may be x or residual, and y, in the storage type, x or residual.
+ * data[k * replica_stride + r * row_stride]; y / scale, both as they are before a rounding, is rounded to nearest even.  sum may be x or residual, and y, in the storage type, x or residual.
  * Errors: as above, and UNSUPPORTED beyond LASGD_NORM_MAX_COLS columns.
  */
 #define LASGD_NORM_MAX_COLS 16384

@@ -276,7 +276,8 @@ extern "C" lasgd_status lasgd_rms_norm(lasgd_ctx *c, int32_t gain, const int64_t
         const dim3 grid(ceil_div(r.most, T / G), v.K);
         const int64_t bytes = (int64_t)r.total * cols * (es * (1 + !!residual + !!sum) + (scales ? 1 : es));
         row_access(v.bf16, vec, bytes, [&](auto bf16, auto wide) {
-            hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV>), grid, dim3(T), 0, (hipStream_t)stream, a);
+            if (scales) hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV, true>), grid, dim3(T), 0, (hipStream_t)stream, a);
+            else hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV, false>), grid, dim3(T), 0, (hipStream_t)stream, a);
         });
     });
     return launched(c);

@@ -5,6 +5,8 @@
 #pragma once
 #include "lasgd_memory.hip.h"
 
+#include <type_traits>
+
 namespace lasgd {
 
 
@@ -213,9 +215,13 @@ __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a)
 // ---- root-mean-square norm ----------------------------------------------------------------------------------------------------
 //     h = residual + m x / (1 - p),   rho = (mean h^2 + eps)^(-1/2),   y = gain (h rho)
 // G threads hold a row, NV groups of eight columns each, so everything is read once; h is rounded where it is stored, and enters the norm
-// as it was before.  In 8 bits: scale = max |y| / 448, at least the smallest normal number, and y / scale to e4m3.
-constexpr float kE4m3Max = 448.f;
-constexpr float kLeastScale = 1.17549435e-38f;
+// as it was before.
+//
+// In 8 bits (OUT8): scale = max |y| / 448, at least the smallest normal number, and y / scale to e4m3, of whose values so few are that 1 in 10^6 quotients
+// lies within fp32's roundings of a border between two and would end up a sixteenth off.  So this form computes in 64 bits from the
+// loaded values on, which the memory hides.
+constexpr double kE4m3Max = 448.0;
+constexpr double kLeastScale = 1.1754943508222875e-38;
 
 struct NormRowsArgs {
     RowsAt x, residual, sum, y, scales;
@@ -226,8 +232,8 @@ struct NormRowsArgs {
     const char *gain[64];
 };
 
-// Sum over the G threads of a row, the same in all of them.  lds: a word a wave.
-template <int G> __device__ __forceinline__ float row_sum(float v, float *lds)
+// Sum over the G threads of a row, the same in all of them.  lds: one a wave.
+template <int G, class T> __device__ __forceinline__ T row_sum(T v, T *lds)
 {
 #pragma unroll
     for (int d = (G < 64 ? G : 64) / 2; d; d >>= 1) v += __shfl_xor(v, d, 64);
@@ -235,7 +241,7 @@ template <int G> __device__ __forceinline__ float row_sum(float v, float *lds)
         __syncthreads();                 // the words of the sum before
         if ((threadIdx.x & 63u) == 0u) lds[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = 0.f;
+        v = T(0);
 #pragma unroll
         for (int w = 0; w < G / 64; ++w) v += lds[w];
     }
@@ -256,8 +262,8 @@ template <int G> __device__ __forceinline__ float2 row_sums(float2 v, float2 *ld
     }
     return v;
 }
-__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }      // a NaN stays
-template <int G> __device__ __forceinline__ float row_max(float v, float *lds)
+template <class T> __device__ __forceinline__ T larger(T a, T b) { return b > a || b != b ? b : a; }      // a NaN stays
+template <int G, class T> __device__ __forceinline__ T row_max(T v, T *lds)
 {
 #pragma unroll
     for (int d = (G < 64 ? G : 64) / 2; d; d >>= 1) v = larger(v, __shfl_xor(v, d, 64));
@@ -274,10 +280,14 @@ template <int G> __device__ __forceinline__ float row_max(float v, float *lds)
 
 constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
 
-template <bool BF16, int VEC, int G, int NV>
+__device__ __forceinline__ float reciprocal_root(float v) { return 1.f / __builtin_sqrtf(v); }
+__device__ __forceinline__ double reciprocal_root(double v) { return 1.0 / __builtin_sqrt(v); }
+
+template <bool BF16, int VEC, int G, int NV, bool OUT8>
 __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRowsArgs a)
 {
-    __shared__ float lds[G > 64 ? G / 64 : 1];
+    typedef std::conditional_t<OUT8, double, float> T;
+    __shared__ T lds[G > 64 ? G / 64 : 1];
     constexpr uint32_t R = norm_threads(G) / G;              // rows a workgroup
     const uint32_t k = blockIdx.y, rows = a.rows[k];
     const uint64_t r = (uint64_t)blockIdx.x * R + threadIdx.x / G;
@@ -285,9 +295,10 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRow
     if (G <= 64 && r >= rows) return;                        // (with G > 64 a workgroup is one row)
     const uint32_t t = threadIdx.x % G;
     const uint64_t call = a.drop.below ? call_number(a.drop) : 0;
+    const T stay = OUT8 ? a.drop.below < 65536u ? T(65536) / T(65536u - a.drop.below) : T(0) : T(a.drop.scale);
     const char *gain = a.gain[k];
-    float h[NV][8];
-    float sum = 0.f;
+    T h[NV][8];
+    T sum = 0;
     {
         Raw8<BF16> x[NV], res[NV];               // all asked for before the first is looked at
 #pragma unroll
@@ -306,35 +317,34 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRow
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            widen8<BF16>(h[i], x[i]);
-            if (a.drop.below) {
-                const Lots lots = draw_lots(a.drop, call, k, r * a.groups + t + i * G);
+            const uint32_t g = t + i * G, c = g * 8u;
+            float v[8];
+            widen8<BF16>(v, x[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[i][j] = stays(lots, j, a.drop.below) ? h[i][j] * a.drop.scale : 0.f;
+            for (int j = 0; j < 8; ++j) h[i][j] = v[j];
+            if (a.drop.below) {
+                const Lots lots = draw_lots(a.drop, call, k, r * a.groups + g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] = stays(lots, j, a.drop.below) ? h[i][j] * stay : T(0);
             }
             if (a.residual.p) {
-                float z[8];
-                widen8<BF16>(z, res[i]);
+                widen8<BF16>(v, res[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[i][j] = z[j] + h[i][j];
+                for (int j = 0; j < 8; ++j) h[i][j] = T(v[j]) + h[i][j];
             }
-        }
-    }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
+            for (int j = 0; j < 8; ++j) sum = OUT8 ? T(__builtin_fma((double)h[i][j], (double)h[i][j], (double)sum))
+                                                   : T(__builtin_fmaf((float)h[i][j], (float)h[i][j], (float)sum));
+            if (a.sum.p && g < a.groups) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(h[i][j], h[i][j], sum);
-    }
-    if (a.sum.p) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t g = t + i * G, c = g * 8u;
-            if (g < a.groups) store8<BF16, VEC>(a.sum.p, k * a.sum.rs + (int64_t)r * a.sum.ss + c, a.cols - c, h[i]);
+                for (int j = 0; j < 8; ++j) v[j] = (float)h[i][j];
+                store8<BF16, VEC>(a.sum.p, k * a.sum.rs + (int64_t)r * a.sum.ss + c, a.cols - c, v);
+            }
         }
     }
     sum = row_sum<G>(sum, lds);
-    const float rho = 1.f / __builtin_sqrtf(__builtin_fmaf(sum, a.inv_cols, a.eps));
-    float most = 0.f;
+    const T rho = reciprocal_root(OUT8 ? sum / T(a.cols) + T(a.eps) : T(__builtin_fmaf((float)sum, a.inv_cols, a.eps)));
+    T most = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t g = t + i * G, c = g * 8u;
@@ -343,38 +353,39 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRow
             load8<BF16, VEC ? WIDE : LOOSE>(w, gain, c, a.cols - c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                h[i][j] = w[j] * (h[i][j] * rho);
-                most = larger(most, __builtin_fabsf(h[i][j]));
+                h[i][j] = T(w[j]) * (h[i][j] * rho);
+                if constexpr (OUT8) most = larger(most, h[i][j] < 0 ? -h[i][j] : h[i][j]);
             }
-            if (!a.scales.p) store8<BF16, VEC>(a.y.p, k * a.y.rs + (int64_t)r * a.y.ss + c, a.cols - c, h[i]);
+            if constexpr (!OUT8) store8<BF16, VEC>(a.y.p, k * a.y.rs + (int64_t)r * a.y.ss + c, a.cols - c, h[i]);
         }
     }
-    if (!a.scales.p) return;
-    most = row_max<G>(most, lds);
-    float scale = most / kE4m3Max;
-    if (scale < kLeastScale) scale = kLeastScale;
-    const float inv = 1.f / scale;
-    if (t == 0u) as_global<float>(a.scales.p)[k * a.scales.rs + (int64_t)r * a.scales.ss] = scale;
+    if constexpr (OUT8) {
+        most = row_max<G>(most, lds);
+        double scale = most / kE4m3Max;
+        if (scale < kLeastScale) scale = kLeastScale;
+        const double inv = 1.0 / scale;
+        if (t == 0u) as_global<float>(a.scales.p)[k * a.scales.rs + (int64_t)r * a.scales.ss] = (float)scale;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const uint32_t g = t + i * G, c = g * 8u;
-        if (g < a.groups) {
-            uint32_t q[2];
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t g = t + i * G, c = g * 8u;
+            if (g < a.groups) {
+                uint32_t q[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                int w = 0;
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][4 * j] * inv, h[i][4 * j + 1] * inv, w, false);
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][4 * j + 2] * inv, h[i][4 * j + 3] * inv, w, true);
-                q[j] = (uint32_t)w;
-            }
-            char *y = a.y.p + (k * a.y.rs + (int64_t)r * a.y.ss + c);
-            typedef uint32_t loose2 __attribute__((ext_vector_type(2), aligned(1)));
-            if constexpr (VEC) *as_global<u32x2>(y) = u32x2{q[0], q[1]};
-            else if (a.cols - c >= 8u) *as_global<loose2>(y) = u32x2{q[0], q[1]};
-            else {
+                for (int j = 0; j < 2; ++j) {
+                    int w = 0;
+                    w = __builtin_amdgcn_cvt_pk_fp8_f32((float)(h[i][4 * j] * inv), (float)(h[i][4 * j + 1] * inv), w, false);
+                    w = __builtin_amdgcn_cvt_pk_fp8_f32((float)(h[i][4 * j + 2] * inv), (float)(h[i][4 * j + 3] * inv), w, true);
+                    q[j] = (uint32_t)w;
+                }
+                char *y = a.y.p + (k * a.y.rs + (int64_t)r * a.y.ss + c);
+                typedef uint32_t loose2 __attribute__((ext_vector_type(2), aligned(1)));
+                if constexpr (VEC) *as_global<u32x2>(y) = u32x2{q[0], q[1]};
+                else if (a.cols - c >= 8u) *as_global<loose2>(y) = u32x2{q[0], q[1]};
+                else {
 #pragma unroll
-                for (uint32_t j = 0; j < 8u; ++j)
-                    if (c + j < a.cols) *as_global<uint8_t>(y + j) = (uint8_t)(q[j >> 2] >> (8u * (j & 3u)));
+                    for (uint32_t j = 0; j < 8u; ++j)
+                        if (c + j < a.cols) *as_global<uint8_t>(y + j) = (uint8_t)(q[j >> 2] >> (8u * (j & 3u)));
+                }
             }
         }
     }

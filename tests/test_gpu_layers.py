@@ -204,6 +204,25 @@ def test_rms_norm_in_8_bits(rows, cols, layout, storage):
     m.close()
 
 
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_rms_norm_in_8_bits_takes_the_nearest_value(storage):
+    """Every one of 2^21 values, with a residual and a mask: the quotients are made in 64 bits, so what lies next to a border goes to its side."""
+    dt, gen, rows, cols, p = dtype_of(storage), generator(21), [512, 512], 2048, 0.125
+    m = Model(2, [(cols,)], storage, gen, plus=1.0)
+    x, res, h = Act(rows, cols, dt, "dense", gen), Act(rows, cols, dt, "dense", gen), Act(rows, cols, dt)
+    q, scales = torch.zeros(2, 512, cols, dtype=torch.uint8, device=DEV), torch.zeros(2, 512, device=DEV)
+    m.ctx.rms_norm(0, rows, x.at, (q.data_ptr(), 512 * cols, cols), residual=res.at, sum=h.at, scales=(scales.data_ptr(), 512, 1), eps=1e-6, p=p, seed=SEED, call=CALL)
+    torch.cuda.synchronize()
+    for k in range(2):
+        f = mask_of(k, 512, cols, p, SEED, CALL).to(DEV).double() * scale_of(p)
+        h64, _, y64 = _norm64(x.d(k), res.d(k), f, m.weight(0, k).double(), float(np.float32(1e-6)))
+        s64 = y64.abs().amax(1, keepdim=True) / 448
+        assert torch.equal(q[k].view(torch.float8_e4m3fn).float(), (y64 / s64).float().to(torch.float8_e4m3fn).float())
+        within(scales[k], s64[:, 0], U * s64[:, 0] * 1.001, "scale")
+        within(h[k], h64, HALF[dt] * h64.abs() * 1.001 + U * h64.abs(), "sum")
+    m.close()
+
+
 def test_rms_norm_without_numbers():
     """An infinity or a NaN stays in its row; a row of zeros gives zeros, whatever eps."""
     gen = generator(5)
