@@ -436,7 +436,10 @@ template <int FORM> void launch_loose(const Gated &d, const ProductArgs &a, bool
     else launch(std::integral_constant<uint32_t, 64>{});
 }
 
-// Rows of a tile of a gated block's products.
+// Rows of a tile of a gated block's products.  Large tiles read their sides less often, small ones fill the chip and waste less of few rows.  us forward / dx (with the
+// sum of its shares) / weights, tiles of 128 and of 256: bf16, K = 8, 2048 rows, 2048 x 5504 985 / 849 / 900 and 802 / 675 / 722; K = 2, 512 rows, 1024 x 2816 24 / 39 / 22
+// and 37 / 53 / 22; K = 16, up to 192 rows, 512 x 1408 31 / 30 / 22 and 32 / 35 / 24; fp32, K = 4, 1024 rows, 1024 x 2816 449 / 416 / 429 and 536 / 410 / 517.
+// Of 64, K = 8, 48 rows, 2048 x 5504 66 / 94, of 256 151 / 98; of 16 with 4 rows 59 / 64.
 template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
 {
     if (FORM != DW && d.r.most <= 16u) return 16u;
@@ -444,7 +447,8 @@ template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
     return tiles_of<FORM>(d, cols, 256, FORM == FWD ? 128 : 256) >= 2 * kCus ? 256u : 128u;
 }
 
-// Workgroups that share a tile of dx, in units of the contraction that every step divides: a contraction of 2 wide, and often few tiles.
+// Workgroups that share a tile of dx, in units of the contraction that every step divides: a contraction of 2 wide, and often few tiles.  us alone / shared, with the
+// sum of the shares: K = 8, 4 rows, 2048 x 5504 179 / 64; 48 rows 185 / 85; K = 2, 512 rows, 1024 x 2816 58 / 39; K = 16, up to 192 rows, 512 x 1408 32 / 30.
 constexpr uint32_t kUnit = 64;
 struct Split {
     uint32_t count;
@@ -498,15 +502,13 @@ template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool 
         }
     }
     const uint32_t tm = tile_rows<FORM>(d, a.cols);
-    if constexpr (FORM == FWD) {
-        // Weights in the cache (K = 4, 1 row, 2048 x 5504, 180 MB): 28 us without the hint, 34 with it; beyond it (K = 8, 4 rows) 75 and 70.
+    if constexpr (FORM != DW) {
+        // The hint on weights beyond the cache.  us, bf16, 2048 x 5504, without / with it: K = 4, 1 row (180 MB) forward 28 / 34; K = 8 (361 MB), 4 rows, forward 75 / 70,
+        // backward 67 / 58; 48 rows 128 / 66 and 115 / 84.
         const bool hint = 2 * (uint64_t)d.es * d.v.K * a.wide * a.cols >= kBeyondCache;
-        if (tm == 16u) return hint ? launch_big<FORM, 16, 128, 1, 4, 8, 2, true>(d, a, split, nullptr, st) : launch_big<FORM, 16, 128, 1, 4, 8, 2>(d, a, split, nullptr, st);
-        if (tm == 64u) return launch_big<FORM, 64, 128, 1, 4, 8, 2>(d, a, split, nullptr, st);
-    }
-    if constexpr (FORM == DX) {
-        if (tm == 16u) return launch_big<FORM, 16, 256, 1, 4, 8, 2, true>(d, a, split, part, st);
-        if (tm == 64u) return launch_big<FORM, 64, 256, 1, 4, 8, 2>(d, a, split, part, st);
+        constexpr uint32_t TN = FORM == FWD ? 128 : 256;
+        if (tm == 16u) return hint ? launch_big<FORM, 16, TN, 1, 4, 8, 2, true>(d, a, split, part, st) : launch_big<FORM, 16, TN, 1, 4, 8, 2>(d, a, split, part, st);
+        if (tm == 64u) return hint ? launch_big<FORM, 64, TN, 1, 4, 8, 2, true>(d, a, split, part, st) : launch_big<FORM, 64, TN, 1, 4, 8, 2>(d, a, split, part, st);
     }
     if (tm == 128u) launch_big<FORM, 128, 128, 2, 2, 8, 2>(d, a, split, part, st);
     else launch_big<FORM, 256, 256, 2, 4, 8, 2>(d, a, split, part, st);

@@ -195,3 +195,68 @@ def test_unbound_replicas_are_refused(exe):
     for name in ("norm", "back", "gated", "gback"):
         assert _call(exe, name, "f32", "unbound").startswith(f"{B.ERR_STATE} ")
     assert _call(exe, "drop", "f32", "unbound").startswith(f"{B.ERR_HIP} ")       # needs no parameters
+
+
+# ---- generated code -------------------------------------------------------------------------------------------------------
+KERNELS = r'''
+#include "%s/paper_2203_13085_amd/csrc/lasgd_gated.hip.h"
+namespace lasgd {
+template __global__ void dropout_kernel<true, STREAM>(const DropoutArgs);
+template __global__ void rms_norm_kernel<true, WIDE, 64, 4, false>(const NormRowsArgs);
+template __global__ void rms_norm_kernel<false, WIDE, 1024, 2, true>(const NormRowsArgs);
+template __global__ void rms_norm_backward_kernel<true, WIDE, 256, 1>(const NormBackArgs);
+template __global__ void rms_norm_backward_kernel<false, WIDE, 1024, 2>(const NormBackArgs);
+template __global__ void gates_backward_kernel<true, WIDE>(const GatesArgs);
+template __global__ void product_kernel<true, FWD, false, false, 128>(const ProductArgs);
+template __global__ void product_kernel<false, DW, true, false, 128>(const ProductArgs);
+template __global__ void big_product_kernel<true, FWD, 256, 256, 2, 4, 8, 2, false>(const ProductArgs, const TileMap);
+template __global__ void big_product_kernel<true, DX, 256, 256, 2, 4, 8, 2, false>(const ProductArgs, const TileMap);
+template __global__ void big_product_kernel<true, DW, 256, 256, 2, 4, 8, 2, false>(const ProductArgs, const TileMap);
+template __global__ void big_product_kernel<false, DX, 128, 128, 2, 2, 8, 2, false>(const ProductArgs, const TileMap);
+template __global__ void big_product_kernel<true, DX, 16, 256, 1, 4, 8, 2, true>(const ProductArgs, const TileMap);
+template __global__ void few_rows_weights_kernel<true, STREAM>(const ProductArgs);
+}
+'''
+
+
+@pytest.fixture(scope="module")
+def asm(tmp_path_factory):
+    d = tmp_path_factory.mktemp("layers_isa")
+    src, out = str(d / "kernels.hip"), str(d / "kernels.s")
+    with open(src, "w") as f:
+        f.write(KERNELS % ROOT)
+    flags = [f for f in build_mod.FLAGS if f not in ("-shared", "-fPIC")]
+    subprocess.check_call([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")] + flags + ["--cuda-device-only", "-S", "-o", out, src], stderr=subprocess.DEVNULL)
+    text = open(out).read()
+    return {m.group(1): text[m.start():text.index(".end_amdhsa_kernel", m.start())] for m in re.finditer(r"\n(_ZN5lasgd\S*):", text)}
+
+
+def test_kernels_stay_in_registers(asm):
+    assert len(asm) == 14
+    for name, body in asm.items():
+        assert re.search(r"\.amdhsa_private_segment_fixed_size 0\b", body), name
+        assert not re.search(r"\b(scratch|flat)_(load|store)", body), name
+        assert not re.search(r"v_pk_(add|mul|fma)_f32", body), name
+
+
+def test_tiles_go_straight_into_lds_and_nothing_waits_for_them_there(asm):
+    """From the barrier that says a step is there to its last product, no wait for loads: those under way belong to later steps. (A compiler that takes them for
+    what is being read waits for all of them, and a tile takes twice as long.)"""
+    big = {n: b for n, b in asm.items() if "big_product" in n}
+    assert len(big) == 5
+    for name, body in big.items():
+        assert re.search(r"buffer_load_dwordx4 [^\n]* lds", body)
+        loop = body[body.rindex("s_barrier", 0, body.index("v_mfma")):body.rindex("v_mfma")]
+        loop = re.sub(r";;#ASMSTART.*?;;#ASMEND", "", loop, flags=re.S)               # the waits that are written out
+        assert len(re.findall("v_mfma", loop)) >= 7, name
+        assert not re.search(r"vmcnt", loop), name
+        assert re.search("ds_read_b64_tr_b16" if re.search("ILb1ELi[12]E", name) else "ds_read_b128", loop), name
+
+
+@pytest.mark.parametrize("name,vgprs", [("dropout_kernel", 96), ("rms_norm_kernelILb1E", 72), ("rms_norm_backward_kernelILb1E", 102)])
+def test_row_kernels_leave_room_for_waves(asm, name, vgprs):
+    """At least five waves a SIMD of a norm's backward pass and of dropout, seven of a norm."""
+    bodies = [b for n, b in asm.items() if name in n]
+    assert bodies
+    for body in bodies:
+        assert int(re.search(r"\.amdhsa_next_free_vgpr (\d+)", body).group(1)) <= vgprs
