@@ -122,6 +122,32 @@ def test_dropout_edges(storage):
     m.close()
 
 
+@pytest.mark.parametrize("storage,K,n,cols", [("bf16", 3, 4096, 4096), ("f32", 2, 4096, 4104)])
+def test_calls_beyond_the_cache_give_the_same_bits(storage, K, n, cols):
+    """Accesses with the streaming hint (over 256 MiB a call), against the replicas one by one, without: dropout, a norm in either output, its backward pass."""
+    dt, gen = dtype_of(storage), generator(22)
+    m = Model(K, [(cols,)], storage, gen, plus=1.0)
+    x, res = (torch.randn(K, n, cols, generator=gen, device=DEV).to(dt) for _ in range(2))
+    at = lambda t: (t.data_ptr(), t.stride(0), t.stride(1))  # noqa: E731
+
+    def all_of(masks):
+        out = {name: torch.zeros(K, n, cols, dtype=torch.uint8 if name == "q" else dt, device=DEV) for name in ("d", "h", "y", "q", "dx", "dr")}
+        scales = torch.zeros(K, n, device=DEV)
+        for rows in masks:
+            drop = dict(p=0.3, seed=SEED, call=CALL)
+            m.ctx.dropout(rows, cols, at(x), at(out["d"]), 0.3, residual=at(res), seed=SEED, call=CALL)
+            m.ctx.rms_norm(0, rows, at(x), at(out["y"]), residual=at(res), sum=at(out["h"]), **drop)
+            m.ctx.rms_norm(0, rows, at(x), at(out["q"]), residual=at(res), scales=(scales.data_ptr(), n, 1), **drop)
+            work = workspace(m.ctx.rms_norm_backward_bytes(0, rows))
+            m.ctx.rms_norm_backward(0, rows, at(out["h"]), at(out["y"]), at(out["dx"]), dsum=at(x), dresidual=at(out["dr"]), workspace=work.data_ptr(),
+                                    workspace_bytes=work.numel(), **drop)
+            torch.cuda.synchronize()
+        return [*out.values(), scales]
+    for a, b in zip(all_of([[n] * K]), all_of([[n if k == i else 0 for k in range(K)] for i in range(K)])):
+        assert torch.equal(a, b)
+    m.close()
+
+
 # ---- norms -------------------------------------------------------------------------------------------------------------------
 NORMS = [  # rows, cols, layout: every shape of the kernels, and columns on either side of their limits
     ([1], 1, "dense"),
@@ -224,7 +250,7 @@ def test_rms_norm_in_8_bits_takes_the_nearest_value(storage):
 
 
 def test_rms_norm_without_numbers():
-    """An infinity or a NaN stays in its row; a row of zeros gives zeros, whatever eps."""
+    """An infinity or a NaN stays in its row; a row of zeros gives zeros."""
     gen = generator(5)
     m = Model(1, [(96,)], "f32", gen)
     x, y = Act([4], 96, torch.float32, "dense", gen), Act([4], 96, torch.float32)
@@ -341,6 +367,14 @@ GATED = [  # rows, cols, wide, layout
 ]
 
 
+LARGE = [  # what only many tiles or many bytes take: tiles of 256 and, unaligned, of 128; weights beyond the cache with few rows
+    ([512, 300, 0, 511] + [257] * 60, 1032, 1000, "dense", "silu"),
+    ([256, 129, 0, 255] + [200] * 12, 2051, 1030, "odd", "gelu"),
+    ([3, 0, 16] + [5] * 61, 1032, 1024, "dense", "relu"),
+    ([40, 64, 0] + [17] * 61, 1032, 1024, "turned", "gelu_tanh"),
+]
+
+
 def _product_off(deep, storage):
     """Roundings of a sum of `deep` products, in any order; twice that, for what the matrix units do not round to nearest."""
     return 2 * (deep + 2) * U
@@ -363,6 +397,16 @@ def _block(rows, cols, wide, layout, act, storage, seed=9, packed=False):
 @pytest.mark.parametrize("rows,cols,wide,layout", GATED)
 @pytest.mark.parametrize("act,packed", [("silu", False), ("gelu", True), ("gelu_tanh", False), ("relu", False)])
 def test_gated(rows, cols, wide, layout, act, packed, storage):
+    check_gated(rows, cols, wide, layout, act, packed, storage)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,wide,layout,act", LARGE)
+def test_gated_large(rows, cols, wide, layout, act, storage):
+    check_gated(rows, cols, wide, layout, act, False, storage)
+
+
+def check_gated(rows, cols, wide, layout, act, packed, storage):
     m, (i, j), x, g, u, a, weights, _ = _block(rows, cols, wide, layout, act, storage, packed=packed)
     dt, off = m.dt, _product_off(cols, storage)
     alone = Act(rows, wide, dt, "dense")
@@ -388,6 +432,17 @@ def test_gated(rows, cols, wide, layout, act, packed, storage):
 @pytest.mark.parametrize("rows,cols,wide,layout", GATED)
 @pytest.mark.parametrize("act,packed,accumulate", [("silu", False, False), ("gelu", True, True), ("gelu_tanh", False, True), ("relu", False, False)])
 def test_gated_backward(rows, cols, wide, layout, act, packed, accumulate, storage):
+    check_gated_backward(rows, cols, wide, layout, act, packed, accumulate, storage)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("rows,cols,wide,layout,act", LARGE)
+def test_gated_backward_large(rows, cols, wide, layout, act, accumulate, storage):
+    check_gated_backward(rows, cols, wide, layout, act, False, accumulate, storage)
+
+
+def check_gated_backward(rows, cols, wide, layout, act, packed, accumulate, storage):
     m, (i, j), x, g, u, a, weights, grads = _block(rows, cols, wide, layout, act, storage, packed=packed)
     dt, gen = m.dt, generator(10)
     da, dx = Act(rows, wide, dt, layout, gen), Act(rows, cols, dt, layout)
@@ -552,4 +607,44 @@ def test_gradients_go_where_the_step_reads_them():
     for i in range(3):
         want = before[i] - 0.5 * 1.9 * m.g[i][1].double()           # Nesterov momentum 0.9 from a buffer of zeros
         within(m.w[i][1], want, 4 * U * (before[i].abs() + m.g[i][1].double().abs()), str(i))
+    m.close()
+
+
+def test_offsets_beyond_32_bits():
+    """Rows a GiB and replicas 4 GiB apart, all activations between each other in one buffer: the same as from dense ones."""
+    K, n, cols, wide, gen = 2, 3, 64, 48, generator(23)
+    buf = torch.empty((1 << 31) + 2 * (1 << 29) + 16 * 4096, dtype=torch.bfloat16, device=DEV)
+    m = Model(K, [(cols,), (wide, cols), (wide, cols)], "bf16", gen, scales=[1.0, 0.1, 0.1])
+    place = {}
+
+    def far(name, width):
+        place[name] = place.get(name, len(place))
+        return buf.as_strided((K, n, width), (1 << 31, 1 << 29, 1), 4096 * place[name])
+
+    def dense(name, width):
+        place[name] = place.get(name) if isinstance(place.get(name), torch.Tensor) else torch.zeros(K, n, width, dtype=torch.bfloat16, device=DEV)
+        return place[name]
+    x0, r0, d0 = (torch.randn(K, n, cols, generator=gen, device=DEV).bfloat16() for _ in range(3))
+    at = lambda t: (t.data_ptr(), t.stride(0), t.stride(1))  # noqa: E731
+    results = []
+    for make in (dense, far):
+        place.clear()
+        m.ctx.zero_grads()
+        rows = [n] * K
+        x, r, dy = make("x", cols), make("r", cols), make("dy", cols)
+        x.copy_(x0), r.copy_(r0), dy.copy_(d0)
+        out = {name: make(name, wide if name in ("a", "g", "u") else cols) for name in ("d", "h", "y", "a", "g", "u", "dx", "dr", "dz")}
+        work = workspace(max(m.ctx.rms_norm_backward_bytes(0, rows), m.ctx.gated_backward_bytes(1, 2, rows, cols)))
+        m.ctx.dropout(rows, cols, at(x), at(out["d"]), 0.5, residual=at(r), seed=1, call=2)
+        m.ctx.rms_norm(0, rows, at(x), at(out["y"]), residual=at(r), sum=at(out["h"]), p=0.5, seed=1, call=2)
+        m.ctx.rms_norm_backward(0, rows, at(out["h"]), at(dy), at(out["dx"]), dsum=at(r), dresidual=at(out["dr"]), p=0.5, seed=1, call=2,
+                                workspace=work.data_ptr(), workspace_bytes=work.numel())
+        m.ctx.gated(1, 2, rows, cols, at(x), at(out["a"]), g=at(out["g"]), u=at(out["u"]))
+        m.ctx.gated_backward(1, 2, rows, cols, at(x), at(out["g"]), at(out["u"]), at(out["a"]), at(out["dz"]), workspace=work.data_ptr(),
+                             workspace_bytes=work.numel())
+        torch.cuda.synchronize()
+        results.append([t.clone() for t in out.values()] + [g.float() for _, g in m.g])
+    for i, (a, b) in enumerate(zip(*results)):
+        # rows this far apart take the other kernels of the products: the same sums in another order, and a rounding may fall the other way
+        assert torch.equal(a, b) if i < 3 or i in (6, 7) else torch.allclose(a.float(), b.float(), rtol=2.0 ** -6, atol=2.0 ** -9), i
     m.close()
