@@ -100,16 +100,84 @@ struct ProductArgs {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// ---- a tile's sides in LDS ------------------------------------------------------------------------------------------------------------
+//   - A side whose contraction is contiguous in memory (ALONG) lies in LDS as [row][LP pieces of 16 bytes], and is read 16 bytes a lane.  Piece p of row i is
+//     at p ^ (i & 7), or p ^ (i / 2 & 3) where a step has four: eight rows' equal pieces are in eight different places of 128 bytes.
+//   - A side whose rows are contiguous (ACROSS) lies as [contraction][T elements].  bf16: read by the transposing read, 16 lanes of which take 4 lines of 16
+//     columns, and a lane gets one column of them; piece p of line c is at p ^ 2 (c & 3) ^ (c & 8) (where a line has sixteen), so that the 8 lines that half a wave reads
+//     are in eight different places of 256 bytes.  fp32: read an element a lane; p ^ (c & 12): the four lines of a wave are in four different places.
+template <bool BF16> struct Width {
+    static constexpr uint32_t bytes = BF16 ? 2 : 4, piece = 16u / bytes, deep = 4u * piece;        // of an element; elements; a fragment's contraction
+};
+// Where piece p of a line is.
+template <uint32_t LP> __device__ __forceinline__ uint32_t along_place(uint32_t row, uint32_t p) { return p ^ (LP == 8u ? row & 7u : row >> 1 & 3u); }
+template <bool BF16, uint32_t T> __device__ __forceinline__ uint32_t across_place(uint32_t line, uint32_t p)
+{
+    static_assert(T >= 64u, "a line has all the places");
+    return p ^ (BF16 ? (line & 3u) * 2u ^ (T >= 128u ? line & 8u : 0u) : line & 12u);
+}
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// What a lane has of 16 rows from row0 on and of the contraction from c0 on: row lane % 16, and of 32 (bf16: 16 bytes) or 16 (fp32) of the contraction
+// the share of its quarter of the wave.  Both sides take it in the same order, which is all that counts.
+template <bool BF16> struct Frag { typedef f32x4 type; };
+template <> struct Frag<true> { typedef bf16x8 type; };
+template <bool BF16, uint32_t LP, bool ALONG, uint32_t T>
+__device__ __forceinline__ typename Frag<BF16>::type fragment(const lds_char *lds, uint32_t row0, uint32_t c0)
+{
+    const uint32_t lane = threadIdx.x & 63u, quad = lane >> 4, i = lane & 15u;
+    if constexpr (ALONG) {
+        const uint32_t row = row0 + i, piece = along_place<LP>(row, c0 / Width<BF16>::piece + quad);
+        return *reinterpret_cast<const __attribute__((address_space(3))) typename Frag<BF16>::type *>(lds + row * (LP * 16u) + piece * 16u);
+    } else if constexpr (BF16) {
+        const uint32_t line = c0 + quad * 8u + (i >> 2), piece = across_place<true, T>(line, row0 / 8u + ((i & 3u) >> 1));
+        const lds_char *at = lds + line * (T * 2u) + piece * 16u + (i & 1u) * 8u;            // four lines on: the same place in its line
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4u * T * 2u));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        const uint32_t line = c0 + quad * 4u, piece = across_place<false, T>(line, (row0 + i) / 4u);
+        const lds_char *at = lds + line * (T * 4u) + piece * 16u + (i & 3u) * 4u;
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const __attribute__((address_space(3))) float *>(at + e * T * 4u);
+        return v;
+    }
+}
+
+// acc += what fragments of both sides make: element (n = 4 * (lane / 16) + reg, m = lane % 16) of each 16 x 16.
+template <bool BF16, uint32_t FM, uint32_t FN>
+__device__ __forceinline__ void products(f32x4 (&acc)[FM][FN], const typename Frag<BF16>::type (&m)[FM], const typename Frag<BF16>::type (&n)[FN])
+{
+    if constexpr (BF16) {
+#pragma unroll
+        for (uint32_t i = 0; i < FM; ++i) {
+#pragma unroll
+            for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m[i], acc[i][j], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+            for (uint32_t i = 0; i < FM; ++i) {
+#pragma unroll
+                for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(n[j][e], m[i][e], acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+}
+
 // ---- any size, stride and alignment ------------------------------------------------------------------------------------------
-// Tiles of T x T (FWD: half of the columns gate's, half up's), four waves, 32 of the contraction at a time through LDS, where both sides lie [T][32] whatever
-// they are in memory; what is outside is zero there.  The next 32 are asked for, in the widest accesses that the alignment allows, before these are multiplied.
+// Tiles of T x T (FWD: half of the columns gate's, half up's), four waves, 32 of the contraction at a time; what is outside is zero in LDS.  The next 32 are asked for, in
+// the widest accesses that the alignment allows, before these are multiplied, and go into the other of two buffers after that.  bf16, K = 8, 2048 rows,
+// 2047 x 5503: TIME_L.
 constexpr uint32_t kDeep = 32;
 
-template <bool BF16> struct Elem { typedef float type; static constexpr uint32_t pitch = kDeep + 4; };
-template <> struct Elem<true> { typedef uint16_t type; static constexpr uint32_t pitch = kDeep + 8; };
-
-// One side's tile: element (i, c) of i < ni, c < nc is at p + i * stride + c (ALONG) or p + c * stride + i.  A thread has eight next to each other in memory
-// of every 64 rows.  VEC: these are aligned, and ni or nc counts whole eights.
+// Eight elements of a side's tile next to each other in memory: element (i, c) of i < ni, c < nc is at p + i * stride + c (ALONG) or p + c * stride + i.  A thread has
+// some of every 64 rows.  VEC: these are aligned, and ni or nc counts whole eights.
 template <bool BF16, bool ALONG, bool VEC>
 __device__ __forceinline__ Raw8<BF16> ask(const char *p, int64_t stride, int64_t i, int64_t ni, int64_t c, int64_t nc)
 {
@@ -121,76 +189,14 @@ __device__ __forceinline__ Raw8<BF16> ask(const char *p, int64_t stride, int64_t
 }
 template <bool ALONG> __device__ __forceinline__ uint32_t own_row() { return ALONG ? threadIdx.x >> 2 : (threadIdx.x & 7u) * 8u; }
 template <bool ALONG> __device__ __forceinline__ uint32_t own_deep() { return ALONG ? (threadIdx.x & 3u) * 8u : threadIdx.x >> 3; }
-template <bool BF16, bool ALONG>
-__device__ __forceinline__ void put(typename Elem<BF16>::type *lds, const Raw8<BF16> &r)
-{
-    constexpr uint32_t P = Elem<BF16>::pitch;
-    typename Elem<BF16>::type *at = lds + own_row<ALONG>() * P + own_deep<ALONG>();
-    if constexpr (ALONG) {
-#pragma unroll
-        for (int i = 0; i < (BF16 ? 1 : 2); ++i) *reinterpret_cast<u32x4 *>(at + i * 4) = r.w[i];
-    } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 8u; ++j) {
-            if constexpr (BF16) at[j * P] = (uint16_t)(r.w[0][j >> 1] >> (16u * (j & 1u)));
-            else at[j * P] = __uint_as_float(r.w[j >> 2][j & 3u]);
-        }
-    }
-}
-
-// Column of C that a wave's fragment j of the n side starts with, in its half of the tile's lines in LDS (FWD: first gate's, then up's).
-template <int FORM, uint32_t T> __device__ __forceinline__ uint32_t loose_n_row(uint32_t wn, uint32_t j)
-{
-    if constexpr (FORM == FWD) return (j >= T / 64u ? T / 2u + (j - T / 64u) * 16u : j * 16u) + wn * (T / 4u);
-    else return wn * (T / 2u) + j * 16u;
-}
-
-// acc += the tile's part of C: element (n = 4 * (lane / 16) + reg, m = lane % 16) of each 16 x 16.
-template <bool BF16, int FORM, uint32_t T>
-__device__ __forceinline__ void multiply(f32x4 (&acc)[T / 32u][T / 32u], const typename Elem<BF16>::type *m, const typename Elem<BF16>::type *n, uint32_t wm, uint32_t wn)
-{
-    constexpr uint32_t P = Elem<BF16>::pitch, F = T / 32u;
-    const uint32_t lane = threadIdx.x & 63u, row = lane & 15u, quad = lane >> 4;
-    if constexpr (BF16) {
-        bf16x8 fm[F], fn[F];
-#pragma unroll
-        for (uint32_t i = 0; i < F; ++i) {
-            fm[i] = *reinterpret_cast<const bf16x8 *>(m + (wm * (T / 2u) + i * 16u + row) * P + quad * 8u);
-            fn[i] = *reinterpret_cast<const bf16x8 *>(n + (loose_n_row<FORM, T>(wn, i) + row) * P + quad * 8u);
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < F; ++i) {
-#pragma unroll
-            for (uint32_t j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fn[j], fm[i], acc[i][j], 0, 0, 0);
-        }
-    } else {
-#pragma unroll
-        for (uint32_t c = 0; c < kDeep; c += 16u) {               // a lane's four of the contraction next to each other, on both sides
-            f32x4 fm[F], fn[F];
-#pragma unroll
-            for (uint32_t i = 0; i < F; ++i) {
-                fm[i] = *reinterpret_cast<const f32x4 *>(m + (wm * (T / 2u) + i * 16u + row) * P + c + quad * 4u);
-                fn[i] = *reinterpret_cast<const f32x4 *>(n + (loose_n_row<FORM, T>(wn, i) + row) * P + c + quad * 4u);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-#pragma unroll
-                for (uint32_t i = 0; i < F; ++i) {
-#pragma unroll
-                    for (uint32_t j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fn[j][e], fm[i][e], acc[i][j], 0, 0, 0);
-                }
-            }
-        }
-    }
-}
 
 template <bool BF16, int FORM, bool VM, bool VN, uint32_t T>
 __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
 {
-    typedef typename Elem<BF16>::type E;
-    constexpr uint32_t ES = BF16 ? 2u : 4u, P = Elem<BF16>::pitch, R = T / 64u, F = T / 32u, NT = FORM == FWD ? T / 2u : T;
+    constexpr uint32_t ES = Width<BF16>::bytes, LP = kDeep / Width<BF16>::piece, R = T / 64u, F = T / 32u, NT = FORM == FWD ? T / 2u : T, SIDE = T * LP * 16u;
     constexpr bool ALONG_M = FORM != DW, ALONG_N = FORM == FWD;
-    __shared__ __attribute__((aligned(16))) E ldsm[T * P], ldsn[T * P];
+    __shared__ __attribute__((aligned(1024))) char mem[4u * SIDE];
+    lds_char *lds = (lds_char *)mem;
     const uint32_t k = blockIdx.y;
     const int64_t rows = a.rows[k], cols = a.cols, wide = a.wide;
     const int64_t M = FORM == DW ? wide : rows, N = FORM == FWD ? wide : cols;
@@ -220,25 +226,53 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
             }
         }
     };
-    const int64_t steps1 = (deep + kDeep - 1) / kDeep, steps = FORM == DX ? 2 * steps1 : steps1;
-    if (steps) ask_both(0, 0);
-    for (int64_t s = 0; s < steps; ++s) {
+    auto put = [&](auto along, lds_char *to, const Raw8<BF16> &r, uint32_t q) {
+        constexpr bool ALONG = decltype(along)::value;
+        const uint32_t row = q * 64u + own_row<ALONG>(), c = own_deep<ALONG>();
+#pragma unroll
+        for (uint32_t i = 0; i < 8u / Width<BF16>::piece; ++i) {
+            uint32_t at;
+            if constexpr (ALONG) at = row * LP + along_place<LP>(row, c / Width<BF16>::piece + i);
+            else at = c * (T / Width<BF16>::piece) + across_place<BF16, T>(c, row / Width<BF16>::piece + i);
+            *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(to + at * 16u) = r.w[i];
+        }
+    };
+    auto put_both = [&](uint32_t buffer) {
 #pragma unroll
         for (uint32_t q = 0; q < R; ++q) {
-            put<BF16, ALONG_M>(ldsm + q * 64u * P, rm[q]);
-            put<BF16, ALONG_N>(ldsn + q * 64u * P, rn[q]);
+            put(std::bool_constant<ALONG_M>{}, lds + buffer * 2u * SIDE, rm[q], q);
+            put(std::bool_constant<ALONG_N>{}, lds + buffer * 2u * SIDE + SIDE, rn[q], q);
         }
+    };
+    // column of C that a wave's fragment j of the n side starts with (FWD: j < F / 2 gate's, then up's), and where it is among the tile's lines in LDS
+    auto n_col = [&](uint32_t j) { return FORM == FWD ? wn * (T / 4u) + j % (F / 2u) * 16u : wn * (T / 2u) + j * 16u; };
+    const int64_t steps1 = (deep + kDeep - 1) / kDeep, steps = FORM == DX ? 2 * steps1 : steps1;
+    if (steps) {
+        ask_both(0, 0);
+        put_both(0u);
+    }
+    for (int64_t s = 0; s < steps; ++s) {
         __syncthreads();
         if (s + 1 < steps) ask_both(FORM == DX && s + 1 >= steps1, (FORM == DX && s + 1 >= steps1 ? s + 1 - steps1 : s + 1) * kDeep);
-        multiply<BF16, FORM, T>(acc, ldsm, ldsn, wm, wn);
-        __syncthreads();
+        const lds_char *side = lds + ((uint32_t)s & 1u) * 2u * SIDE;
+#pragma unroll
+        for (uint32_t c = 0; c < kDeep; c += Width<BF16>::deep) {
+            typename Frag<BF16>::type m[F], n[F];
+#pragma unroll
+            for (uint32_t i = 0; i < F; ++i) {
+                m[i] = fragment<BF16, LP, ALONG_M, T>(side, wm * (T / 2u) + i * 16u, c);
+                n[i] = fragment<BF16, LP, ALONG_N, T>(side + SIDE, n_col(i) + (FORM == FWD && i >= F / 2u ? T / 2u : 0u), c);
+            }
+            products<BF16, F, F>(acc, m, n);
+        }
+        if (s + 1 < steps) put_both(((uint32_t)s + 1u) & 1u);
     }
     const uint32_t lane = threadIdx.x & 63u;
 #pragma unroll
     for (uint32_t i = 0; i < F; ++i) {
 #pragma unroll
         for (uint32_t j = 0; j < (FORM == FWD ? F / 2u : F); ++j) {
-            const int64_t m = m0 + wm * (T / 2u) + i * 16 + (lane & 15u), n1 = n0 + loose_n_row<FORM, T>(wn, j) + (lane >> 4) * 4u;
+            const int64_t m = m0 + wm * (T / 2u) + i * 16 + (lane & 15u), n1 = n0 + n_col(j) + (lane >> 4) * 4u;
             if (m >= M) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -271,29 +305,13 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
 //
 // A workgroup makes TM x TN of C, wave by wave, and takes the contraction a step (LP pieces of 16 bytes) at a time through NS
 // buffers in LDS: while the waves multiply one, the next ones are on their way from memory straight into the others.
-//   - A side whose contraction is contiguous in memory (ALONG) lies in LDS as [row][LP pieces], and is read 16 bytes a lane.  Piece p of row i is
-//     at p ^ (i & 7), or p ^ (i / 2 & 3) where a step has four: eight rows' equal pieces are in eight different places of 128 bytes.
-//   - A side whose rows are contiguous (ACROSS) lies as [contraction][T elements].  bf16: read by the transposing read, 16 lanes of which take 4 lines of 16
-//     columns, and a lane gets one column of them; piece p of line c is at p ^ 2 (c & 3) ^ (c & 8), so that the 8 lines that half a wave reads
-//     are in eight different places of 256 bytes.  fp32: read an element a lane; p ^ (c & 12): the four lines of a wave are in four different places.
 // What is outside is asked for beyond the end of a buffer resource, which gives zeros.
-template <bool BF16> struct Width {
-    static constexpr uint32_t bytes = BF16 ? 2 : 4, piece = 16u / bytes, deep = 4u * piece;        // of an element; elements; a fragment's contraction
-};
-// Where piece p of a line is.
-template <uint32_t LP> __device__ __forceinline__ uint32_t along_place(uint32_t row, uint32_t p) { return p ^ (LP == 8u ? row & 7u : row >> 1 & 3u); }
-template <bool BF16> __device__ __forceinline__ uint32_t across_place(uint32_t line, uint32_t p) { return p ^ (BF16 ? (line & 3u) * 2u ^ (line & 8u) : line & 12u); }
-
 // A tile's place and how far what may be read reaches from there: T lines along, or a step's lines across.
 struct Side {
     const char *p;               // of the tile's first element
     int64_t bytes;               // from there to the end of what is there
     int64_t stride;              // bytes from one line to the next
 };
-
-typedef __attribute__((address_space(3))) char lds_char;
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ uint32_t records(int64_t bytes) { return bytes <= 0 ? 0u : bytes > 0xfffffff0ll ? 0xfffffff0u : (uint32_t)bytes; }
 
@@ -309,37 +327,12 @@ __device__ __forceinline__ void fetch(lds_char *lds, const Side &s, int64_t left
     for (uint32_t i = 0; i < (PIECES + THREADS - 1u) / THREADS; ++i) {
         if ((i + 1u) * THREADS > PIECES && i * THREADS + wave * 64u >= PIECES) break;
         const uint32_t at = i * THREADS + threadIdx.x, line = at / LINE;
-        const uint32_t piece = ALONG ? along_place<LP>(line, at % LINE) : across_place<BF16>(line, at % LINE);
+        uint32_t piece;
+        if constexpr (ALONG) piece = along_place<LP>(line, at % LINE);
+        else piece = across_place<BF16, T>(line, at % LINE);
         uint32_t off = line * (uint32_t)s.stride + piece * 16u;
         if (ALONG && (int64_t)(piece * Width<BF16>::piece) >= left) off = 0xfffffff0u;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64u) * 16u), 16, off, 0, 0, HINT ? 2 : 0);
-    }
-}
-
-// What a lane has of 16 rows from row0 on and of the contraction from c0 on: row lane % 16, and of 32 (bf16: 16 bytes) or 16 (fp32) of the contraction
-// the share of its quarter of the wave.  Both sides take it in the same order, which is all that counts.
-template <bool BF16> struct Frag { typedef f32x4 type; };
-template <> struct Frag<true> { typedef bf16x8 type; };
-template <bool BF16, uint32_t LP, bool ALONG, uint32_t T>
-__device__ __forceinline__ typename Frag<BF16>::type fragment(const lds_char *lds, uint32_t row0, uint32_t c0)
-{
-    const uint32_t lane = threadIdx.x & 63u, quad = lane >> 4, i = lane & 15u;
-    if constexpr (ALONG) {
-        const uint32_t row = row0 + i, piece = along_place<LP>(row, c0 / Width<BF16>::piece + quad);
-        return *reinterpret_cast<const __attribute__((address_space(3))) typename Frag<BF16>::type *>(lds + row * (LP * 16u) + piece * 16u);
-    } else if constexpr (BF16) {
-        const uint32_t line = c0 + quad * 8u + (i >> 2), piece = across_place<true>(line, row0 / 8u + ((i & 3u) >> 1));
-        const lds_char *at = lds + line * (T * 2u) + piece * 16u + (i & 1u) * 8u;            // four lines on: the same place in its line
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4u * T * 2u));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-        const uint32_t line = c0 + quad * 4u, piece = across_place<false>(line, (row0 + i) / 4u);
-        const lds_char *at = lds + line * (T * 4u) + piece * 16u + (i & 3u) * 4u;
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const __attribute__((address_space(3))) float *>(at + e * T * 4u);
-        return v;
     }
 }
 
@@ -384,22 +377,7 @@ template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t W
             for (uint32_t j = 0; j < FN; ++j) n[j] = fragment<BF16, LP, along_n, TN>(lds + n_at, n_row(wn, j), c);
 #pragma unroll
             for (uint32_t i = 0; i < FM; ++i) m[i] = fragment<BF16, LP, along_m, TM>(lds, wm * (TM / WM) + i * 16u, c);
-            if constexpr (BF16) {
-#pragma unroll
-                for (uint32_t i = 0; i < FM; ++i) {
-#pragma unroll
-                    for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n[j], m[i], acc[i][j], 0, 0, 0);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-#pragma unroll
-                    for (uint32_t i = 0; i < FM; ++i) {
-#pragma unroll
-                        for (uint32_t j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(n[j][e], m[i][e], acc[i][j], 0, 0, 0);
-                    }
-                }
-            }
+            products<BF16, FM, FN>(acc, m, n);
             // The order of a fragment's worth: enough reads to begin with, then one after every FN products, four rows of fragments ahead.
             if constexpr (BF16 && FM > 4u) {
                 constexpr int NB = along_n ? 1 : 2, MB = along_m ? 1 : 2;
@@ -640,7 +618,7 @@ __global__ __launch_bounds__(256) void few_rows_weights_kernel(const ProductArgs
     char *grad = blockIdx.z ? a.up[k] : a.gate[k];
 #pragma unroll
     for (uint32_t t = threadIdx.x; t < kFewRows * T / 8u; t += 256u) {
-        const uint32_t line = t / (T / 8u), c = t % (T / 8u) * 8u, at = line * (T * 2u) + across_place<true>(line, c / 8u) * 16u;
+        const uint32_t line = t / (T / 8u), c = t % (T / 8u) * 8u, at = line * (T * 2u) + across_place<true, T>(line, c / 8u) * 16u;
         u32x4 h{}, m{};
         if (line < rows && f0 + c < a.pitch) h = *as_global<u32x4>(from + ((uint64_t)line * a.pitch + f0 + c) * 2u);
         if (line < rows && d0 + c < cols) m = *as_global<u32x4>(x + ((int64_t)line * a.x.ss + d0 + c) * 2);
