@@ -91,6 +91,7 @@ struct ProductArgs {
     const char *dg, *du;         // DX, DW: [rows of all replicas][pitch]
     uint32_t cols, wide, pitch;
     int32_t act, accumulate;
+    uint32_t tiles, tiles_m;     // product_kernel: of a replica, and of its rows
     int32_t wide_out;            // outputs take accesses of eight elements
     uint32_t rows[64];
     uint32_t first[64];
@@ -99,6 +100,16 @@ struct ProductArgs {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// A quotient: divisions are made by the vector unit, and what comes of one stays in vector registers, with all that is computed from it.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Workgroups are dealt out to the eight XCDs in turn; each XCD gets tiles that follow each other, which share their sides in its L2.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total)
+{
+    const uint32_t x = id & 7u, per = total >> 3, more = total & 7u;
+    return x * per + (x < more ? x : more) + (id >> 3);
+}
 
 // ---- a tile's sides in LDS ------------------------------------------------------------------------------------------------------------
 //   - A side whose contraction is contiguous in memory (ALONG) lies in LDS as [row][LP pieces of 16 bytes], and is read 16 bytes a lane.  Piece p of row i is
@@ -173,7 +184,8 @@ __device__ __forceinline__ void products(f32x4 (&acc)[FM][FN], const typename Fr
 // ---- any size, stride and alignment ------------------------------------------------------------------------------------------
 // Tiles of T x T (FWD: half of the columns gate's, half up's), four waves, 32 of the contraction at a time; what is outside is zero in LDS.  The next 32 are asked for, in
 // the widest accesses that the alignment allows, before these are multiplied, and go into the other of two buffers after that.  bf16, K = 8, 2048 rows,
-// 2047 x 5503: TIME_L.
+// 2047 x 5503: forward 1950 us, dx 1836, weights 1381 (380 to 540 TFLOP/s; with tiles in the order of rows and replicas spread over all XCDs 2083, 3346, 2281);
+// fp32, K = 4, 1023 rows, 1023 x 2815 487, 480, 448.
 constexpr uint32_t kDeep = 32;
 
 // Eight elements of a side's tile next to each other in memory: element (i, c) of i < ni, c < nc is at p + i * stride + c (ALONG) or p + c * stride + i.  A thread has
@@ -197,11 +209,11 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
     constexpr bool ALONG_M = FORM != DW, ALONG_N = FORM == FWD;
     __shared__ __attribute__((aligned(1024))) char mem[4u * SIDE];
     lds_char *lds = (lds_char *)mem;
-    const uint32_t k = blockIdx.y;
+    const uint32_t order = xcd_order(blockIdx.x, gridDim.x), k = uniform(order / a.tiles), tile = order - k * a.tiles;
     const int64_t rows = a.rows[k], cols = a.cols, wide = a.wide;
     const int64_t M = FORM == DW ? wide : rows, N = FORM == FWD ? wide : cols;
-    const uint32_t tn = (uint32_t)((N + NT - 1) / NT);
-    const int64_t m0 = (int64_t)(blockIdx.x / tn) * T, n0 = (int64_t)(blockIdx.x % tn) * NT;
+    const uint32_t tile_n = uniform(tile / a.tiles_m);                           // tiles next to each other have the same columns
+    const int64_t m0 = (int64_t)(tile - tile_n * a.tiles_m) * T, n0 = (int64_t)tile_n * NT;
     if (m0 >= M) return;
     const uint32_t w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1u;
     f32x4 acc[F][F] = {};
@@ -424,16 +436,6 @@ struct TileMap {
     float *part;                 // more than one: what each of them has, [splits][rows of all replicas][cols]
     uint64_t part_stride;        // elements from one split to the next
 };
-
-// A quotient: divisions are made by the vector unit, and what comes of one stays in vector registers, with all that is computed from it.
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// Workgroups are dealt out to the eight XCDs in turn; each XCD gets tiles that follow each other, which share their sides in its L2.
-__device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total)
-{
-    const uint32_t x = id & 7u, per = total >> 3, more = total & 7u;
-    return x * per + (x < more ? x : more) + (id >> 3);
-}
 
 template <bool BF16, int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, uint32_t LP, uint32_t NS, bool HINT>
 __global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, LP, NS, HINT>::threads)) void big_product_kernel(const ProductArgs a, const TileMap map)

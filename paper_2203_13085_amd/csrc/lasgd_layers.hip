@@ -372,7 +372,7 @@ lasgd_status check_gated(lasgd_ctx *c, Gated &d, int32_t gate, int32_t up, const
     d.wide = n / per;
     d.pitch = (d.wide + 7) / 8 * 8;
     // workgroups of a launch, at the smallest tiles there are (16 x 64, 32 splits and more only of few tiles)
-    const __int128 wide64 = (d.wide + 31) / 32, cols64 = (cols + 31) / 32, rows16 = (int64_t)d.r.total / 16 + d.v.K;
+    const __int128 wide64 = (d.wide + 31) / 32, cols64 = (cols + 31) / 32, rows16 = ((int64_t)d.r.most / 16 + 1) * d.v.K;
     CHECK(rows16 * wide64 <= kMaxBlocks / 4 && rows16 * cols64 <= kMaxBlocks / 4 && wide64 * cols64 * d.v.K <= kMaxBlocks, LASGD_ERR_UNSUPPORTED,
           "more workgroups than a launch has");
     return LASGD_OK;
@@ -426,10 +426,13 @@ template <int FORM> void launch_loose(const Gated &d, const ProductArgs &a, bool
     auto launch = [&](auto tile) {
         constexpr uint32_t T = decltype(tile)::value;
         const uint64_t M = FORM == DW ? d.wide : d.r.most, N = FORM == FWD ? a.wide : a.cols;
-        const dim3 grid(ceil_div(M, T) * ceil_div(N, FORM == FWD ? T / 2 : T), d.v.K, FORM == DW ? 2 : 1);
+        ProductArgs b = a;
+        b.tiles_m = ceil_div(M, T);
+        b.tiles = b.tiles_m * ceil_div(N, FORM == FWD ? T / 2 : T);
+        const dim3 grid(b.tiles * d.v.K, 1, FORM == DW ? 2 : 1);
         two_flags(vm, vn, [&](auto m, auto n) {
-            if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n, T>), grid, dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((product_kernel<false, FORM, m, n, T>), grid, dim3(256), 0, st, a);
+            if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n, T>), grid, dim3(256), 0, st, b);
+            else hipLaunchKernelGGL((product_kernel<false, FORM, m, n, T>), grid, dim3(256), 0, st, b);
         });
     };
     if (tiles_of<FORM>(d, a.cols, 128, FORM == FWD ? 64 : 128) >= 2 * kCus) launch(std::integral_constant<uint32_t, 128>{});
