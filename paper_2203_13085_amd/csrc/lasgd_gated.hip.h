@@ -1,7 +1,7 @@
 // Gated blocks of the replicas' forward and backward passes: device code.
 //     g = x Wg^T,  u = x Wu^T,  a = f(g) u
 //     dg = da u f'(g),  du = da f(g);   dx = dg Wg + du Wu,   dWg = dg^T x,  dWu = du^T x
-// Each replica (blockIdx.y) has weights of its own, as many rows as it likes, and all are in one launch.
+// Each replica has weights of its own and as many rows as it likes, and all are in one launch.
 #pragma once
 #include "lasgd_rows.hip.h"
 
@@ -30,13 +30,13 @@ template <bool BF16> __device__ __forceinline__ ActPair activation(int act, floa
         return {v * s, s * __builtin_fmaf(v, 1.f - s, 1.f)};
     }
     case ACT_GELU: {
-        const float cdf = 0.5f * (1.f + erff(v * 0.70710678118654752f));
+        const float cdf = 0.5f * erfcf(v * -0.70710678118654752f);             // 1 + erf would lose what is small
         return {v * cdf, __builtin_fmaf(v * 0.39894228040143268f, expf(-0.5f * v * v), cdf)};
     }
     case ACT_GELU_TANH: {
         constexpr float b = 0.79788456080286536f, c = 0.044715f;
-        const float t = tanhf(b * __builtin_fmaf(c * v * v, v, v));
-        return {0.5f * v * (1.f + t), 0.5f * (1.f + t) + 0.5f * v * (1.f - t * t) * b * __builtin_fmaf(3.f * c * v, v, 1.f)};
+        const float s = sigmoid<BF16>(2.f * b * __builtin_fmaf(c * v * v, v, v));             // (1 + tanh z) / 2
+        return {v * s, __builtin_fmaf(2.f * b * v * __builtin_fmaf(3.f * c * v, v, 1.f), s * (1.f - s), s)};
     }
     default: return {v > 0.f ? v : v == v ? 0.f : v, v > 0.f ? 1.f : 0.f};
     }
@@ -130,7 +130,6 @@ template <bool BF16, uint32_t T> __device__ __forceinline__ uint32_t across_plac
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // What a lane has of 16 rows from row0 on and of the contraction from c0 on: row lane % 16, and of 32 (bf16: 16 bytes) or 16 (fp32) of the contraction
 // the share of its quarter of the wave.  Both sides take it in the same order, which is all that counts.
@@ -181,6 +180,21 @@ __device__ __forceinline__ void products(f32x4 (&acc)[FM][FN], const typename Fr
     }
 }
 
+// fp32: a sum of thousands of products in one accumulator loses more than the rest of the pass, so after every 512 of the contraction it is added to
+// a second one and starts again: 4096 of them end up 23 + 3 roundings off (root of the count) in place of 64.  (That case: 5.8e-7 to 6.2e-7 off, relative, where it was 9.3e-7 and a library's products are 1.2e-6.)
+constexpr uint32_t kFold = 512;
+template <uint32_t FM, uint32_t FN> __device__ __forceinline__ void fold(f32x4 (&sum)[FM][FN], f32x4 (&acc)[FM][FN])
+{
+#pragma unroll
+    for (uint32_t i = 0; i < FM; ++i) {
+#pragma unroll
+        for (uint32_t j = 0; j < FN; ++j) {
+            sum[i][j] += acc[i][j];
+            acc[i][j] = f32x4{};
+        }
+    }
+}
+
 // ---- any size, stride and alignment ------------------------------------------------------------------------------------------
 // Tiles of T x T (FWD: half of the columns gate's, half up's), four waves, 32 of the contraction at a time; what is outside is zero in LDS.  The next 32 are asked for, in
 // the widest accesses that the alignment allows, before these are multiplied, and go into the other of two buffers after that.  bf16, K = 8, 2048 rows,
@@ -216,7 +230,7 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
     const int64_t m0 = (int64_t)(tile - tile_n * a.tiles_m) * T, n0 = (int64_t)tile_n * NT;
     if (m0 >= M) return;
     const uint32_t w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1u;
-    f32x4 acc[F][F] = {};
+    f32x4 acc[F][F] = {}, sum[F][F] = {};
     const char *dg = a.dg + (uint64_t)a.first[k] * a.pitch * ES, *du = a.du + (uint64_t)a.first[k] * a.pitch * ES;
     const char *x = a.x.p + k * a.x.rs * (int64_t)ES;
     const int64_t deep = FORM == FWD ? cols : FORM == DX ? wide : rows;
@@ -278,6 +292,17 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
             products<BF16, F, F>(acc, m, n);
         }
         if (s + 1 < steps) put_both(((uint32_t)s + 1u) & 1u);
+        if constexpr (!BF16) {
+            if ((uint32_t)s % (kFold / kDeep) == kFold / kDeep - 1u) fold<F, F>(sum, acc);
+        }
+    }
+    if constexpr (!BF16) {
+        fold<F, F>(sum, acc);
+#pragma unroll
+        for (uint32_t i = 0; i < F; ++i) {
+#pragma unroll
+            for (uint32_t j = 0; j < F; ++j) acc[i][j] = sum[i][j];
+        }
     }
     const uint32_t lane = threadIdx.x & 63u;
 #pragma unroll
@@ -313,11 +338,12 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
 // ---- aligned ------------------------------------------------------------------------------------------------------------------------
 // Bound by the matrix cores and what feeds them.  bf16, K = 8, 2048 rows, 2048 x 5504: forward 802 us (920 TFLOP/s), dx 675 (1095), weights 722 (1023), where a library's plain product
 // of such sizes reaches 870 to 1070; of the forward pass, 526 are the products with LDS as it is, 500 the loads without the products, and 170 its three outputs.
-// fp32, K = 4, 1024 rows, 1024 x 2816: 449, 402 and 429 us (105 to 117 TFLOP/s; a library 140 on 4096 x 4096 x 4096).  A few rows: the weights' bytes, 361 MB in 59 to 70 us.
+// fp32, K = 4, 1024 rows, 1024 x 2816: 464, 412 and 435 us (102 to 115 TFLOP/s; a library 140 on 4096 x 4096 x 4096); the second accumulator takes 2 % of it.  A few rows: the weights' bytes, 361 MB in 59 to 70 us.
 //
 // A workgroup makes TM x TN of C, wave by wave, and takes the contraction a step (LP pieces of 16 bytes) at a time through NS
 // buffers in LDS: while the waves multiply one, the next ones are on their way from memory straight into the others.
 // What is outside is asked for beyond the end of a buffer resource, which gives zeros.
+
 // A tile's place and how far what may be read reaches from there: T lines along, or a step's lines across.
 struct Side {
     const char *p;               // of the tile's first element
@@ -485,7 +511,7 @@ __global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, LP, NS, HINT>::thr
     const uint32_t steps1 = (uint32_t)((deep + STEP - 1) / STEP), all = FORM == DX ? 2u * steps1 : steps1;
     const uint32_t begin = FORM == DX ? split * map.per_split : 0u, end = FORM == DX && begin + map.per_split < all ? begin + map.per_split : all;
     const int64_t to_du = FORM == DX ? a.du - a.dg : 0, to_up = FORM == DX ? a.up[k] - a.gate[k] : 0;
-    f32x4 acc[S::FM][S::FN] = {};
+    f32x4 acc[S::FM][S::FN] = {}, sum[S::FM][S::FN] = {};
     // The sides of the step that is asked for next.  DX goes through the first pair and then through the second; beyond the last step there is nothing to read.
     const int64_t on_m = S::along_m ? LP * 16 : STEP * m.stride, on_n = S::along_n ? LP * 16 : STEP * n.stride;
     const Side m_first = m, n_first = n;
@@ -516,6 +542,17 @@ __global__ __launch_bounds__((Big<BF16, FORM, TM, TN, WM, WN, LP, NS, HINT>::thr
         if (t + 1u >= steps) m.bytes = n.bytes = n2.bytes = 0;
         into = into + 1u == NS ? 0u : into + 1u;
         if (ready) cur = cur + 1u == NS ? 0u : cur + 1u;
+        if constexpr (!BF16) {
+            if (t % (kFold / STEP) == 0u) fold<S::FM, S::FN>(sum, acc);
+        }
+    }
+    if constexpr (!BF16) {
+        fold<S::FM, S::FN>(sum, acc);
+#pragma unroll
+        for (uint32_t i = 0; i < S::FM; ++i) {
+#pragma unroll
+            for (uint32_t j = 0; j < S::FN; ++j) acc[i][j] = sum[i][j];
+        }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // C through LDS, each wave in a part of its own, so that a lane has eight columns next to each other and the activation's code is there once.

@@ -177,7 +177,8 @@ template <class F> void norm_back_shape(uint32_t groups, F f)
     else f(NormShape<1024, 2>{});
 }
 
-// Workgroups a replica of a norm's backward pass, each of which leaves a share of the gain's gradient.
+// Workgroups a replica of a norm's backward pass, each of which leaves a share of the gain's gradient: 1024 in all, four a CU.  (8 x 4096 x 2048 bf16, with the
+// shares' sum: 1024 144 us, 1280 145, 2048 163.)
 struct Shares {
     uint32_t parts;
     int64_t bytes;
@@ -371,9 +372,9 @@ lasgd_status check_gated(lasgd_ctx *c, Gated &d, int32_t gate, int32_t up, const
     CHECK(gate == up || d.v.numel[up] == n, LASGD_ERR_INVALID, "gate has %lld elements, up %lld", (long long)n, (long long)d.v.numel[up]);
     d.wide = n / per;
     d.pitch = (d.wide + 7) / 8 * 8;
-    // workgroups of a launch, at the smallest tiles there are (16 x 64, 32 splits and more only of few tiles)
-    const __int128 wide64 = (d.wide + 31) / 32, cols64 = (cols + 31) / 32, rows16 = ((int64_t)d.r.most / 16 + 1) * d.v.K;
-    CHECK(rows16 * wide64 <= kMaxBlocks / 4 && rows16 * cols64 <= kMaxBlocks / 4 && wide64 * cols64 * d.v.K <= kMaxBlocks, LASGD_ERR_UNSUPPORTED,
+    // a launch's workgroups: no tile is smaller than 16 rows of 32 columns, nor those of the weights' gradients than 32 x 32 (shares of dx are for few tiles)
+    const __int128 tiles_w = (d.wide + 31) / 32, tiles_c = (cols + 31) / 32, tiles_r = ((int64_t)d.r.most / 16 + 1) * d.v.K;
+    CHECK(tiles_r * tiles_w <= kMaxBlocks && tiles_r * tiles_c <= kMaxBlocks && 2 * tiles_w * tiles_c * d.v.K <= kMaxBlocks, LASGD_ERR_UNSUPPORTED,
           "more workgroups than a launch has");
     return LASGD_OK;
 }
@@ -435,19 +436,22 @@ template <int FORM> void launch_loose(const Gated &d, const ProductArgs &a, bool
             else hipLaunchKernelGGL((product_kernel<false, FORM, m, n, T>), grid, dim3(256), 0, st, b);
         });
     };
+    // us forward / dx / weights, tiles of 128 and of 64: bf16, K = 8, 2048 rows, 2047 x 5503 1923 / 1831 / 1349 and 3433 / 3154 / 2137; fp32, K = 4, 1023 rows, 1023 x 2815
+    // 531 / 504 / 485 and 550 / 539 / 542; K = 3, up to 333 rows, 515 x 1030 forward 58 and 43.
     if (tiles_of<FORM>(d, a.cols, 128, FORM == FWD ? 64 : 128) >= 2 * kCus) launch(std::integral_constant<uint32_t, 128>{});
     else launch(std::integral_constant<uint32_t, 64>{});
 }
 
 // Rows of a tile of a gated block's products.  Large tiles read their sides less often, small ones fill the chip and waste less of few rows.  us forward / dx (with the
 // sum of its shares) / weights, tiles of 128 and of 256: bf16, K = 8, 2048 rows, 2048 x 5504 985 / 849 / 900 and 802 / 675 / 722; K = 2, 512 rows, 1024 x 2816 24 / 39 / 22
-// and 37 / 53 / 22; K = 16, up to 192 rows, 512 x 1408 31 / 30 / 22 and 32 / 35 / 24; fp32, K = 4, 1024 rows, 1024 x 2816 449 / 416 / 429 and 536 / 410 / 517.
+// and 37 / 53 / 22; K = 16, up to 192 rows, 512 x 1408 31 / 30 / 22 and 32 / 35 / 24; fp32, K = 4, 1024 rows, 1024 x 2816 449 / 416 / 429 and 536 / 410 / 517: fp32, whose
+// products take sixteen times as long beside the same reads, has none of 256.
 // Of 64, K = 8, 48 rows, 2048 x 5504 66 / 94, of 256 151 / 98; of 16 with 4 rows 59 / 64.
 template <int FORM> uint32_t tile_rows(const Gated &d, int64_t cols)
 {
     if (FORM != DW && d.r.most <= 16u) return 16u;
     if (FORM != DW && d.r.most <= 64u) return 64u;
-    return tiles_of<FORM>(d, cols, 256, FORM == FWD ? 128 : 256) >= 2 * kCus ? 256u : 128u;
+    return d.v.bf16 && tiles_of<FORM>(d, cols, 256, FORM == FWD ? 128 : 256) >= 2 * kCus ? 256u : 128u;
 }
 
 // Workgroups that share a tile of dx, in units of the contraction that every step divides: a contraction of 2 wide, and often few tiles.  us alone / shared, with the
@@ -489,7 +493,7 @@ void launch_big(const Gated &d, const ProductArgs &a, const Split &split, float 
     map.first[d.v.K] = total;
     const dim3 grid(total * split.count), threads(64u * WM * WN);
     if (d.v.bf16) hipLaunchKernelGGL((big_product_kernel<true, FORM, TM, TN, WM, WN, LP, NS, HINT>), grid, threads, 0, st, a, map);
-    else hipLaunchKernelGGL((big_product_kernel<false, FORM, TM, TN, WM, WN, LP, NS, HINT>), grid, threads, 0, st, a, map);
+    else if constexpr (TM < 256u) hipLaunchKernelGGL((big_product_kernel<false, FORM, TM, TN, WM, WN, LP, NS, HINT>), grid, threads, 0, st, a, map);
 }
 
 template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, const Split &split, float *part, hipStream_t st)
