@@ -50,6 +50,12 @@ def _load_walk():
 _walk = _load_walk()
 
 
+def _place(module: torch.nn.Module, name: str):
+    """(the parameters of the submodule that owns this one, its name there)."""
+    owner, _, leaf = name.rpartition(".")
+    return module.get_submodule(owner)._parameters, leaf
+
+
 class LASGD:
     def __init__(self, replicas: Sequence[torch.nn.Module], lr: float, momentum: float = 0.9,
                  nesterov: bool = True, weight_decay: float = 0.0, m: int = 1,
@@ -87,6 +93,7 @@ class LASGD:
         self.grad_norms = torch.zeros(len(self.replicas), device=dev)
         self.device, self.dtype = dev, dtype
         self._names = [n for n, p in self.replicas[0].named_parameters() if p.requires_grad]
+        self._places = [[_place(r, n) for n, p in r.named_parameters() if p.requires_grad] for r in self.replicas]
         self.seed, self._masks = int(seed), 0
         self.mask_counter = torch.zeros(1, dtype=torch.int64, device=dev)        # added to the call numbers of recorded masks
         self.main = torch.cuda.Stream(device=dev)
@@ -186,8 +193,9 @@ class LASGD:
     # ---- layers of all replicas ------------------------------------------------------------------------------------------
     # x: [K, ..., columns] of the replicas' type, row by row; a weight: its name in named_parameters(), or its index among the trainable
     # parameters.  rows: how many of each replica's rows (of [K, rows, columns]) there are, None: all; the outputs' others are zeros, and
-    # nothing flows back through them.  They run on the current stream.  A backward pass takes the weights as they are when it runs, so
-    # step() comes after it, and adds their gradients to the buffers that __init__ attached, past autograd.
+    # nothing flows back through them.  They run on the current stream.  The weights are read where they were bound, and a pass over one that is
+    # no longer there is refused.  A backward pass takes the weights as they are when it runs, so step() comes after it, and adds their gradients to
+    # the buffers that __init__ attached, past autograd.
     #
     # Masks: every dropout takes the next call number (`call`: another one, as for a forward pass that is run again).  A recorded call's number is fixed,
     # and `mask_counter` is added to it, forward and backward: move it on by the number of dropouts before each replay.
@@ -199,6 +207,17 @@ class LASGD:
         if not 0 <= int(name) < len(self._names):
             raise KeyError(f"no parameter {name}")
         return int(name)
+
+    def _check_weights(self, *tensors: int) -> None:
+        # The kernels read the memory that was bound.  A parameter that lives elsewhere by now (p.data = ..., to(), load_state_dict(assign=True)) would
+        # leave them with old weights, or with memory that something else has.
+        for t in tensors:
+            for (owner, leaf), ps, at in zip((places[t] for places in self._places), self.params, self.ctx.bound_params):
+                p = ps[t]
+                if (owner.get(leaf) is not p or p.data_ptr() != at[t] or p.dtype != self.dtype or not p.is_contiguous()
+                        or p.numel() != self.ctx.numels[t]):
+                    raise RuntimeError(f"{self._names[t]} of a replica is not the parameter, or not the memory, that was bound "
+                                       "(replicas whose parameters are replaced need a new LASGD)")
 
     def _grads_to_add_to(self, t: int) -> List[torch.Tensor]:
         grads = [ps[t].grad for ps in self.params]
@@ -233,6 +252,7 @@ class LASGD:
         r = L.Rows(self, x.shape, rows)
         self._same_shape(x, residual)
         self._same_columns(x, t, 1)
+        self._check_weights(t)
         self._trainable(t)
         return L.RmsNorm.apply(self, r, t, x, residual, L._anchor(self), float(eps), self._drop(p, call), residual is not None)
 
@@ -244,6 +264,7 @@ class LASGD:
         r = L.Rows(self, x.shape, rows)
         self._same_shape(x, residual)
         self._same_columns(x, t, 1)
+        self._check_weights(t)
         v = r.view(self, x, "x")
         res = None if residual is None else r.view(self, residual, "residual")
         q, scales = r.new(v, x.shape[-1], torch.uint8), r.new(v, 1, torch.float32)
@@ -260,6 +281,7 @@ class LASGD:
         r = L.Rows(self, x.shape, rows)
         self._same_columns(x, g, 2)
         self._same_columns(x, u, 2)
+        self._check_weights(*{g, u})
         self._trainable(g, u)
         if activation not in L.ACTIVATIONS:
             raise ValueError(f"activation {activation!r} is none of {sorted(L.ACTIVATIONS)}")

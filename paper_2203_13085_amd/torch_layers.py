@@ -125,6 +125,7 @@ class RmsNorm(torch.autograd.Function):
         dropped = ctx.drop["p"] > 0.0
         dres = rows.new(h, cols) if ctx.needs_input_grad[4] or (ctx.needs_input_grad[3] and not dropped) else None
         dx = rows.new(h, cols) if ctx.needs_input_grad[3] and dropped else None
+        opt._check_weights(gain)
         grads = opt._grads_to_add_to(gain)
         with torch.cuda.device(opt.device):
             work = _workspace(opt, opt.ctx.rms_norm_backward_bytes(gain, rows.counts))
@@ -160,6 +161,7 @@ class Gated(torch.autograd.Function):
         cols = ctx.shape[-1]
         v = rows.view(opt, da, "the gradient")
         dx = rows.new(x, cols) if ctx.needs_input_grad[4] else None
+        opt._check_weights(*{gate, up})
         grads = opt._grads_to_add_to(gate) + ([] if gate == up else opt._grads_to_add_to(up))
         with torch.cuda.device(opt.device):
             work = _workspace(opt, opt.ctx.gated_backward_bytes(gate, up, rows.counts, cols))
