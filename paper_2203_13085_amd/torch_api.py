@@ -94,7 +94,7 @@ class LASGD:
         self.device, self.dtype = dev, dtype
         self._names = [n for n, p in self.replicas[0].named_parameters() if p.requires_grad]
         self._places = [[_place(r, n) for n, p in r.named_parameters() if p.requires_grad] for r in self.replicas]
-        self.seed, self._masks = int(seed), 0
+        self.seed, self._masks, self._recorded = int(seed), 0, 0                # dropouts so far, eager and recorded
         self.mask_counter = torch.zeros(1, dtype=torch.int64, device=dev)        # added to the call numbers of recorded masks
         self.main = torch.cuda.Stream(device=dev)
         self.side = torch.cuda.Stream(device=dev) if side_stream else self.main
@@ -197,8 +197,9 @@ class LASGD:
     # no longer there is refused.  A backward pass takes the weights as they are when it runs, so step() comes after it, and adds their gradients to
     # the buffers that __init__ attached, past autograd.
     #
-    # Masks: every dropout takes the next call number (`call`: another one, as for a forward pass that is run again).  A recorded call's number is fixed,
-    # and `mask_counter` is added to it, forward and backward: move it on by the number of dropouts before each replay.
+    # Masks: every dropout takes the next call number (`call`: another one, as for a forward pass that is run again).  Recorded ones count by
+    # themselves, from 2^63 on.  A recorded number is fixed, and `mask_counter` is added to it where the graph runs, forward and backward: call next_masks()
+    # before each replay of a graph with a forward pass, whichever of them it is, and no mask comes twice, in a replay or an eager call.
     def _tensor(self, name) -> int:
         if isinstance(name, str):
             if name not in self._names:
@@ -233,10 +234,20 @@ class LASGD:
     def _drop(self, p: float, call: Optional[int]) -> dict:
         if not p:
             return dict(p=0.0)
-        if call is None:
-            call, self._masks = self._masks, self._masks + 1
         recorded = torch.cuda.is_current_stream_capturing()
+        if recorded:
+            call = (1 << 63) + self._recorded if call is None else call
+            self._recorded += 1
+        elif call is None:
+            call, self._masks = self._masks, self._masks + 1
         return dict(p=float(p), seed=self.seed, call=call, counter=self.mask_counter.data_ptr() if recorded else None)
+
+    def next_masks(self) -> None:
+        """New masks for the next replay of recorded passes: moves `mask_counter` on, on the current stream, by the number of all dropouts that
+        were recorded so far, so that the numbers of two replays never meet, of one graph or of two."""
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("next_masks() belongs between replays: recorded, it would move on by the dropouts recorded before it alone")
+        self.mask_counter.add_(self._recorded)
 
     def dropout(self, x: torch.Tensor, p: float, residual: Optional[torch.Tensor] = None, *, rows: Optional[Sequence[int]] = None,
                 call: Optional[int] = None) -> torch.Tensor:

@@ -1,4 +1,6 @@
 """The layers through the torch class, where a program can go wrong without a word."""
+import gc
+
 import pytest
 import torch
 
@@ -67,4 +69,73 @@ def test_a_weight_that_moved_is_refused(change, replica):
         for q, d in zip(m.parameters(), data):
             q.data = d
     assert torch.equal(opt.gated("gate.weight", "up.weight", x), a.detach()) and len(alive) == 16
+    opt.close()
+
+
+# ---- call numbers of recorded masks ----------------------------------------------------------------------------------------
+def test_masks_of_eager_calls_and_of_two_graphs_never_meet():
+    """Two graphs with two and three dropouts, replayed in turn, a third one recorded in between, and eager calls before, between and after: no mask comes twice."""
+    K, rows, cols = 2, 8, 64
+    replicas, opt = make(K, cols, 8, seed=5)
+    x = torch.ones(K, rows, cols, device=DEV)
+    masks = []
+
+    def keep(*outs):
+        torch.cuda.synchronize()
+        masks.extend((o[k] != 0).cpu() for o in outs for k in range(K))
+    side = torch.cuda.Stream()
+
+    def record(n):
+        graph = torch.cuda.CUDAGraph()
+        gc.collect()                                        # a graph that is freed while another one is recorded ends the process
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            outs = [opt.dropout(x, 0.5) for _ in range(n - 1)]
+            outs.append(opt.rms_norm("norm", x, torch.zeros_like(x), p=0.5)[1])
+        return graph, outs
+    with torch.no_grad():
+        for _ in range(4):
+            keep(opt.dropout(x, 0.5))
+        graphs = [record(2), record(3)]
+        for turn in range(6):
+            if turn == 4:
+                graphs.append(record(4))
+            for graph, outs in graphs:
+                opt.next_masks()
+                graph.replay()
+                keep(*outs)
+            for _ in range(5):
+                keep(opt.dropout(x, 0.5))
+    seen = {m.numpy().tobytes() for m in masks}
+    assert len(seen) == len(masks) == K * (4 + 6 * 5 + 6 * 5 + 2 * 4)
+    opt.close()
+
+
+def test_a_replay_without_moving_on_repeats_its_masks_and_its_backward_pass_has_the_same():
+    K, cols = 2, 64
+    replicas, opt = make(K, cols, 8, seed=6)
+    x = torch.ones(K, 5, cols, device=DEV, requires_grad=True)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    warm = torch.ones(3, device=DEV, requires_grad=True)
+    torch.autograd.grad(warm.sum(), warm)                   # what torch loads at its first gradient
+    gc.collect()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        y = opt.dropout(x, 0.5)
+        dx, = torch.autograd.grad(y, x, torch.ones_like(y))
+    seen = []
+    for turn in range(3):
+        opt.next_masks()
+        for _ in range(2):
+            graph.replay()
+            torch.cuda.synchronize()
+            seen.append(y.detach().clone())
+            assert torch.equal(y.detach(), dx)
+        assert torch.equal(seen[-1], seen[-2])
+    assert not torch.equal(seen[0], seen[2]) and not torch.equal(seen[2], seen[4])
+    with pytest.raises(RuntimeError, match="record"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=side):
+            opt.dropout(x.detach(), 0.5)
+            opt.next_masks()
+    torch.cuda.synchronize()
     opt.close()
