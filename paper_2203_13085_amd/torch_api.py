@@ -69,7 +69,8 @@ class LASGD:
         step() then leaves the norms before clipping in `grad_norms`, a tensor of K floats on the GPU.
         skip_nonfinite (with max_grad_norm): a replica whose gradients hold an infinity or a NaN takes no local update in
         that step, and keeps its momentum; it still takes part in a global update.
-        seed: key of the dropout masks, 64 bits."""
+        seed: key of the dropout masks, 64 bits; another one for a run that goes on from saved weights, or its masks are the first run's.
+        Dropouts under torch.utils.checkpoint need `call` numbers (dropout(), rms_norm())."""
         assert len(replicas) >= 1 and m >= 1
         assert max_grad_norm is None or max_grad_norm >= 0.0
         assert max_grad_norm is not None or not skip_nonfinite, "skip_nonfinite needs a max_grad_norm (infinity: no limit)"
@@ -200,6 +201,9 @@ class LASGD:
     # Masks: every dropout takes the next call number (`call`: another one, as for a forward pass that is run again).  Recorded ones count by
     # themselves, from 2^63 on.  A recorded number is fixed, and `mask_counter` is added to it where the graph runs, forward and backward: call next_masks()
     # before each replay of a graph with a forward pass, whichever of them it is, and no mask comes twice, in a replay or an eager call.
+    # Activation checkpointing runs a forward pass again, in the backward pass, where torch's generators are set back but nobody sets back these numbers:
+    # its dropouts have to be given theirs, and without one they are refused there.  A new LASGD counts from 0 again: a run that goes on from saved weights
+    # takes another `seed`, or it has the first run's masks once more.
     def _tensor(self, name) -> int:
         if isinstance(name, str):
             if name not in self._names:
@@ -234,6 +238,9 @@ class LASGD:
     def _drop(self, p: float, call: Optional[int]) -> dict:
         if not p:
             return dict(p=0.0)
+        if call is None and torch._C._current_graph_task_id() != -1:
+            raise RuntimeError("a dropout in a forward pass that is run again in a backward pass (activation checkpointing) would draw another mask: "
+                               "give it a call number, the same both times (call=)")
         recorded = torch.cuda.is_current_stream_capturing()
         if recorded:
             call = (1 << 63) + self._recorded if call is None else call
@@ -251,14 +258,17 @@ class LASGD:
 
     def dropout(self, x: torch.Tensor, p: float, residual: Optional[torch.Tensor] = None, *, rows: Optional[Sequence[int]] = None,
                 call: Optional[int] = None) -> torch.Tensor:
-        """residual + drop(x); a mask of its own for each replica, which is made again in the backward pass."""
+        """residual + drop(x); a mask of its own for each replica, which is made again in the backward pass.
+        call: the mask's number (under activation checkpointing, which runs this call twice: one of the program's own, the same both times; from 2^62 to
+        2^63 they do not meet the counted ones)."""
         r = L.Rows(self, x.shape, rows)
         self._same_shape(x, residual)
         return L.Dropout.apply(self, r, x, residual, self._drop(p, call))
 
     def rms_norm(self, gain, x: torch.Tensor, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-6, p: float = 0.0,
                  rows: Optional[Sequence[int]] = None, call: Optional[int] = None):
-        """gain * h / rms(h) with h = residual + drop(x).  With a residual: (that, h), h being the next residual."""
+        """gain * h / rms(h) with h = residual + drop(x).  With a residual: (that, h), h being the next residual.
+        call: the mask's number, as for dropout()."""
         t = self._tensor(gain)
         r = L.Rows(self, x.shape, rows)
         self._same_shape(x, residual)

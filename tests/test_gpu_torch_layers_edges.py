@@ -139,3 +139,35 @@ def test_a_replay_without_moving_on_repeats_its_masks_and_its_backward_pass_has_
             opt.next_masks()
     torch.cuda.synchronize()
     opt.close()
+
+
+# ---- forward passes that are run again in the backward pass ---------------------------------------------------------------------
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_a_repeated_forward_pass_needs_its_call_numbers(reentrant):
+    """torch.utils.checkpoint runs a forward pass again: without numbers of its own a dropout would draw another mask there."""
+    from torch.utils.checkpoint import checkpoint
+    K, D, H, p = 2, 48, 32, 0.5
+    replicas, opt = make(K, D, H, seed=8)
+    x, res = torch.randn(K, 6, D, device=DEV, requires_grad=True), torch.randn(K, 6, D, device=DEV)
+
+    def block(x, *calls):
+        y, h = opt.rms_norm("norm", x, res, p=p, call=calls[0] if calls else None)
+        return opt.dropout(opt.gated("gate.weight", "up.weight", y), p, call=calls[1] if calls else None).square().sum() + h.sum()
+
+    def grads():
+        return [x.grad.clone(), *(q.grad.clone() for m in replicas for q in m.parameters())]
+    opt.zero_grad()
+    block(x, 1, 2).backward()
+    want = grads()
+    x.grad = None
+    opt.zero_grad()
+    checkpoint(lambda x: block(x, 1, 2), x, use_reentrant=reentrant).backward()
+    for a, b in zip(grads(), want):
+        assert torch.equal(a, b)
+    loss = checkpoint(block, x, use_reentrant=reentrant)
+    with pytest.raises(RuntimeError, match="call"):
+        loss.backward()
+    loss = checkpoint(lambda x: opt.dropout(x, 0.0).sum(), x, use_reentrant=reentrant)         # no mask, no number
+    loss.backward()
+    torch.cuda.synchronize()
+    opt.close()
