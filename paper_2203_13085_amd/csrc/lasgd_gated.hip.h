@@ -36,7 +36,8 @@ template <bool BF16> __device__ __forceinline__ ActPair activation(int act, floa
     case ACT_GELU_TANH: {
         constexpr float b = 0.79788456080286536f, c = 0.044715f;
         const float s = sigmoid<BF16>(2.f * b * __builtin_fmaf(c * v * v, v, v));             // (1 + tanh z) / 2
-        return {v * s, __builtin_fmaf(2.f * b * v * __builtin_fmaf(3.f * c * v, v, 1.f), s * (1.f - s), s)};
+        const float t = s * (1.f - s);                                           // 0 long before v^3 is beyond fp32, from 1.3e13 on
+        return {v * s, t == 0.f ? s : __builtin_fmaf(2.f * b * v * __builtin_fmaf(3.f * c * v, v, 1.f), t, s)};
     }
     default: return {v > 0.f ? v : v == v ? 0.f : v, v > 0.f ? 1.f : 0.f};
     }

@@ -1,0 +1,46 @@
+"""Dropout, root-mean-square norms and gated blocks at the ends of what their arguments may be.
+
+U is half a step of fp32 relative to the value, HALF half a step of the storage type."""
+import pytest
+import torch
+
+from tests.layers_util import ACTS, DEV, HALF, U, Act, Model, act64, dtype_of, generator, within, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- activations at every size of their argument ---------------------------------------------------------------------------
+SIZES = [0.0, 1e-30, 1e-3, 0.3, 1.0, 2.5, 5.0, 12.0, 30.0, 200.0, 1e4, 1e9, 1e12, 1.2e13, 1e15, 1e18, 2e19, 1e25, 1e38, 3e38]
+
+
+def _slopes(act, storage, values):
+    """(f, slope) of the values, from a backward pass whose gate's weight is 1 and whose up's is 0: dx = dg, and dWu = du^T x with x = 1."""
+    n = len(values)
+    m = Model(1, [(8, 8), (8, 8)], storage, generator(0))
+    m.w[0][1].copy_(torch.eye(8, device=DEV).to(m.dt))
+    m.w[1][1].zero_()
+    rows = [n]
+    x, g, u, da, dx = (Act(rows, 8, m.dt) for _ in range(5))
+    for t in (x, u, da):
+        t[0].fill_(1.0)
+    g[0].copy_(torch.tensor(values, device=DEV, dtype=torch.float32).to(m.dt)[:, None].expand(n, 8))
+    work = workspace(m.ctx.gated_backward_bytes(0, 1, rows, 8))
+    m.ctx.gated_backward(0, 1, rows, 8, x.at, g.at, u.at, da.at, dx.at, activation=ACTS[act], accumulate=False, workspace=work.data_ptr(),
+                         workspace_bytes=work.numel())
+    torch.cuda.synchronize()
+    out = g[0][:, 0].double(), dx[0].double()
+    m.close()
+    return out
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("act", list(ACTS))
+def test_slopes_of_large_arguments(act, storage):
+    """From 200 on the slope is 1 or 0 to the bit: what is left of it, e^-200 of the argument, is below fp32's least value. Below, 16 roundings of the slope's
+    terms, each at most 1 + |g|, and one to the storage type."""
+    g, slope = _slopes(act, storage, SIZES + [-v for v in SIZES])
+    want = act64(act, g)[1]
+    want = torch.where(g.abs() > 150.0, (g > 0).double(), want)
+    bound = torch.where(g.abs() > 150.0, 0.0, 16 * U * (1 + g.abs()) + HALF[dtype_of(storage)] * want.abs())
+    for j in range(8):
+        within(slope[:, j], want, bound, (act, j))
