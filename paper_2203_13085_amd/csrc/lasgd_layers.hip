@@ -498,9 +498,13 @@ void launch_big(const Gated &d, const ProductArgs &a, const Split &split, float 
 
 template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, const Split &split, float *part, hipStream_t st)
 {
+    const bool few = FORM == DW && d.v.bf16 && d.r.most <= kFewRows;
+    // The tiles find the end of DW's rows of x by their address alone.  Rows that overlap do not end there: what is behind them counts 0 times, but an infinity
+    // among it would still make a NaN of every sum.
+    if (FORM == DW && !few && a.x.ss < (int64_t)a.cols) big = false;
     if (!big) return launch_loose<FORM>(d, a, vm, vn, st);
     if constexpr (FORM == DW) {
-        if (d.v.bf16 && d.r.most <= kFewRows) {
+        if (few) {
             const dim3 grid(ceil_div(a.wide, 256) * ceil_div(a.cols, 256), d.v.K, 2);
             two_flags(a.accumulate, 4 * (uint64_t)d.v.K * a.wide * a.cols >= kBeyondCache, [&](auto add, auto stream) {
                 hipLaunchKernelGGL((few_rows_weights_kernel<add, stream ? STREAM : WIDE>), grid, dim3(256), 0, st, a);
@@ -627,6 +631,7 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
         }
     }
     p.accumulate = accumulate;
+    if (d.r.most <= 1) p.x.ss = cols;                        // no second row: any stride, and with this one the rows end where x does
     weights(p, d, d.v.grads, gate, up, cols);
     launch_form<DW>(d, p, big, true, vx, Split{1, 0}, nullptr, st);
     return launched(c);

@@ -1,6 +1,8 @@
 """Dropout, root-mean-square norms and gated blocks at the ends of what their arguments may be.
 
 U is half a step of fp32 relative to the value, HALF half a step of the storage type."""
+import math
+
 import pytest
 import torch
 
@@ -44,3 +46,40 @@ def test_slopes_of_large_arguments(act, storage):
     bound = torch.where(g.abs() > 150.0, 0.0, 16 * U * (1 + g.abs()) + HALF[dtype_of(storage)] * want.abs())
     for j in range(8):
         within(slope[:, j], want, bound, (act, j))
+
+
+# ---- rows that overlap ----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,stride", [([40, 37], 8), ([70, 1], 0), ([50, 33], 56), ([1, 1], 64), ([1, 0], 0), ([300, 290], 8), ([20, 3], 8)])
+def test_weight_gradients_of_overlapping_rows_with_an_infinity(rows, stride, storage):
+    """Windows of a sequence, one row for all, single rows: an infinity counts in the columns where a row has it, and nowhere else."""
+    dt, gen, K, cols, wide, most = dtype_of(storage), generator(41), len(rows), 64, 48, max(rows)
+    m = Model(K, [(wide, cols), (wide, cols)], storage, gen)
+    own = (most - 1) * stride + cols
+    x = torch.randn(K, own, generator=gen, device=DEV).to(dt)
+    view = x.as_strided((K, most, cols), (own, stride, 1))
+    for k, n in enumerate(rows):
+        if n:
+            view[k, n - 1, -1] = float("inf")               # the last element that this replica reads
+    g, u, da = (Act(rows, wide, dt, "dense", gen) for _ in range(3))
+    work = workspace(m.ctx.gated_backward_bytes(0, 1, rows, cols))
+    m.ctx.gated_backward(0, 1, rows, cols, (x.data_ptr(), own, stride), g.at, u.at, da.at, None, accumulate=False, workspace=work.data_ptr(),
+                         workspace_bytes=work.numel())
+    torch.cuda.synchronize()
+    for k, n in enumerate(rows):
+        f, slope = act64("silu", g.d(k))
+        xk = view[k, :n].double()
+        there = xk.isfinite().all(0)                        # columns without one
+        for which, d, o in ((0, da.d(k) * u.d(k) * slope, (16 * U * (1 + g.d(k).abs()) + HALF[dt] * slope.abs()) * (da.d(k) * u.d(k)).abs()),
+                            (1, da.d(k) * f, (16 * U * (f.abs() + g.d(k).abs()) + HALF[dt] * f.abs()) * da.d(k).abs())):
+            o = o + 4 * U * d.abs()
+            got, xs = m.grad(which, k)[:, there], xk[:, there]
+            want = d.T @ xs
+            bound = o.T @ xs.abs() + 2 * (n + 2) * U * ((d.abs() + o).T @ xs.abs())
+            within(got, want, bound + HALF[dt] * (want.abs() + bound), ("gate", "up")[which])
+            if n == 1:
+                one = m.grad(which, k)[:, -1].double()
+                assert torch.equal(one, torch.where(d[0] > 0, math.inf, -math.inf).double())
+            elif n:
+                assert bool((~m.grad(which, k)[:, ~there].isfinite()).all())
+    m.close()
