@@ -406,7 +406,8 @@ lasgd_status lasgd_dropout(lasgd_ctx *ctx, const int64_t *rows, int64_t cols, co
  * h = residual + drop(x),  y = gain * h / sqrt(mean(h^2) + eps) over a row.  gain: index of a bound tensor, whose length is the number of columns.
  * residual may be NULL (none), sum too (h is not written; h enters the norm before it is rounded), and drop (no dropout).  scales NULL: y of the
  * storage type.  Otherwise y is e4m3 (OCP, one byte an element) and scales, fp32, gets scale = max |y| / 448 of each row (at least 2^-126) at
- * data[k * replica_stride + r * row_stride]; y / scale, both as they are before a rounding, is rounded to nearest even.  sum may be x or residual, and y, in the storage type, x or residual.
+ * data[k * replica_stride + r * row_stride]; y / scale, both as they are in fp64, is
+ * rounded to fp32 and then to e4m3, each to nearest even.  sum may be x or residual, and y, in the storage type, x or residual.
  * Errors: as above, and UNSUPPORTED beyond LASGD_NORM_MAX_COLS columns.
  */
 #define LASGD_NORM_MAX_COLS 16384

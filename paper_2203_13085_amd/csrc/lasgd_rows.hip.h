@@ -219,9 +219,10 @@ __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a)
 // G threads hold a row, NV groups of eight columns each, so everything is read once; h is rounded where it is stored, and enters the norm
 // as it was before.
 //
-// In 8 bits (OUT8): scale = max |y| / 448, at least the smallest normal number, and y / scale to e4m3, of whose values so few are that 1 in 10^6 quotients
-// lies within fp32's roundings of a border between two and would end up a sixteenth off.  So this form computes in 64 bits from the
-// loaded values on, which the memory hides.
+// In 8 bits (OUT8): scale = max |y| / 448, at least the smallest normal number, and y / scale to e4m3, of whose values so few are that with a norm in fp32, whose
+// roundings add up to some of its last places, 1 in 10^6 quotients would cross a border between two and end up an eighth off. So this form computes in 64 bits from
+// the loaded values on, which the memory hides. The instruction that makes e4m3 takes fp32: a quotient within half a step of fp32 (2^-24) of a border comes to lie on it and
+// goes to its even side, as in any conversion of an fp32 array (of uniform quotients 3 in 10^7 change sides so).
 constexpr double kE4m3Max = 448.0;
 constexpr double kLeastScale = 1.1754943508222875e-38;
 

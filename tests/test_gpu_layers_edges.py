@@ -83,3 +83,45 @@ def test_weight_gradients_of_overlapping_rows_with_an_infinity(rows, stride, sto
             elif n:
                 assert bool((~m.grad(which, k)[:, ~there].isfinite()).all())
     m.close()
+
+
+# ---- quotients next to a border of e4m3 -----------------------------------------------------------------------------------------
+def test_quotients_next_to_a_border_are_rounded_by_way_of_fp32():
+    """Every border between two values of e4m3, with products gain * h that are closer to it than half a step of fp32, on either side: 48 bits make the
+    quotient, whose scale is a power of two (the largest element is 448 times it), so it is known to the bit. To fp32 it becomes the border, and
+    then goes to its even side."""
+    q8 = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).double()             # 0 to 448
+    lower, upper = q8[:-1], q8[1:]
+    border = (lower + upper) / 2
+    e, f = 2.0 ** -13, 2.0 ** -12
+    # (1 + e)(1 - e) = 1 - 2^-26,   (1 + f)(1 - f + f^2) = 1 + 2^-36;  border has five bits, so both factors are fp32 values
+    h = torch.cat([border * (1 + e), border * (1 + f)])
+    w = torch.cat([torch.full_like(border, 1 - e), torch.full_like(border, 1 - f + f * f)])
+    even = torch.where((torch.arange(126) & 1) == 0, lower, upper)
+    want = torch.cat([even, even])
+    assert torch.equal((h * w).float().double(), torch.cat([border, border])) and bool((h * w != torch.cat([border, border])).all())
+    assert torch.equal(h.float().double(), h) and torch.equal(w.float().double(), w)
+    h, w, want = (torch.cat([t, t.new_tensor([s])]) for t, s in ((h, 448.0), (w, 1.0), (want, 448.0)))
+    cols = h.numel()
+    assert cols == 253                                       # eight bytes at a time, and one by one behind them
+    for K, pad in ((1, 0), (2, 3)):
+        width = cols + pad
+        gain, rows = torch.ones(width, dtype=torch.float64), [4] * K
+        gain[:cols] = w
+        m = Model(K, [(width,)], "f32", generator(0))
+        x = torch.zeros(K, 4, width, dtype=torch.float64)
+        x[:, :, :cols] = h
+        for r in range(4):
+            x[:, r] *= (-1.0) ** r * 2.0 ** (3 * r - 4)
+        x = x.float().to(DEV)
+        for k in range(K):
+            m.weight(0, k).copy_(gain.float().to(DEV))
+        q, s = torch.zeros(K, 4, width, dtype=torch.uint8, device=DEV), torch.zeros(K, 4, device=DEV)
+        m.ctx.rms_norm(0, rows, (x.data_ptr(), 4 * width, width), (q.data_ptr(), 4 * width, width), scales=(s.data_ptr(), 4, 1), eps=0.0)
+        torch.cuda.synchronize()
+        got = q.view(torch.float8_e4m3fn).double().cpu()
+        for k in range(K):
+            for r in range(4):
+                assert torch.equal(got[k, r, :cols] * (-1.0) ** r, want), (K, k, r, int((got[k, r, :cols] * (-1.0) ** r != want).sum()))
+                assert bool((got[k, r, cols:] == 0).all())
+        m.close()
