@@ -435,6 +435,8 @@ typedef enum {
  * g = x Wg^T,  u = x Wu^T,  a = f(g) u.  gate, up: indices of bound tensors, [wide][cols] row by row, wide = their length / cols; one index for both: a
  * tensor [2][wide][cols] that holds the two.  x has `cols` columns; a, g and u have `wide`.  g and u, which the backward pass reads, are both given or both NULL.
  * a is made from g and u before these are rounded.
+ * Errors: as above, and UNSUPPORTED, here and in the backward pass, where a product has 2^32 threads or more (2^23 tiles of 256 rows and columns, 2^24 of smaller ones; with
+ * addresses, strides or columns that are not aligned, K times the tiles of the replica with the most rows).
  */
 lasgd_status lasgd_gated(lasgd_ctx *ctx, int32_t gate, int32_t up, const int64_t *rows, int64_t cols, const lasgd_rows *x, const lasgd_rows *g,
                          const lasgd_rows *u, const lasgd_rows *a, lasgd_activation activation, void *stream);

@@ -11,7 +11,8 @@ namespace {
 
 constexpr int64_t kMaxRows = 0x7fffffff;             // of all replicas together
 constexpr int64_t kMaxGroups = 1ll << 48;            // of eight columns, a replica's, where a mask's counter names them
-constexpr int64_t kMaxBlocks = 0x7fffffff;           // of a launch, along x
+constexpr int64_t kMaxTiles = 0x7fffffff;            // of a gated block's products, what their kernels count
+constexpr uint64_t kMaxThreads = 0xffffffff;         // of a launch, along x
 
 // What a call's rows come to.
 struct Rows {
@@ -136,6 +137,13 @@ template <class F> void two_flags(bool a, bool b, F f)
     }
 }
 
+// launch(first row, workgroups) for all rows of a call whose workgroups take `each` of them, in as few launches as hold them.
+template <class F> void in_launches(const Rows &r, uint32_t each, uint32_t threads, F launch)
+{
+    const uint64_t all = ceil_div(r.most, each), most = kMaxThreads / threads;
+    for (uint64_t at = 0; at < all; at += most) launch(at * each, (uint32_t)(all - at < most ? all - at : most));
+}
+
 constexpr int64_t kBeyondCache = 256ll << 20;        // the memory-side cache
 
 // f(storage is bf16, Access) for a call whose accesses are aligned or not, and that moves so many bytes.  The hint beyond the memory-side
@@ -237,9 +245,11 @@ extern "C" lasgd_status lasgd_dropout(lasgd_ctx *c, const int64_t *rows, int64_t
     a.groups = ceil_div(cols, 8);
     while (a.tx_shift < 8u && (1u << a.tx_shift) < a.groups) ++a.tx_shift;
     copy_rows(a, r, v.K);
-    const dim3 grid(ceil_div(r.most, (256u >> a.tx_shift) * kDropRows), v.K);
     row_access(v.bf16, vec, (int64_t)r.total * cols * es * (residual ? 3 : 2), [&](auto bf16, auto wide) {
-        hipLaunchKernelGGL((dropout_kernel<bf16, wide>), grid, dim3(256), 0, (hipStream_t)stream, a);
+        in_launches(r, (256u >> a.tx_shift) * kDropRows, 256, [&](uint64_t row0, uint32_t blocks) {
+            a.row0 = row0;
+            hipLaunchKernelGGL((dropout_kernel<bf16, wide>), dim3(blocks, v.K), dim3(256), 0, (hipStream_t)stream, a);
+        });
     });
     return launched(c);
 }
@@ -274,11 +284,13 @@ extern "C" lasgd_status lasgd_rms_norm(lasgd_ctx *c, int32_t gain, const int64_t
     for (int32_t k = 0; k < v.K; ++k) a.gain[k] = (const char *)v.params[(size_t)k * v.n_tensors + gain];
     norm_shape(a.groups, [&](auto shape) {
         constexpr int G = decltype(shape)::G, NV = decltype(shape)::NV, T = norm_threads(G);
-        const dim3 grid(ceil_div(r.most, T / G), v.K);
         const int64_t bytes = (int64_t)r.total * cols * (es * (1 + !!residual + !!sum) + (scales ? 1 : es));
         row_access(v.bf16, vec, bytes, [&](auto bf16, auto wide) {
-            if (scales) hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV, true>), grid, dim3(T), 0, (hipStream_t)stream, a);
-            else hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV, false>), grid, dim3(T), 0, (hipStream_t)stream, a);
+            in_launches(r, T / G, T, [&](uint64_t row0, uint32_t blocks) {
+                a.row0 = row0;
+                if (scales) hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV, true>), dim3(blocks, v.K), dim3(T), 0, (hipStream_t)stream, a);
+                else hipLaunchKernelGGL((rms_norm_kernel<bf16, wide, G, NV, false>), dim3(blocks, v.K), dim3(T), 0, (hipStream_t)stream, a);
+            });
         });
     });
     return launched(c);
@@ -357,6 +369,7 @@ struct Gated {
     Rows r;
     int64_t wide, pitch;
     int es;
+    bool few_tiles;                                  // no launch comes near kMaxThreads
 };
 
 lasgd_status check_gated(lasgd_ctx *c, Gated &d, int32_t gate, int32_t up, const int64_t *rows, int64_t cols)
@@ -374,8 +387,9 @@ lasgd_status check_gated(lasgd_ctx *c, Gated &d, int32_t gate, int32_t up, const
     d.pitch = (d.wide + 7) / 8 * 8;
     // a launch's workgroups: no tile is smaller than 16 rows of 32 columns, nor those of the weights' gradients than 32 x 32 (shares of dx are for few tiles)
     const __int128 tiles_w = (d.wide + 31) / 32, tiles_c = (cols + 31) / 32, tiles_r = ((int64_t)d.r.most / 16 + 1) * d.v.K;
-    CHECK(tiles_r * tiles_w <= kMaxBlocks && tiles_r * tiles_c <= kMaxBlocks && 2 * tiles_w * tiles_c * d.v.K <= kMaxBlocks, LASGD_ERR_UNSUPPORTED,
-          "more workgroups than a launch has");
+    const auto each_below = [&](int64_t most) { return tiles_r * tiles_w <= most && tiles_r * tiles_c <= most && 2 * tiles_w * tiles_c * d.v.K <= most; };
+    CHECK(each_below(kMaxTiles), LASGD_ERR_UNSUPPORTED, "more tiles than a launch counts");
+    d.few_tiles = each_below(1 << 16);               // of 512 threads, and 64 shares of a contraction: 2^31
     return LASGD_OK;
 }
 
@@ -422,7 +436,11 @@ template <int FORM> uint64_t tiles_of(const Gated &d, int64_t cols, uint32_t tm,
 
 constexpr uint32_t kCus = 256;
 
-template <int FORM> void launch_loose(const Gated &d, const ProductArgs &a, bool vm, bool vn, hipStream_t st)
+// The launches below: `go` false only says whether the product's launch has no more threads than it may.
+constexpr const char *kTooManyThreads = "a product of 2^32 threads or more";
+constexpr bool fits(uint64_t blocks, uint32_t threads) { return blocks <= kMaxThreads / threads; }
+
+template <int FORM> bool launch_loose(const Gated &d, const ProductArgs &a, bool vm, bool vn, hipStream_t st, bool go)
 {
     auto launch = [&](auto tile) {
         constexpr uint32_t T = decltype(tile)::value;
@@ -430,16 +448,18 @@ template <int FORM> void launch_loose(const Gated &d, const ProductArgs &a, bool
         ProductArgs b = a;
         b.tiles_m = ceil_div(M, T);
         b.tiles = b.tiles_m * ceil_div(N, FORM == FWD ? T / 2 : T);
+        if (!go || !fits((uint64_t)b.tiles * d.v.K, 256)) return fits((uint64_t)b.tiles * d.v.K, 256);
         const dim3 grid(b.tiles * d.v.K, 1, FORM == DW ? 2 : 1);
         two_flags(vm, vn, [&](auto m, auto n) {
             if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n, T>), grid, dim3(256), 0, st, b);
             else hipLaunchKernelGGL((product_kernel<false, FORM, m, n, T>), grid, dim3(256), 0, st, b);
         });
+        return true;
     };
     // us forward / dx / weights, tiles of 128 and of 64: bf16, K = 8, 2048 rows, 2047 x 5503 1923 / 1831 / 1349 and 3433 / 3154 / 2137; fp32, K = 4, 1023 rows, 1023 x 2815
     // 531 / 504 / 485 and 550 / 539 / 542; K = 3, up to 333 rows, 515 x 1030 forward 58 and 43.
-    if (tiles_of<FORM>(d, a.cols, 128, FORM == FWD ? 64 : 128) >= 2 * kCus) launch(std::integral_constant<uint32_t, 128>{});
-    else launch(std::integral_constant<uint32_t, 64>{});
+    if (tiles_of<FORM>(d, a.cols, 128, FORM == FWD ? 64 : 128) >= 2 * kCus) return launch(std::integral_constant<uint32_t, 128>{});
+    return launch(std::integral_constant<uint32_t, 64>{});
 }
 
 // Rows of a tile of a gated block's products.  Large tiles read their sides less often, small ones fill the chip and waste less of few rows.  us forward / dx (with the
@@ -474,7 +494,7 @@ Split dx_split(const Gated &d, int64_t cols)
 }
 
 template <int FORM, uint32_t TM, uint32_t TN, uint32_t WM, uint32_t WN, uint32_t LP, uint32_t NS, bool HINT = false>
-void launch_big(const Gated &d, const ProductArgs &a, const Split &split, float *part, hipStream_t st)
+bool launch_big(const Gated &d, const ProductArgs &a, const Split &split, float *part, hipStream_t st, bool go)
 {
     static_assert(kUnit % (LP * 8u) == 0, "whole steps");
     constexpr uint32_t NT = FORM == FWD ? TN / 2u : TN;
@@ -491,25 +511,29 @@ void launch_big(const Gated &d, const ProductArgs &a, const Split &split, float 
         total += tm * ceil_div(FORM == FWD ? a.wide : a.cols, NT) * (FORM == DW ? 2u : 1u);
     }
     map.first[d.v.K] = total;
+    if (!go || !fits((uint64_t)total * split.count, 64u * WM * WN)) return fits((uint64_t)total * split.count, 64u * WM * WN);
     const dim3 grid(total * split.count), threads(64u * WM * WN);
     if (d.v.bf16) hipLaunchKernelGGL((big_product_kernel<true, FORM, TM, TN, WM, WN, LP, NS, HINT>), grid, threads, 0, st, a, map);
     else if constexpr (TM < 256u) hipLaunchKernelGGL((big_product_kernel<false, FORM, TM, TN, WM, WN, LP, NS, HINT>), grid, threads, 0, st, a, map);
+    return true;
 }
 
-template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, const Split &split, float *part, hipStream_t st)
+template <int FORM> bool launch_form(const Gated &d, const ProductArgs &a, bool big, bool vm, bool vn, const Split &split, float *part, hipStream_t st, bool go)
 {
     const bool few = FORM == DW && d.v.bf16 && d.r.most <= kFewRows;
     // The tiles find the end of DW's rows of x by their address alone.  Rows that overlap do not end there: what is behind them counts 0 times, but an infinity
     // among it would still make a NaN of every sum.
     if (FORM == DW && !few && a.x.ss < (int64_t)a.cols) big = false;
-    if (!big) return launch_loose<FORM>(d, a, vm, vn, st);
+    if (!big) return launch_loose<FORM>(d, a, vm, vn, st, go);
     if constexpr (FORM == DW) {
         if (few) {
-            const dim3 grid(ceil_div(a.wide, 256) * ceil_div(a.cols, 256), d.v.K, 2);
+            const uint64_t blocks = (uint64_t)ceil_div(a.wide, 256) * ceil_div(a.cols, 256);
+            if (!go || !fits(blocks, 256)) return fits(blocks, 256);
+            const dim3 grid((uint32_t)blocks, d.v.K, 2);
             two_flags(a.accumulate, 4 * (uint64_t)d.v.K * a.wide * a.cols >= kBeyondCache, [&](auto add, auto stream) {
                 hipLaunchKernelGGL((few_rows_weights_kernel<add, stream ? STREAM : WIDE>), grid, dim3(256), 0, st, a);
             });
-            return;
+            return true;
         }
     }
     const uint32_t tm = tile_rows<FORM>(d, a.cols);
@@ -518,11 +542,11 @@ template <int FORM> void launch_form(const Gated &d, const ProductArgs &a, bool 
         // backward 67 / 58; 48 rows 128 / 66 and 115 / 84.
         const bool hint = 2 * (uint64_t)d.es * d.v.K * a.wide * a.cols >= kBeyondCache;
         constexpr uint32_t TN = FORM == FWD ? 128 : 256;
-        if (tm == 16u) return hint ? launch_big<FORM, 16, TN, 1, 4, 8, 2, true>(d, a, split, part, st) : launch_big<FORM, 16, TN, 1, 4, 8, 2>(d, a, split, part, st);
-        if (tm == 64u) return hint ? launch_big<FORM, 64, TN, 1, 4, 8, 2, true>(d, a, split, part, st) : launch_big<FORM, 64, TN, 1, 4, 8, 2>(d, a, split, part, st);
+        if (tm == 16u) return hint ? launch_big<FORM, 16, TN, 1, 4, 8, 2, true>(d, a, split, part, st, go) : launch_big<FORM, 16, TN, 1, 4, 8, 2>(d, a, split, part, st, go);
+        if (tm == 64u) return hint ? launch_big<FORM, 64, TN, 1, 4, 8, 2, true>(d, a, split, part, st, go) : launch_big<FORM, 64, TN, 1, 4, 8, 2>(d, a, split, part, st, go);
     }
-    if (tm == 128u) launch_big<FORM, 128, 128, 2, 2, 8, 2>(d, a, split, part, st);
-    else launch_big<FORM, 256, 256, 2, 4, 8, 2>(d, a, split, part, st);
+    if (tm == 128u) return launch_big<FORM, 128, 128, 2, 2, 8, 2>(d, a, split, part, st, go);
+    return launch_big<FORM, 256, 256, 2, 4, 8, 2>(d, a, split, part, st, go);
 }
 
 int64_t gates_bytes(const Gated &d) { return (int64_t)round_up16((uint64_t)d.r.total * d.pitch * d.es); }          // dg, and du again
@@ -555,7 +579,9 @@ extern "C" lasgd_status lasgd_gated(lasgd_ctx *c, int32_t gate, int32_t up, cons
     if (!d.r.most) return LASGD_OK;
     weights(p, d, d.v.params, gate, up, cols);
     p.wide_out = vo;
-    launch_form<FWD>(d, p, streams(d, cols, p.x, vx), vx, cols % 8 == 0, Split{1, 0}, nullptr, (hipStream_t)stream);
+    const auto product = [&](bool go) { return launch_form<FWD>(d, p, streams(d, cols, p.x, vx), vx, cols % 8 == 0, Split{1, 0}, nullptr, (hipStream_t)stream, go); };
+    CHECK(d.few_tiles || product(false), LASGD_ERR_UNSUPPORTED, "%s", kTooManyThreads);
+    product(true);
     return launched(c);
 }
 
@@ -596,6 +622,19 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
     e.du = e.dg + gates_bytes(d);
     p.dg = e.dg;
     p.du = e.du;
+    const bool big = streams(d, cols, p.x, vx);
+    ProductArgs q = p;
+    q.a = out;
+    weights(q, d, d.v.params, gate, up, cols);
+    q.wide_out = vo;
+    const Split split = big ? dx_split(d, cols) : Split{1, 0};
+    float *part = (float *)(e.du + gates_bytes(d));
+    p.accumulate = accumulate;
+    if (d.r.most <= 1) p.x.ss = cols;                        // no second row: any stride, and with this one the rows end where x does
+    weights(p, d, d.v.grads, gate, up, cols);
+    const auto rows_product = [&](bool go) { return launch_form<DX>(d, q, big, true, cols % 8 == 0, split, part, st, go); };
+    const auto weights_product = [&](bool go) { return launch_form<DW>(d, p, big, true, vx, Split{1, 0}, nullptr, st, go); };
+    CHECK(d.few_tiles || ((!dx || rows_product(false)) && weights_product(false)), LASGD_ERR_UNSUPPORTED, "%s", kTooManyThreads);
     if (d.r.most) {
         e.wide = (uint32_t)d.wide;
         e.groups = ceil_div(d.wide, 8);
@@ -609,19 +648,11 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
         });
         TRY(launched(c));
     }
-    const bool big = streams(d, cols, p.x, vx);
     if (dx && d.r.most) {
-        ProductArgs q = p;
-        q.a = out;
-        weights(q, d, d.v.params, gate, up, cols);
-        q.wide_out = vo;
-        const Split split = big ? dx_split(d, cols) : Split{1, 0};
-        const uint32_t splits = split.count;
-        float *part = (float *)(e.du + gates_bytes(d));
-        launch_form<DX>(d, q, big, true, cols % 8 == 0, split, part, st);
+        rows_product(true);
         TRY(launched(c));
-        if (splits > 1) {
-            JoinRowsArgs j{out, part, (uint64_t)d.r.total * cols, splits, (uint32_t)cols, vo, {}, {}};
+        if (split.count > 1) {
+            JoinRowsArgs j{out, part, (uint64_t)d.r.total * cols, split.count, (uint32_t)cols, vo, {}, {}};
             copy_rows(j, d.r, d.v.K);
             memcpy(j.first, d.r.first, d.v.K * sizeof(uint32_t));
             const dim3 grid(d.r.most < 4096u ? d.r.most : 4096u, d.v.K);
@@ -630,9 +661,6 @@ extern "C" lasgd_status lasgd_gated_backward(lasgd_ctx *c, int32_t gate, int32_t
             TRY(launched(c));
         }
     }
-    p.accumulate = accumulate;
-    if (d.r.most <= 1) p.x.ss = cols;                        // no second row: any stride, and with this one the rows end where x does
-    weights(p, d, d.v.grads, gate, up, cols);
-    launch_form<DW>(d, p, big, true, vx, Split{1, 0}, nullptr, st);
+    weights_product(true);
     return launched(c);
 }

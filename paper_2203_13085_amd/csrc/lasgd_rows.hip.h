@@ -171,6 +171,7 @@ struct DropoutArgs {
     DropArgs drop;
     uint32_t cols, groups;       // groups of eight columns
     uint32_t tx_shift;           // log2 of tx
+    uint64_t row0;               // of a replica, that the launch starts with
     uint32_t rows[64];
 };
 
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a)
 {
     const uint32_t k = blockIdx.y, rows = a.rows[k];
     const uint32_t ty = 256u >> a.tx_shift;
-    const uint64_t r0 = (uint64_t)blockIdx.x * (ty * kDropRows);
+    const uint64_t r0 = a.row0 + (uint64_t)blockIdx.x * (ty * kDropRows);
     if (r0 >= rows) return;
     const uint32_t tx = threadIdx.x & ((1u << a.tx_shift) - 1u);
     const uint64_t r1 = r0 + (threadIdx.x >> a.tx_shift);
@@ -231,6 +232,7 @@ struct NormRowsArgs {
     DropArgs drop;
     uint32_t cols, groups;
     float eps, inv_cols;
+    uint64_t row0;               // of a replica, that the launch starts with
     uint32_t rows[64];
     const char *gain[64];
 };
@@ -293,8 +295,8 @@ __global__ __launch_bounds__(norm_threads(G)) void rms_norm_kernel(const NormRow
     __shared__ T lds[G > 64 ? G / 64 : 1];
     constexpr uint32_t R = norm_threads(G) / G;              // rows a workgroup
     const uint32_t k = blockIdx.y, rows = a.rows[k];
-    const uint64_t r = (uint64_t)blockIdx.x * R + threadIdx.x / G;
-    if ((uint64_t)blockIdx.x * R >= rows) return;
+    const uint64_t r0 = a.row0 + (uint64_t)blockIdx.x * R, r = r0 + threadIdx.x / G;
+    if (r0 >= rows) return;
     if (G <= 64 && r >= rows) return;                        // (with G > 64 a workgroup is one row)
     const uint32_t t = threadIdx.x % G;
     const uint64_t call = a.drop.below ? call_number(a.drop) : 0;

@@ -125,3 +125,23 @@ def test_quotients_next_to_a_border_are_rounded_by_way_of_fp32():
                 assert torch.equal(got[k, r, :cols] * (-1.0) ** r, want), (K, k, r, int((got[k, r, :cols] * (-1.0) ** r != want).sum()))
                 assert bool((got[k, r, cols:] == 0).all())
         m.close()
+
+
+# ---- more rows than a launch has threads for ------------------------------------------------------------------------------------
+def test_a_norm_of_more_rows_than_one_launch_holds():
+    """2^28 + 2^20 + 7 rows of eight columns, sixteen threads each: the second launch goes on where the first ends."""
+    gen, period, times, tail = generator(51), 1 << 20, 257, 7
+    m = Model(1, [(8,)], "bf16", gen, plus=1.0)
+    n = period * times + tail
+    part = torch.randn(period, 8, generator=gen, device=DEV).bfloat16()
+    want, y = torch.empty_like(part), torch.full((n + 1, 8), 77.0, dtype=torch.bfloat16, device=DEV)
+    m.ctx.rms_norm(0, [period], (part.data_ptr(), 0, 8), (want.data_ptr(), 0, 8))
+    x = torch.empty(n, 8, dtype=torch.bfloat16, device=DEV)
+    x[: period * times].view(times, period, 8).copy_(part.expand(times, period, 8))
+    x[period * times:] = part[:tail]
+    m.ctx.rms_norm(0, [n], (x.data_ptr(), 0, 8), (y.data_ptr(), 0, 8))
+    torch.cuda.synchronize()
+    for i in range(times):
+        assert torch.equal(y[i * period: (i + 1) * period], want), i
+    assert torch.equal(y[period * times: n], want[:tail]) and bool((y[n] == 77.0).all())
+    m.close()
