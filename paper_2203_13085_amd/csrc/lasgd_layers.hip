@@ -450,9 +450,12 @@ template <int FORM> bool launch_loose(const Gated &d, const ProductArgs &a, bool
         b.tiles = b.tiles_m * ceil_div(N, FORM == FWD ? T / 2 : T);
         if (!go || !fits((uint64_t)b.tiles * d.v.K, 256)) return fits((uint64_t)b.tiles * d.v.K, 256);
         const dim3 grid(b.tiles * d.v.K, 1, FORM == DW ? 2 : 1);
+        // dg and du lie in the workspace, aligned; an aligned x has whole eights of columns, and so have the weights
         two_flags(vm, vn, [&](auto m, auto n) {
-            if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n, T>), grid, dim3(256), 0, st, b);
-            else hipLaunchKernelGGL((product_kernel<false, FORM, m, n, T>), grid, dim3(256), 0, st, b);
+            if constexpr (FORM == FWD ? !m || n : m) {
+                if (d.v.bf16) hipLaunchKernelGGL((product_kernel<true, FORM, m, n, T>), grid, dim3(256), 0, st, b);
+                else hipLaunchKernelGGL((product_kernel<false, FORM, m, n, T>), grid, dim3(256), 0, st, b);
+            }
         });
         return true;
     };

@@ -1,6 +1,7 @@
 """The layers' launches, on the CPU: a launch has fewer than 2^32 threads along x. Dropout and norms of more rows than one holds take several, which
 cover every row once; a gated block of more tiles is refused before anything is launched."""
 import os
+import re
 import subprocess
 
 import pytest
@@ -73,3 +74,12 @@ def test_a_product_beyond_a_launch_is_refused_before_the_first(ask, what, storag
         assert st == B.OK and launches and all(0 < blocks * threads <= MOST for blocks, threads, _ in launches)
     else:
         assert st == B.ERR_UNSUPPORTED and not launches
+
+
+def test_every_product_kernel_can_be_reached(tmp_path):
+    """Aligned sides imply each other (an aligned x whole eights of columns; dg and du always are), so no kernel is there for the rest."""
+    obj = str(tmp_path / "layers.o")
+    _host_object(build_mod.LAYERS_SRC, obj)
+    names = set(re.findall(r"__device_stub__product_kernel<(.*?)>\(", subprocess.check_output(["nm", "-C", obj], text=True)))
+    forms = [(0, a, b) for a, b in (("true", "true"), ("false", "true"), ("false", "false"))] + [(f, "true", b) for f in (1, 2) for b in ("true", "false")]
+    assert names == {f"{t}, {f}, {a}, {b}, {tile}u" for t in ("true", "false") for f, a, b in forms for tile in (64, 128)}
