@@ -93,7 +93,7 @@ def _rows_of(rows, g):
         return g
     at = torch.arange(rows.most, device=g.device)
     there = torch.stack([at < n for n in rows.counts])
-    return torch.where(there[:, :, None], g.reshape(rows.K, rows.most, -1), 0).view(g.shape)
+    return torch.where(there[:, :, None], g.reshape(rows.K, rows.most, g.shape[-1]), 0).view(g.shape)
 
 
 class RmsNorm(torch.autograd.Function):

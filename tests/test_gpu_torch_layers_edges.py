@@ -171,3 +171,19 @@ def test_a_repeated_forward_pass_needs_its_call_numbers(reentrant):
     loss.backward()
     torch.cuda.synchronize()
     opt.close()
+
+
+# ---- batches without rows -------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [None, [0, 0]])
+def test_a_batch_without_rows_has_a_backward_pass(rows):
+    K, D, H = 2, 32, 24
+    replicas, opt = make(K, D, H)
+    x, res = (torch.randn(K, 0, D, device=DEV, requires_grad=True) for _ in range(2))
+    opt.zero_grad()
+    y, h = opt.rms_norm("norm", x, res, p=0.5, rows=rows)
+    a = opt.gated("gate.weight", "up.weight", y, rows=rows)
+    d = opt.dropout(h, 0.5, res, rows=rows)
+    (a.sum() + d.sum()).backward()
+    assert x.grad.shape == res.grad.shape == (K, 0, D) and a.shape == (K, 0, H)
+    assert all(bool(q.grad.eq(0).all()) for m in replicas for q in m.parameters())
+    opt.close()
