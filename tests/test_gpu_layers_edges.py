@@ -48,6 +48,39 @@ def test_slopes_of_large_arguments(act, storage):
         within(slope[:, j], want, bound, (act, j))
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_small_values_of_an_activation_keep_their_bits(act):
+    """a = f(v) for v = -12 to -0.01, in fp32, within roundings of the VALUE: forms that subtract from 1 lose all of it.
+
+    The value goes with exp(-|z|), z being v, v^2 / 2 or sqrt(8 / pi) (v + 0.044715 v^3): a relative error d of z's own is |z| d of the value. z is made in
+    six roundings at most (0.044715, that times v, times v again, the sum, sqrt(8 / pi), the product; gelu: v / sqrt(2) in two, and erfc moves 2 x^2 + 1
+    times as much as x does, which is less than six times v^2 / 2 + 1). 24 for the exponential or erfc (a few steps of 2 U), the division and the products.
+    A factor 1 / (1 + exp(-z)) below 2^-126, fp32's least normal number, may be off by as much as it is."""
+    values = [-12.0 + 0.0625 * i for i in range(192)]
+    m = Model(1, [(8, 8), (8, 8)], "f32", generator(0))
+    m.w[0][1].zero_(), m.w[1][1].zero_()
+    m.w[0][1][0, :, 0] = 1.0                                 # g = x[0]
+    m.w[1][1][0, :, 1] = 1.0                                 # u = x[1]
+    rows = [len(values)]
+    x, a = Act(rows, 8, m.dt), Act(rows, 8, m.dt)
+    x[0].zero_()
+    x[0][:, 0] = torch.tensor(values, device=DEV)
+    x[0][:, 1] = 1.0
+    m.ctx.gated(0, 1, rows, 8, x.at, a.at, activation=ACTS[act])
+    torch.cuda.synchronize()
+    v = x[0][:, 0].double()
+    if act == "silu":
+        want, moves = v * torch.sigmoid(v), v.abs()
+    elif act == "gelu":
+        want, moves = 0.5 * v * torch.special.erfc(-v / math.sqrt(2.0)), v * v / 2 + 1
+    else:
+        z = math.sqrt(8 / math.pi) * (v + 0.044715 * v ** 3)
+        want, moves = v * torch.sigmoid(z), z.abs()
+    for j in range(8):
+        within(a[0][:, j], want, (24 + 6 * moves) * U * want.abs() + v.abs() * 2.0 ** -126, (act, j))
+    m.close()
+
+
 # ---- rows that overlap ----------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,stride", [([40, 37], 8), ([70, 1], 0), ([50, 33], 56), ([1, 1], 64), ([1, 0], 0), ([300, 290], 8), ([20, 3], 8)])

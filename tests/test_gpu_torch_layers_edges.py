@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests.layers_util import DEV
-from tests.test_gpu_torch_layers import make
+from tests.test_gpu_torch_layers import close, forward64, make
 
 pytestmark = pytest.mark.gpu
 
@@ -186,4 +186,40 @@ def test_a_batch_without_rows_has_a_backward_pass(rows):
     (a.sum() + d.sum()).backward()
     assert x.grad.shape == res.grad.shape == (K, 0, D) and a.shape == (K, 0, H)
     assert all(bool(q.grad.eq(0).all()) for m in replicas for q in m.parameters())
+    opt.close()
+
+
+# ---- unlike numbers of rows -------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D,H,R,rows", [(40, 24, 12, [12, 0, 5]), (64, 88, 70, [1, 70, 33]), (33, 17, 9, [0, 2, 9])])
+def test_ragged_rows_against_64_bits(D, H, R, rows, dtype):
+    """Outputs and all gradients of every replica's rows, as if it were alone with them."""
+    K, p, calls = 3, 0.25, (11, 12)
+    replicas, opt = make(K, D, H, dtype, seed=31)
+    x, res, dy = (torch.randn(K, R, D, device=DEV).to(dtype) for _ in range(3))
+    for k, n in enumerate(rows):
+        x[k, n:], res[k, n:], dy[k, n:] = float("nan"), float("inf"), float("nan")       # counts for nothing
+    downs = [m.down.weight for m in replicas]
+
+    x.requires_grad_(), res.requires_grad_()
+    opt.zero_grad()
+    y, h = opt.rms_norm("norm", x, res, p=p, rows=rows, call=calls[0], eps=1e-5)
+    a = opt.gated("gate.weight", "up.weight", y, rows=rows)
+    out = opt.dropout(torch.stack([a[k] @ downs[k].T for k in range(K)]), p, h, rows=rows, call=calls[1])
+    out.backward(dy)
+    out = out.detach()
+    for k, (n, m) in enumerate(zip(rows, replicas)):
+        assert all(bool((t[k, n:] == 0).all()) for t in (out, x.grad, res.grad))
+        if not n:
+            assert all(bool(q.grad.eq(0).all()) for q in m.parameters())
+            continue
+        W = {name: q.detach().double().requires_grad_() for name, q in m.named_parameters()}
+        xk, rk = x[k, :n].detach().double().requires_grad_(), res[k, :n].detach().double().requires_grad_()
+        want = forward64(W, k, xk, rk, p, calls, 31)
+        want.backward(dy[k, :n].double())
+        close(out[k, :n], want, dtype, D + H, "out")
+        for name, q in m.named_parameters():
+            close(q.grad, W[name].grad, dtype, D + H + 2 * n, name)
+        close(x.grad[k, :n], xk.grad, dtype, 2 * (D + H), "dx")
+        close(res.grad[k, :n], rk.grad, dtype, 2 * (D + H), "dres")
     opt.close()
