@@ -199,8 +199,8 @@ template <uint32_t FM, uint32_t FN> __device__ __forceinline__ void fold(f32x4 (
 // ---- any size, stride and alignment ------------------------------------------------------------------------------------------
 // Tiles of T x T (FWD: half of the columns gate's, half up's), four waves, 32 of the contraction at a time; what is outside is zero in LDS.  The next 32 are asked for, in
 // the widest accesses that the alignment allows, before these are multiplied, and go into the other of two buffers after that.  bf16, K = 8, 2048 rows,
-// 2047 x 5503: forward 1950 us, dx 1836, weights 1381 (380 to 540 TFLOP/s; with tiles in the order of rows and replicas spread over all XCDs 2083, 3346, 2281);
-// fp32, K = 4, 1023 rows, 1023 x 2815 487, 480, 448.
+// 2047 x 5503: forward 1918 us, dx 1829, weights 1343 (385 to 550 TFLOP/s; with tiles in the order of rows and replicas spread over all XCDs 2083, 3346, 2281);
+// fp32, K = 4, 1023 rows, 1023 x 2815 488, 477, 447 (a chip at rest; behind others of their kind 8 % more).
 constexpr uint32_t kDeep = 32;
 
 // Eight elements of a side's tile next to each other in memory: element (i, c) of i < ni, c < nc is at p + i * stride + c (ALONG) or p + c * stride + i.  A thread has
@@ -217,8 +217,9 @@ __device__ __forceinline__ Raw8<BF16> ask(const char *p, int64_t stride, int64_t
 template <bool ALONG> __device__ __forceinline__ uint32_t own_row() { return ALONG ? threadIdx.x >> 2 : (threadIdx.x & 7u) * 8u; }
 template <bool ALONG> __device__ __forceinline__ uint32_t own_deep() { return ALONG ? (threadIdx.x & 3u) * 8u : threadIdx.x >> 3; }
 
+// (fp32 with its second accumulator: two workgroups a CU, or the 128-tiles take 269 to 285 registers and a CU has one: that forward product 640 us.)
 template <bool BF16, int FORM, bool VM, bool VN, uint32_t T>
-__global__ __launch_bounds__(256) void product_kernel(const ProductArgs a)
+__global__ __launch_bounds__(256, BF16 ? 1 : 2) void product_kernel(const ProductArgs a)
 {
     constexpr uint32_t ES = Width<BF16>::bytes, LP = kDeep / Width<BF16>::piece, R = T / 64u, F = T / 32u, NT = FORM == FWD ? T / 2u : T, SIDE = T * LP * 16u;
     constexpr bool ALONG_M = FORM != DW, ALONG_N = FORM == FWD;

@@ -459,8 +459,9 @@ template <int FORM> bool launch_loose(const Gated &d, const ProductArgs &a, bool
         });
         return true;
     };
-    // us forward / dx / weights, tiles of 128 and of 64: bf16, K = 8, 2048 rows, 2047 x 5503 1923 / 1831 / 1349 and 3433 / 3154 / 2137; fp32, K = 4, 1023 rows, 1023 x 2815
-    // 531 / 504 / 485 and 550 / 539 / 542; K = 3, up to 333 rows, 515 x 1030 forward 58 and 43.
+    // us forward / dx / weights, tiles of 128 and of 64, behind others of their kind (a chip at rest clocks higher: fp32 488 / 477 / 447): bf16, K = 8, 2048 rows,
+    // 2047 x 5503 1942 / 1828 / 1348 and 3487 / 3170 / 2158; fp32, K = 4, 1023 rows, 1023 x 2815 528 / 510 / 486 and 549 / 537 / 544; K = 8, 700 rows, 1535 x 1901
+    // 756 / 896 / 680 and 739 / 772 / 736 (of dx there are 576 tiles of 128 in 512 places: a second round for 64); K = 3, up to 333 rows, 515 x 1030 61 / 188 / 60 and 46 / 75 / 38.
     if (tiles_of<FORM>(d, a.cols, 128, FORM == FWD ? 64 : 128) >= 2 * kCus) return launch(std::integral_constant<uint32_t, 128>{});
     return launch(std::integral_constant<uint32_t, 64>{});
 }

@@ -83,3 +83,18 @@ def test_every_product_kernel_can_be_reached(tmp_path):
     names = set(re.findall(r"__device_stub__product_kernel<(.*?)>\(", subprocess.check_output(["nm", "-C", obj], text=True)))
     forms = [(0, a, b) for a, b in (("true", "true"), ("false", "true"), ("false", "false"))] + [(f, "true", b) for f in (1, 2) for b in ("true", "false")]
     assert names == {f"{t}, {f}, {a}, {b}, {tile}u" for t in ("true", "false") for f, a, b in forms for tile in (64, 128)}
+
+
+def test_two_workgroups_of_the_large_fp32_tile_fit_on_a_cu(tmp_path):
+    """Registers and LDS of the unaligned product, whose second accumulator is a quarter of them."""
+    src, out = str(tmp_path / "kernels.hip"), str(tmp_path / "kernels.s")
+    root = os.path.dirname(HERE)
+    with open(src, "w") as f:
+        f.write(f'#include "{root}/paper_2203_13085_amd/csrc/lasgd_gated.hip.h"\nnamespace lasgd {{\n' + "".join(
+            f"template __global__ void product_kernel<false, {form}, {m}, false, 128>(const ProductArgs);\n" for form, m in (("FWD", "false"), ("DX", "true"), ("DW", "true"))) + "}\n")
+    flags = [f for f in build_mod.FLAGS if f not in ("-shared", "-fPIC")]
+    subprocess.check_call([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")] + flags + ["--cuda-device-only", "-S", "-o", out, src], stderr=subprocess.DEVNULL)
+    text = open(out).read()
+    vgprs, lds = ([int(v) for v in re.findall(r"\.amdhsa_%s (\d+)" % name, text)] for name in ("next_free_vgpr", "group_segment_fixed_size"))
+    assert len(vgprs) == len(lds) == 3 and max(vgprs) <= 256 and max(lds) <= 80 << 10
+    assert re.findall(r"\.amdhsa_private_segment_fixed_size (\d+)", text) == ["0"] * 3
