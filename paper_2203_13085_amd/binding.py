@@ -186,8 +186,8 @@ class Context:
         self._act_refs = [ctypes.byref(r) for r in self._acts]
         self._drop_arg = Drop()
         self._drop_ref = ctypes.byref(self._drop_arg)
-        self.bound_params = [None] * self.K       # per replica: the addresses in effect (ctypes arrays)
-        self.bound_grads = [None] * self.K
+        self.bound_params = np.zeros((len(self.numels), self.K), dtype=np.uint64)     # the parameter addresses in effect, tensor by tensor
+        self.bound_grads = [None] * self.K        # per replica: the gradient addresses in effect (a ctypes array)
 
     # -- plumbing ---------------------------------------------------------
     def _check(self, st: int) -> None:
@@ -217,7 +217,7 @@ class Context:
         pa = (ctypes.c_void_p * n)(*params)
         ga = (ctypes.c_void_p * n)(*grads)
         self._check(self._L.lasgd_bind(self._h, k, pa, ga))
-        self.bound_params[k], self.bound_grads[k] = pa, ga
+        self.bound_params[:, k], self.bound_grads[k] = params, ga
 
     def init_master(self) -> None:
         self._check(self._L.lasgd_init_master(self._h))

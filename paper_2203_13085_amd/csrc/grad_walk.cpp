@@ -1,9 +1,11 @@
-// A walk over a list of torch parameters' gradients in native code: p.grad costs 95 ns from Python, and an optimizer
+// Walks over lists of torch parameters and their gradients in native code: p.grad costs 95 ns from Python, and an optimizer
 // over K replicas asks for hundreds of them twice an iteration (632 tensors: 60 us to see that none is
-// missing, 60 more to gather them).  Host code only; nothing is kept between calls.
+// missing, 60 more to gather them); a layer of 64 replicas looks at 64 weights before each pass, 0.34 us each from Python.
+// Host code only; nothing is kept between calls.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <c10/core/impl/COW.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/variable.h>
 
@@ -86,7 +88,41 @@ PyObject *state(PyObject *, PyObject *args)
     return PyLong_FromLong(found);
 }
 
+// placed(owners, leaves, params, addresses, elements, dtype) -> whether every parameter is what its owner (a dict) holds under its name, and lies, dense and of
+// this type and so many elements, at its address.
+PyObject *placed(PyObject *, PyObject *args)
+{
+    PyObject *owners, *leaves, *params, *addresses, *dtype;
+    long long elements;
+    if (!PyArg_ParseTuple(args, "O!O!O!OLO", &PyList_Type, &owners, &PyList_Type, &leaves, &PyList_Type, &params, &addresses, &elements, &dtype)) return nullptr;
+    const Py_ssize_t n = PyList_GET_SIZE(params);
+    Column address;
+    if (!address.take(addresses, n, "one address for every parameter")) return nullptr;
+    if (!address.at || PyList_GET_SIZE(owners) != n || PyList_GET_SIZE(leaves) != n || !THPDtype_Check(dtype)) {
+        PyErr_SetString(PyExc_ValueError, "one owner, name and address for every parameter, and a dtype");
+        return nullptr;
+    }
+    try {
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            PyObject *o = PyList_GET_ITEM(params, i), *owner = PyList_GET_ITEM(owners, i);
+            if (!PyDict_Check(owner) || !THPVariable_Check(o)) Py_RETURN_FALSE;
+            const PyObject *held = PyDict_GetItemWithError(owner, PyList_GET_ITEM(leaves, i));
+            if (!held && PyErr_Occurred()) return nullptr;
+            if (held != o) Py_RETURN_FALSE;
+            const at::Tensor &p = THPVariable_Unpack(o);
+            if (p.layout() != c10::kStrided || p.scalar_type() != reinterpret_cast<THPDtype *>(dtype)->scalar_type || p.numel() != elements || !p.is_contiguous() ||
+                (uint64_t)(uintptr_t)p.const_data_ptr() != address.at[i])
+                Py_RETURN_FALSE;
+        }
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+    Py_RETURN_TRUE;
+}
+
 PyMethodDef methods[] = {{"state", state, METH_VARARGS, "What a list of parameters' gradients are: 0 plain, 1 other, 2 one is missing."},
+                         {"placed", placed, METH_VARARGS, "Whether parameters are where they were bound."},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_grad_walk", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -94,7 +94,8 @@ class LASGD:
         self.grad_norms = torch.zeros(len(self.replicas), device=dev)
         self.device, self.dtype = dev, dtype
         self._names = [n for n, p in self.replicas[0].named_parameters() if p.requires_grad]
-        self._places = [[_place(r, n) for n, p in r.named_parameters() if p.requires_grad] for r in self.replicas]
+        places = [[_place(r, n) for n, p in r.named_parameters() if p.requires_grad] for r in self.replicas]
+        self._places = [([owner for owner, _ in at], [leaf for _, leaf in at], list(ps)) for at, ps in zip(zip(*places), zip(*self.params))]
         self.seed, self._masks, self._recorded = int(seed), 0, 0                # dropouts so far, eager and recorded
         self.mask_counter = torch.zeros(1, dtype=torch.int64, device=dev)        # added to the call numbers of recorded masks
         self.main = torch.cuda.Stream(device=dev)
@@ -217,12 +218,15 @@ class LASGD:
         # The kernels read the memory that was bound.  A parameter that lives elsewhere by now (p.data = ..., to(), load_state_dict(assign=True)) would
         # leave them with old weights, or with memory that something else has.
         for t in tensors:
-            for (owner, leaf), ps, at in zip((places[t] for places in self._places), self.params, self.ctx.bound_params):
-                p = ps[t]
-                if (owner.get(leaf) is not p or p.data_ptr() != at[t] or p.dtype != self.dtype or not p.is_contiguous()
-                        or p.numel() != self.ctx.numels[t]):
-                    raise RuntimeError(f"{self._names[t]} of a replica is not the parameter, or not the memory, that was bound "
-                                       "(replicas whose parameters are replaced need a new LASGD)")
+            bound, n = self.ctx.bound_params[t], self.ctx.numels[t]
+            if _walk:
+                there = _walk.placed(*self._places[t], bound, n, self.dtype)
+            else:
+                there = all(owner.get(leaf) is p and p.data_ptr() == at and p.numel() == n and p.dtype == self.dtype and p.is_contiguous()
+                            for owner, leaf, p, at in zip(*self._places[t], bound.tolist()))
+            if not there:
+                raise RuntimeError(f"{self._names[t]} of a replica is not the parameter, or not the memory, that was bound "
+                                   "(replicas whose parameters are replaced need a new LASGD)")
 
     def _grads_to_add_to(self, t: int) -> List[torch.Tensor]:
         grads = [ps[t].grad for ps in self.params]

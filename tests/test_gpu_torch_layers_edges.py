@@ -4,6 +4,7 @@ import gc
 import pytest
 import torch
 
+from paper_2203_13085_amd import torch_api
 from tests.layers_util import DEV
 from tests.test_gpu_torch_layers import close, forward64, make
 
@@ -35,13 +36,16 @@ def _fewer(opt, m):
     m.gate.weight.data = m.gate.weight.data[:4]             # the same address
 
 
+@pytest.mark.parametrize("native", [True, False])
 @pytest.mark.parametrize("replica", [0, 1])
 @pytest.mark.parametrize("change", [_other_data, _other_parameter, _assigned, _other_type, _other_layout, _fewer])
-def test_a_weight_that_moved_is_refused(change, replica):
+def test_a_weight_that_moved_is_refused(change, replica, native, monkeypatch):
     """Forward passes, with and without gradients, and the backward pass of a call that was made before. What was bound stays alive here, so that
     a call that goes wrong reads old weights and nothing worse."""
     K, D, H = 2, 32, 32
     replicas, opt = make(K, D, H)
+    if not native:
+        monkeypatch.setattr(torch_api, "_walk", None)       # the class does without it where it is not built
     alive = [t for m in replicas for q in m.parameters() for t in (q.detach(), q.grad.detach())]
     old = [(m, dict(m._parameters), {n: dict(c._parameters) for n, c in m.named_children()}, [q.data for q in m.parameters()]) for m in replicas]
     x = torch.randn(K, 4, D, device=DEV)

@@ -190,3 +190,63 @@ def test_the_torch_class_works_without_the_walk(monkeypatch, missing):
         monkeypatch.undo()
         importlib.reload(torch_api)
     assert torch_api._walk is _grad_walk
+
+
+# ---- parameters at the addresses that were bound ------------------------------------------------------------------------------
+def _module(dtype=torch.float32):
+    m = torch.nn.Module()
+    m.a, m.b = P(torch.zeros(4, 4, dtype=dtype)), P(torch.ones(4, 4, dtype=dtype))
+    return m
+
+
+def _placed(m, ps, at, n=16, dtype=torch.float32):
+    return _grad_walk.placed([m._parameters] * 2, ["a", "b"], ps, at, n, dtype)
+
+
+def _moved(m):
+    m.b.data = m.b.data.clone()
+
+
+def _replaced(m):
+    m.b = P(m.b.detach())
+
+
+def _gone(m):
+    del m.b
+
+
+def _shorter(m):
+    m.b.data = m.b.data[:2]
+
+
+def _turned(m):
+    m.b.data = m.b.data.t()
+
+
+@pytest.mark.parametrize("change", [_moved, _replaced, _gone, _shorter, _turned])
+def test_a_parameter_that_is_not_where_it_was_bound(change):
+    m = _module()
+    ps, at = [m.a, m.b], np.array([m.a.data_ptr(), m.b.data_ptr()], dtype=np.uint64)
+    alive = m.b.detach()
+    assert _placed(m, ps, at) and _placed(m, ps, at.tobytes())
+    change(m)
+    assert not _placed(m, ps, at)
+    assert alive.numel() == 16
+
+
+def test_what_the_walk_over_parameters_refuses():
+    m = _module(torch.bfloat16)
+    ps, at = [m.a, m.b], np.array([m.a.data_ptr(), m.b.data_ptr()], dtype=np.uint64)
+    assert _placed(m, ps, at, dtype=torch.bfloat16) and not _placed(m, ps, at) and not _placed(m, ps, at, n=15, dtype=torch.bfloat16)
+    assert not _placed(m, ps, at[::-1].copy(), dtype=torch.bfloat16)
+    for bad in (at[:1].copy(), None):
+        with pytest.raises(ValueError):
+            _placed(m, ps, bad)
+    with pytest.raises(ValueError):
+        _grad_walk.placed([m._parameters], ["a", "b"], ps, at, 16, torch.float32)
+    with pytest.raises(ValueError):
+        _placed(m, ps, at, dtype="float32")
+    with pytest.raises(TypeError):
+        _grad_walk.placed((m._parameters,) * 2, ["a", "b"], ps, at, 16, torch.float32)
+    assert not _grad_walk.placed([m._parameters, 5], ["a", "b"], ps, at, 16, torch.bfloat16)
+    assert not _grad_walk.placed([m._parameters] * 2, ["a", "b"], [m.a, 5], at, 16, torch.bfloat16)
