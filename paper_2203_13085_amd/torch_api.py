@@ -50,10 +50,14 @@ def _load_walk():
 _walk = _load_walk()
 
 
-def _place(module: torch.nn.Module, name: str):
-    """(the parameters of the submodule that owns this one, its name there)."""
+def _place(module: torch.nn.Module, name: str, p: torch.nn.Parameter):
+    """(the parameters of the submodule that owns p, its name there); modules that name their parameters otherwise: p itself."""
     owner, _, leaf = name.rpartition(".")
-    return module.get_submodule(owner)._parameters, leaf
+    try:
+        held = module.get_submodule(owner)._parameters
+    except AttributeError:
+        held = {}
+    return held if held.get(leaf) is p else {leaf: p}, leaf
 
 
 class LASGD:
@@ -94,7 +98,7 @@ class LASGD:
         self.grad_norms = torch.zeros(len(self.replicas), device=dev)
         self.device, self.dtype = dev, dtype
         self._names = [n for n, p in self.replicas[0].named_parameters() if p.requires_grad]
-        places = [[_place(r, n) for n, p in r.named_parameters() if p.requires_grad] for r in self.replicas]
+        places = [[_place(r, n, p) for n, p in r.named_parameters() if p.requires_grad] for r in self.replicas]
         self._places = [([owner for owner, _ in at], [leaf for _, leaf in at], list(ps)) for at, ps in zip(zip(*places), zip(*self.params))]
         self.seed, self._masks, self._recorded = int(seed), 0, 0                # dropouts so far, eager and recorded
         self.mask_counter = torch.zeros(1, dtype=torch.int64, device=dev)        # added to the call numbers of recorded masks

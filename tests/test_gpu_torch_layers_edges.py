@@ -76,6 +76,30 @@ def test_a_weight_that_moved_is_refused(change, replica, native, monkeypatch):
     opt.close()
 
 
+class Renamed(torch.nn.Linear):
+    """A module that names its parameters in its own way."""
+
+    def named_parameters(self, *args, **kwargs):
+        for n, q in super().named_parameters(*args, **kwargs):
+            yield "shard.0." + n, q
+
+
+def test_modules_that_name_their_parameters_in_their_own_way():
+    """The submodule that the name speaks of is not there: the parameter's own place is compared all the same."""
+    replicas = [Renamed(16, 16, bias=False).to(DEV) for _ in range(2)]
+    opt = torch_api.LASGD(replicas, lr=0.1)
+    x = torch.randn(2, 3, 16, device=DEV)
+    opt.zero_grad()
+    assert opt.gated("shard.0.weight", "shard.0.weight", x).shape == (2, 3, 8)          # both weights in one
+    alive = replicas[1].weight.data
+    replicas[1].weight.data = alive.clone()
+    with pytest.raises(RuntimeError, match="bound"):
+        opt.gated("shard.0.weight", "shard.0.weight", x)
+    replicas[1].weight.data = alive
+    opt.step()
+    opt.close()
+
+
 # ---- call numbers of recorded masks ----------------------------------------------------------------------------------------
 def test_masks_of_eager_calls_and_of_two_graphs_never_meet():
     """Two graphs with two and three dropouts, replayed in turn, a third one recorded in between, and eager calls before, between and after: no mask comes twice."""
